@@ -359,6 +359,113 @@ int nova_layer_ratio(nova_ctx* ctx, void* stream, const float* mean_entropy, flo
                      const float* ratio_t, int j, int B, int N, float* ratio_tj, int32_t* k_per_row);
 
 /*
+ * A key/value cache in 4 bits: a quarter of the memory of a bf16 one (dh / 2 + dh / 32 bytes a row against 2 dh), read by
+ * attention as it lies.  Keys and values have one layout, a row per key:
+ *   codes   [B, kv_heads, capacity, dh / 2]   two codes per byte, the even channel in the low nibble; a code is a sign
+ *           (bit 3) and a rank (bits 0-2) on the levels 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ *   scales  [B, kv_heads, capacity, dh / 32]  one byte t per 32 channels (a group): the code's level times 2^(t - 127);
+ *           t = 255 makes every value of the group NaN
+ * A group with largest magnitude a is stored with the smallest e, -124 <= e <= 125, for which a <= 6 * 2^e (t = e + 127),
+ * every value as the nearest level times 2^e, of two the one of even rank, magnitudes past 6 * 2^125 as that.  A group that
+ * holds a NaN or an infinity is stored as NaN (codes 0).  Every value is a bf16 number: reading it back rounds nothing.
+ * dh is 64 or 128; heads that attend share a key head in runs of heads / kv_heads.  All four arrays are the caller's, dense,
+ * 16-byte aligned; B images share one capacity, each may hold a number of rows of its own.
+ * Per-image arrays (..._per_row) are DEVICE int32 [B] or NULL, clamped on the device like those of nova_pruned_block_rows.
+ */
+typedef struct nova_fourbit_cache {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+  int32_t B;
+  int32_t kv_heads;
+  int32_t capacity; /* rows allocated per (image, key head), at most 2^24 */
+  int32_t dh;
+} nova_fourbit_cache;
+
+/* Rows [B, n, heads, dh] in a buffer of the caller's, with strides in elements (any sign is refused but >= 0; the stride of
+ * an extent of 1 is not looked at). */
+typedef struct nova_rows {
+  void* data;
+  int64_t stride_b;
+  int64_t stride_row;
+  int64_t stride_head;
+  int64_t stride_channel;
+} nova_rows;
+
+/*
+ * Quantises n new rows of every image into the cache, behind the rows it has, in one launch.
+ *   k, v            [B, n, kv_heads, dh] in dtype NOVA_F32 | NOVA_BF16, any strides: rows of a projection's output, or the
+ *                   16-bit caches of nova_pruned_block (keys by row, values key-minor)
+ *   n_per_row       rows of image b that are appended (clamped to [0, n]); NULL: n
+ *   kv_len          rows every image has, or the upper bound of kv_len_per_row; kv_len + n <= capacity
+ *   kv_len_per_row  rows of image b (clamped to [0, kv_len]); row s goes to cache row kv_len_per_row[b] + s
+ *   kv_len_next     out DEVICE int32 [B] or NULL: rows image b has afterwards; must not overlap kv_len_per_row or n_per_row
+ * Other rows of the cache are untouched.  n == 0 only writes kv_len_next.
+ */
+int nova_fourbit_append(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int n, const nova_rows* k,
+                        const nova_rows* v, const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row,
+                        int32_t* kv_len_next);
+
+/* The values of n cached rows of every image, from row `first` (first_per_row[b], clamped to [0, first], where given) on, in
+ * dtype, to k and v (either may be NULL) of any strides; no two elements may share an address.  first + n <= capacity.  Slots
+ * past n_per_row[b] get zeros. */
+int nova_fourbit_unpack(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int first, int n,
+                        const int32_t* first_per_row, const int32_t* n_per_row, const nova_rows* k, const nova_rows* v);
+
+/*
+ * Attention of n queries per image over the cached rows, for whole scales and prompts as for single tokens:
+ *   out[b, s, h] = sum_j softmax_j(scale * <q[b, s, h], K[b, g, j]>) V[b, g, j],  g = h / (heads / kv_heads),
+ * over the rows j < kv_len_per_row[b] (NULL: kv_len; clamped to [0, kv_len]), no other mask.
+ *   q          [B, n, heads, dh] in dtype, stride_channel 1, every other stride a multiple of 16 bytes, 16-byte aligned
+ *   n_per_row  live queries of image b (clamped to [0, n]); NULL: n
+ *   out        out [B, n, heads, dh] dense, 16-byte aligned; must not alias q
+ *   lse        out fp32 [B, n, heads] or NULL: ln of the sum of e^(scale * score)
+ *   workspace  of at least nova_fourbit_attention_workspace_bytes, 16-byte aligned (may be NULL where that is 0); calls that
+ *              overlap, captured graphs among them, need one each
+ * Queries past n_per_row[b], and all queries of an image without rows, get zeros and lse = -inf.  NOVA_F32: queries and
+ * probabilities take part with all their 24 bits; NOVA_BF16: probabilities are rounded to bf16 in front of the second product.
+ */
+size_t nova_fourbit_attention_workspace_bytes(const nova_fourbit_cache* cache, int heads, int n, int kv_len);
+int nova_fourbit_attention(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int heads, int n,
+                           const nova_rows* q, const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row, float scale,
+                           void* out, float* lse, void* workspace, size_t workspace_bytes);
+
+/*
+ * Attention weight that the cached rows collect, summed over queries and heads:
+ *   mass[b, j] = m0 + sum_{s, h} exp(scale * <q[b, s, h], K[b, g, j]> - lse[b, s, h])     for j < kv_len_per_row[b]
+ *   mass[b, j] = -1                                                                      for the other j < capacity
+ *   mass_in    fp32 [B, capacity] or NULL: m0 = mass_in[b, j] if that is > 0, else 0 (so a row that was marked -1 when it did
+ *              not exist yet starts from 0); may be the mass array itself
+ *   mass       out fp32 [B, capacity], the scores nova_select ranks for nova_fourbit_evict.  A row that a caller sets to
+ *              +inf in between (recent rows, say) stays at +inf and is kept
+ *   lse        fp32 [B, n, heads], as written by nova_fourbit_attention for the same queries and rows
+ *   workspace  of at least nova_fourbit_mass_workspace_bytes, 16-byte aligned, as above
+ * Everything else as nova_fourbit_attention; queries past n_per_row[b] do not count.  Sums are taken in a fixed order: the same
+ * bits on every run.
+ */
+size_t nova_fourbit_mass_workspace_bytes(const nova_fourbit_cache* cache, int heads, int n, int kv_len);
+int nova_fourbit_mass(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int heads, int n,
+                      const nova_rows* q, const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row, float scale,
+                      const float* lse, const float* mass_in, float* mass, void* workspace, size_t workspace_bytes);
+
+/*
+ * Eviction: the rows in kept_idx move to the front of another cache, in that order.
+ *   src, dst     caches of one B, kv_heads and dh; capacities may differ; no array may be shared
+ *   kept_idx     [B, k] int32 (nova_select of the masses writes it); 0 <= k <= dst->capacity
+ *   k_per_row    NULL, or rows of image b that stay (clamped to [0, k])
+ *   kv_len, kv_len_per_row   rows of src as in nova_fourbit_attention
+ * Image b has m = min(k_per_row[b], kv_len_per_row[b]) rows afterwards: dst row s < m = src row kept_idx[b, s].  An index that is
+ * no row of the image gives a row of zeros, never an access out of bounds.  dst rows from m on are untouched.
+ *   kv_len_next  out DEVICE int32 [B] or NULL: m; must not overlap k_per_row, kv_len_per_row or kept_idx
+ *   mass_src     fp32 [B, src->capacity] or NULL;  mass_dst  out fp32 [B, dst->capacity], with mass_src only: the kept rows'
+ *                masses, -1 from m on; must not alias mass_src
+ */
+int nova_fourbit_evict(nova_ctx* ctx, void* stream, const nova_fourbit_cache* src, const nova_fourbit_cache* dst, int k,
+                       const int32_t* kept_idx, const int32_t* k_per_row, int kv_len, const int32_t* kv_len_per_row,
+                       int32_t* kv_len_next, const float* mass_src, float* mass_dst);
+
+/*
  * Instrumentation (not part of the hot path): per-kernel device timing with HIP events on
  * the caller's stream.  While a stage's bit is set in `stage_mask`, every launch of that
  * stage by the four entry points is bracketed by a pair of events (created on the host as

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import Dict, Optional, Sequence
+from typing import Dict, Optional, Sequence, Union
 
 import torch
 
@@ -39,6 +39,51 @@ class _Variant(C.Structure):
     _fields_ = [("gelu_tanh", C.c_int32), ("qk_norm", C.c_int32), ("qk_scale", C.c_void_p), ("ada", C.c_void_p),
                 ("w_cq", C.c_void_p), ("b_cq", C.c_void_p), ("w_co", C.c_void_p), ("b_co", C.c_void_p),
                 ("k_text", C.c_void_p), ("v_text", C.c_void_p), ("text_len", C.c_int32), ("text_capacity", C.c_int32)]
+
+
+class _FourBitCache(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] +
+                [(n, C.c_int32) for n in ("B", "kv_heads", "capacity", "dh")])
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("stride_b", "stride_row", "stride_head", "stride_channel")]
+
+
+@dataclass
+class FourBitCache:
+    """nova_fourbit_cache: keys and values of B images in 4 bits, uint8 device tensors: codes [B, kv_heads, capacity, dh / 2]
+    and scales [B, kv_heads, capacity, dh / 32] of either."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+    @classmethod
+    def empty(cls, B: int, kv_heads: int, capacity: int, dh: int, device: Union[str, int, torch.device] = "cuda") -> "FourBitCache":
+        """A cache without rows (every value in it reads as zero)."""
+        def half():
+            return (torch.zeros((B, kv_heads, capacity, dh // 2), dtype=torch.uint8, device=device),
+                    torch.full((B, kv_heads, capacity, dh // 32), 127, dtype=torch.uint8, device=device))
+        return cls(*half(), *half())
+
+    @property
+    def capacity(self) -> int:
+        return self.k_codes.shape[2]
+
+    @property
+    def dh(self) -> int:
+        return self.k_codes.shape[3] * 2
+
+    def c_struct(self) -> "_FourBitCache":
+        codes, scales = self.k_codes.shape, self.k_scales.shape
+        if (self.v_codes.shape != codes or self.v_scales.shape != scales or codes[:3] != scales[:3]
+                or codes[3] != 16 * scales[3]):
+            raise ValueError(f"no cache in 4 bits: codes {tuple(codes)}, {tuple(self.v_codes.shape)}, "
+                             f"scales {tuple(scales)}, {tuple(self.v_scales.shape)}")
+        ts = (self.k_codes, self.k_scales, self.v_codes, self.v_scales)
+        assert all(t.dtype == torch.uint8 for t in ts), "codes and scales are uint8"
+        return _FourBitCache(*[_ptr(t) for t in ts], *codes[:3], codes[3] * 2)
 
 
 @dataclass
@@ -138,6 +183,17 @@ def load_library() -> C.CDLL:
     lib.nova_activation_scale.argtypes = [C.POINTER(C.c_double), i32, i32, C.c_double, C.POINTER(i32)]
     lib.nova_scale_ratio.argtypes = [i32, i32, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)]
     lib.nova_layer_ratio.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]
+    cache, rows, sz = C.POINTER(_FourBitCache), C.POINTER(_Rows), C.c_size_t
+    lib.nova_fourbit_append.argtypes = [vp, vp, i32, cache, i32, rows, rows, vp, i32, vp, vp]
+    lib.nova_fourbit_unpack.argtypes = [vp, vp, i32, cache, i32, i32, vp, vp, rows, rows]
+    lib.nova_fourbit_attention.argtypes = [vp, vp, i32, cache, i32, i32, rows, vp, i32, vp, C.c_float, vp, vp, vp, sz]
+    lib.nova_fourbit_mass.argtypes = [vp, vp, i32, cache, i32, i32, rows, vp, i32, vp, C.c_float, vp, vp, vp, vp, sz]
+    lib.nova_fourbit_evict.argtypes = [vp, vp, cache, cache, i32, vp, vp, i32, vp, vp, vp, vp]
+    for f in (lib.nova_fourbit_append, lib.nova_fourbit_unpack, lib.nova_fourbit_attention, lib.nova_fourbit_mass,
+              lib.nova_fourbit_evict):
+        f.restype = i32
+    for f in (lib.nova_fourbit_attention_workspace_bytes, lib.nova_fourbit_mass_workspace_bytes):
+        f.argtypes, f.restype = [cache, i32, i32, i32], sz
     lib.nova_probe.argtypes = [vp, vp, i32, vp, vp, i64, i32, vp, C.POINTER(C.c_double)]
     lib.nova_probe.restype = i32
     lib.nova_profile_stages.restype = i32
@@ -168,6 +224,23 @@ def _ptrs(ts: Sequence[torch.Tensor]) -> "C.Array":
     return (C.c_void_p * len(ts))(*[_ptr(t) for t in ts])
 
 
+def _rows(t: torch.Tensor, heads: int, dh: int, name: str) -> "_Rows":
+    """nova_rows of a [B, n, heads, dh] tensor of any strides."""
+    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != dh:
+        raise ValueError(f"{name}: {tuple(t.shape)}, expected [B, n, {heads}, {dh}]")
+    assert t.is_cuda, "device-resident tensors only"
+    return _Rows(t.data_ptr(), *t.stride())
+
+
+def _shaped(name: str, t: Optional[torch.Tensor], shape: Sequence[int], dtype: torch.dtype) -> Optional[int]:
+    """Pointer of an optional dense tensor that has to have this shape and type."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+    return _ptr(t)
+
+
 def _check_lengths(n: int, **lists):
     """Host arrays the library reads n entries of."""
     for name, ts in lists.items():
@@ -180,10 +253,11 @@ def _check_lengths(n: int, **lists):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream() -> int:
+def _stream(device: Optional[int] = None) -> int:
+    """Handle of the current stream, of the current device or of a given one."""
     if _raw_stream is None:
-        return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+        return (torch.cuda.current_stream() if device is None else torch.cuda.current_stream(device)).cuda_stream
+    return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
 def activation_scale(hbar: Sequence[float], t_est: int, alpha: float) -> int:
@@ -427,6 +501,113 @@ class Nova:
                                               _ptr(x), _ptr(y_kept), _ptr(kept_idx), _ptr(keep_mask),
                                               _ptr(cache_prev), _ptr(out), _ptr(cache_new))
         self._check(rc, "nova_merge_cache_interp")
+
+    # -- a cache in 4 bits ----------------------------------------------------------
+    # These work on the context's device, on that device's current stream, whichever device is current.
+    def _here(self, *ts: Optional[torch.Tensor]):
+        for t in ts:
+            if t is not None and t.device.index != self.device:
+                raise ValueError(f"tensor on {t.device}, context on device {self.device}")
+
+    def fourbit_append(self, cache: FourBitCache, k: torch.Tensor, v: torch.Tensor, kv_len: int,
+                       n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None,
+                       kv_len_next: Optional[torch.Tensor] = None):
+        """Quantises k, v [B, n, kv_heads, dh] (f32|bf16, any strides) behind the images' rows.  kv_len: rows every image
+        has, or the upper bound of kv_len_per_row ([B] int32, like n_per_row and kv_len_next)."""
+        c = cache.c_struct()
+        if k.shape != v.shape or k.dtype != v.dtype or k.shape[0] != c.B:
+            raise ValueError(f"k {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}, {c.B} images in the cache")
+        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, k, v, n_per_row, kv_len_per_row, kv_len_next)
+        kr, vr = _rows(k, c.kv_heads, c.dh, "k"), _rows(v, c.kv_heads, c.dh, "v")
+        rc = self.lib.nova_fourbit_append(
+            self.ctx, _stream(self.device), _dtype_code(k), C.byref(c), k.shape[1], C.byref(kr), C.byref(vr),
+            _shaped("n_per_row", n_per_row, (c.B,), torch.int32), int(kv_len),
+            _shaped("kv_len_per_row", kv_len_per_row, (c.B,), torch.int32),
+            _shaped("kv_len_next", kv_len_next, (c.B,), torch.int32))
+        self._check(rc, "nova_fourbit_append")
+
+    def fourbit_unpack(self, cache: FourBitCache, first: int, k: Optional[torch.Tensor], v: Optional[torch.Tensor],
+                       first_per_row: Optional[torch.Tensor] = None, n_per_row: Optional[torch.Tensor] = None):
+        """Values of cached rows from row `first` on, into k and v [B, n, kv_heads, dh] (f32|bf16, any strides)."""
+        c = cache.c_struct()
+        out = [t for t in (k, v) if t is not None]
+        if not out:
+            return
+        if any(t.shape[:2] != out[0].shape[:2] or t.dtype != out[0].dtype or t.shape[0] != c.B for t in out):
+            raise ValueError(f"outputs {[(tuple(t.shape), t.dtype) for t in out]}, {c.B} images in the cache")
+        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, k, v, first_per_row, n_per_row)
+        kr, vr = (None if t is None else C.byref(_rows(t, c.kv_heads, c.dh, "output")) for t in (k, v))
+        rc = self.lib.nova_fourbit_unpack(
+            self.ctx, _stream(self.device), _dtype_code(out[0]), C.byref(c), int(first), out[0].shape[1],
+            _shaped("first_per_row", first_per_row, (c.B,), torch.int32),
+            _shaped("n_per_row", n_per_row, (c.B,), torch.int32), kr, vr)
+        self._check(rc, "nova_fourbit_unpack")
+
+    def fourbit_attention_workspace_bytes(self, cache: FourBitCache, heads: int, n: int, kv_len: int) -> int:
+        return int(self.lib.nova_fourbit_attention_workspace_bytes(C.byref(cache.c_struct()), heads, n, kv_len))
+
+    def fourbit_attention(self, cache: FourBitCache, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor],
+                          kv_len: int, scale: Optional[float] = None, lse: Optional[torch.Tensor] = None,
+                          n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None):
+        """out [B, n, heads, dh] = attention of q [B, n, heads, dh] (f32|bf16, channels dense) over the cached rows; lse
+        [B, n, heads] f32 or None.  scale: 1 / sqrt(dh) where None."""
+        c = cache.c_struct()
+        B, n, heads, dh = q.shape
+        if B != c.B:
+            raise ValueError(f"{B} images of queries, {c.B} in the cache")
+        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, q, out, lse, workspace, n_per_row,
+                   kv_len_per_row)
+        qr = _rows(q, heads, c.dh, "q")
+        rc = self.lib.nova_fourbit_attention(
+            self.ctx, _stream(self.device), _dtype_code(q), C.byref(c), heads, n, C.byref(qr),
+            _shaped("n_per_row", n_per_row, (B,), torch.int32), int(kv_len),
+            _shaped("kv_len_per_row", kv_len_per_row, (B,), torch.int32), dh ** -0.5 if scale is None else float(scale),
+            _shaped("out", out, q.shape, q.dtype), _shaped("lse", lse, (B, n, heads), torch.float32),
+            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+        self._check(rc, "nova_fourbit_attention")
+
+    def fourbit_mass_workspace_bytes(self, cache: FourBitCache, heads: int, n: int, kv_len: int) -> int:
+        return int(self.lib.nova_fourbit_mass_workspace_bytes(C.byref(cache.c_struct()), heads, n, kv_len))
+
+    def fourbit_mass(self, cache: FourBitCache, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor,
+                     workspace: Optional[torch.Tensor], kv_len: int, scale: Optional[float] = None,
+                     mass_in: Optional[torch.Tensor] = None, n_per_row: Optional[torch.Tensor] = None,
+                     kv_len_per_row: Optional[torch.Tensor] = None):
+        """mass [B, capacity] f32: mass_in (may be the same tensor; None: zeros) plus what the cached rows collect from q; lse
+        as fourbit_attention wrote it."""
+        c = cache.c_struct()
+        B, n, heads, dh = q.shape
+        if B != c.B:
+            raise ValueError(f"{B} images of queries, {c.B} in the cache")
+        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, q, lse, mass, mass_in, workspace, n_per_row,
+                   kv_len_per_row)
+        qr = _rows(q, heads, c.dh, "q")
+        rc = self.lib.nova_fourbit_mass(
+            self.ctx, _stream(self.device), _dtype_code(q), C.byref(c), heads, n, C.byref(qr),
+            _shaped("n_per_row", n_per_row, (B,), torch.int32), int(kv_len),
+            _shaped("kv_len_per_row", kv_len_per_row, (B,), torch.int32), dh ** -0.5 if scale is None else float(scale),
+            _shaped("lse", lse, (B, n, heads), torch.float32), _shaped("mass_in", mass_in, (B, c.capacity), torch.float32),
+            _shaped("mass", mass, (B, c.capacity), torch.float32),
+            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+        self._check(rc, "nova_fourbit_mass")
+
+    def fourbit_evict(self, src: FourBitCache, dst: FourBitCache, kept_idx: torch.Tensor, kv_len: int,
+                      k_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None,
+                      kv_len_next: Optional[torch.Tensor] = None, mass_src: Optional[torch.Tensor] = None,
+                      mass_dst: Optional[torch.Tensor] = None):
+        """Rows kept_idx [B, k] of src to the front of dst, with their masses."""
+        s, d = src.c_struct(), dst.c_struct()
+        k = kept_idx.shape[1]
+        self._here(src.k_codes, src.k_scales, src.v_codes, src.v_scales, dst.k_codes, dst.k_scales, dst.v_codes, dst.v_scales,
+                   kept_idx, k_per_row, kv_len_per_row, kv_len_next, mass_src, mass_dst)
+        rc = self.lib.nova_fourbit_evict(
+            self.ctx, _stream(self.device), C.byref(s), C.byref(d), k, _shaped("kept_idx", kept_idx, (s.B, k), torch.int32),
+            _shaped("k_per_row", k_per_row, (s.B,), torch.int32), int(kv_len),
+            _shaped("kv_len_per_row", kv_len_per_row, (s.B,), torch.int32),
+            _shaped("kv_len_next", kv_len_next, (s.B,), torch.int32),
+            _shaped("mass_src", mass_src, (s.B, s.capacity), torch.float32),
+            _shaped("mass_dst", mass_dst, (s.B, d.capacity), torch.float32))
+        self._check(rc, "nova_fourbit_evict")
 
 
 # ------------------------------------------------------------------------------------

@@ -41,6 +41,82 @@ int set_device(const nova_ctx* ctx) {
   return NOVA_OK;
 }
 
+// Makes the context's device current for a call and puts the caller's back afterwards.
+struct DeviceScope {
+  int before = -1;
+  int rc = NOVA_OK;
+  explicit DeviceScope(const nova_ctx* ctx) {
+    int cur = -1;
+    if (hipGetDevice(&cur) != hipSuccess) { rc = NOVA_ERR_HIP; return; }
+    if (cur == ctx->device) return;
+    if (hipSetDevice(ctx->device) != hipSuccess) { rc = NOVA_ERR_HIP; return; }
+    before = cur;
+  }
+  ~DeviceScope() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Two arrays share a byte.
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  if (!a || !b) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+// A cache in 4 bits.  At most 2^24 rows: a head's codes are 1 GiB, offsets within a head have 32 bits (between heads 64).
+int fourbit_error(const nova_fourbit_cache* c) {
+  if (!c) return NOVA_ERR_INVALID_ARG;
+  if (c->B < 0 || c->kv_heads < 1 || c->capacity < 0) return NOVA_ERR_INVALID_ARG;
+  if (c->dh != 64 && c->dh != 128) return NOVA_ERR_UNSUPPORTED;
+  if (c->B > 65535 || c->kv_heads > 32767 || c->capacity > 1 << 24) return NOVA_ERR_UNSUPPORTED;
+  if (c->B == 0 || c->capacity == 0) return NOVA_OK;
+  for (const void* p : {c->k_codes, c->k_scales, c->v_codes, c->v_scales})
+    if (!p || !aligned16(p)) return NOVA_ERR_INVALID_ARG;
+  return NOVA_OK;
+}
+
+int counts_error(std::initializer_list<const void*> arrays) {
+  for (const void* p : arrays)
+    if (!aligned(p, 4)) return NOVA_ERR_INVALID_ARG;
+  return NOVA_OK;
+}
+
+// Rows [B, n, heads, dh] of the caller's.  vector: channels side by side, everything else a multiple of 16 bytes.
+int rows_error(const nova_rows* r, int dtype, int B, int n, int heads, bool vector) {
+  if (!r->data || !aligned(r->data, vector ? 16 : esize(dtype))) return NOVA_ERR_INVALID_ARG;
+  const int64_t stride[4] = {r->stride_b, r->stride_row, r->stride_head, r->stride_channel};
+  const int64_t extent[4] = {B, n, heads, 2};
+  for (int i = 0; i < 4; ++i) {
+    if (extent[i] <= 1) continue;
+    if (stride[i] < 0 || stride[i] > (int64_t)1 << 40) return NOVA_ERR_INVALID_ARG;
+    if (vector && (i == 3 ? stride[i] != 1 : stride[i] * (int64_t)esize(dtype) % 16 != 0)) return NOVA_ERR_INVALID_ARG;
+  }
+  return NOVA_OK;
+}
+
+// Strides of extents of 1 mean nothing and may be anything: zero, so that no kernel multiplies by them.
+nova_rows settled(const nova_rows& r, int B, int n, int heads) {
+  nova_rows s = r;
+  if (B <= 1) s.stride_b = 0;
+  if (n <= 1) s.stride_row = 0;
+  if (heads <= 1) s.stride_head = 0;
+  return s;
+}
+
+// What nova_fourbit_attention and nova_fourbit_mass have in common; 1: nothing to do.
+int fourbit_query_error(int dtype, const nova_fourbit_cache* cache, int heads, int n, const nova_rows* q, int kv_len) {
+  if (!valid_dtype(dtype)) return NOVA_ERR_UNSUPPORTED;
+  if (int rc = fourbit_error(cache)) return rc;
+  if (heads < 1 || n < 0 || kv_len < 0 || kv_len > cache->capacity || heads % cache->kv_heads != 0) return NOVA_ERR_INVALID_ARG;
+  if ((int64_t)cache->B * heads * std::max(n, 1) > (int64_t)1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (cache->B == 0 || n == 0) return NOVA_OK;
+  if (!q) return NOVA_ERR_INVALID_ARG;
+  return rows_error(q, dtype, cache->B, n, heads, true);
+}
+
 }  // namespace
 
 BlockWorkspace carve_workspace(const nova_block_shape& s, void* base) {
@@ -437,6 +513,140 @@ int nova_merge_cache_rows(nova_ctx* ctx, void* stream, int dtype, int interp, in
   hipError_t e = launch_merge(static_cast<hipStream_t>(stream), dtype, interp, B, C, h, w, hp, wp, k, x, y_kept, kept_idx,
                               keep_mask, cache_prev, out, cache_new, k_per_row);
   return e == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+int nova_fourbit_append(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int n, const nova_rows* k,
+                        const nova_rows* v, const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row,
+                        int32_t* kv_len_next) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  if (!valid_dtype(dtype)) return NOVA_ERR_UNSUPPORTED;
+  if (int rc = fourbit_error(cache)) return rc;
+  if (n < 0 || kv_len < 0 || (int64_t)kv_len + n > cache->capacity) return NOVA_ERR_INVALID_ARG;
+  if (int rc = counts_error({n_per_row, kv_len_per_row, kv_len_next})) return rc;
+  const int B = cache->B, hk = cache->kv_heads;
+  for (const void* p : {n_per_row, kv_len_per_row})
+    if (overlap(kv_len_next, (size_t)B * 4, p, (size_t)B * 4)) return NOVA_ERR_INVALID_ARG;
+  if ((int64_t)B * hk * n > (int64_t)1 << 36) return NOVA_ERR_UNSUPPORTED;
+  if (B == 0) return NOVA_OK;
+  nova_rows ks = {}, vs = {};
+  if (n > 0) {
+    if (!k || !v) return NOVA_ERR_INVALID_ARG;
+    for (const nova_rows* r : {k, v})
+      if (int rc = rows_error(r, dtype, B, n, hk, false)) return rc;
+    ks = settled(*k, B, n, hk);
+    vs = settled(*v, B, n, hk);
+  }
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  return launch_fourbit_append(static_cast<hipStream_t>(stream), dtype, *cache, n, &ks, &vs, n_per_row, kv_len, kv_len_per_row,
+                               kv_len_next) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+int nova_fourbit_unpack(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int first, int n,
+                        const int32_t* first_per_row, const int32_t* n_per_row, const nova_rows* k, const nova_rows* v) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  if (!valid_dtype(dtype)) return NOVA_ERR_UNSUPPORTED;
+  if (int rc = fourbit_error(cache)) return rc;
+  if (n < 0 || first < 0 || (int64_t)first + n > cache->capacity) return NOVA_ERR_INVALID_ARG;
+  if (int rc = counts_error({first_per_row, n_per_row})) return rc;
+  const int B = cache->B, hk = cache->kv_heads;
+  if ((int64_t)B * hk * n > (int64_t)1 << 36) return NOVA_ERR_UNSUPPORTED;
+  if (B == 0 || n == 0 || (!k && !v)) return NOVA_OK;
+  nova_rows out[2] = {};
+  const nova_rows* in[2] = {k, v};
+  for (int i = 0; i < 2; ++i) {
+    if (!in[i]) continue;
+    if (int rc = rows_error(in[i], dtype, B, n, hk, false)) return rc;
+    out[i] = settled(*in[i], B, n, hk);
+    if (out[i].stride_channel == 0 || (n > 1 && out[i].stride_row == 0) || (hk > 1 && out[i].stride_head == 0) ||
+        (B > 1 && out[i].stride_b == 0))
+      return NOVA_ERR_INVALID_ARG;
+  }
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  return launch_fourbit_unpack(static_cast<hipStream_t>(stream), dtype, *cache, first, n, first_per_row, n_per_row, &out[0],
+                               &out[1]) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+size_t nova_fourbit_attention_workspace_bytes(const nova_fourbit_cache* cache, int heads, int n, int kv_len) {
+  if (!cache || heads < 1 || n < 1 || kv_len < 0 || cache->B < 1 || cache->kv_heads < 1 || heads % cache->kv_heads != 0 ||
+      (cache->dh != 64 && cache->dh != 128) || (int64_t)cache->B * heads * n > (int64_t)1 << 30)
+    return 0;
+  return fourbit_attention_workspace_bytes(*cache, heads, n, kv_len);
+}
+
+int nova_fourbit_attention(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int heads, int n,
+                           const nova_rows* q, const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row, float scale,
+                           void* out, float* lse, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  if (int rc = fourbit_query_error(dtype, cache, heads, n, q, kv_len)) return rc;
+  if (int rc = counts_error({n_per_row, kv_len_per_row, lse})) return rc;
+  if (cache->B == 0 || n == 0) return NOVA_OK;
+  if (!out || !aligned16(out) || out == q->data) return NOVA_ERR_INVALID_ARG;
+  const size_t need = nova_fourbit_attention_workspace_bytes(cache, heads, n, kv_len);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace))) return NOVA_ERR_WORKSPACE;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  return launch_fourbit_attention(ctx, static_cast<hipStream_t>(stream), dtype, *cache, heads, n,
+                                  settled(*q, cache->B, n, heads), n_per_row, kv_len, kv_len_per_row, scale * kAttnLog2e, out,
+                                  lse, workspace) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+size_t nova_fourbit_mass_workspace_bytes(const nova_fourbit_cache* cache, int heads, int n, int kv_len) {
+  if (!cache || heads < 1 || n < 1 || kv_len < 0 || cache->B < 1 || cache->kv_heads < 1 || heads % cache->kv_heads != 0 ||
+      (cache->dh != 64 && cache->dh != 128) || (int64_t)cache->B * heads * n > (int64_t)1 << 30)
+    return 0;
+  return fourbit_mass_workspace_bytes(*cache, heads, n, kv_len);
+}
+
+int nova_fourbit_mass(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int heads, int n,
+                      const nova_rows* q, const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row, float scale,
+                      const float* lse, const float* mass_in, float* mass, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  if (int rc = fourbit_query_error(dtype, cache, heads, n, q, kv_len)) return rc;
+  if (int rc = counts_error({n_per_row, kv_len_per_row, lse, mass_in, mass})) return rc;
+  if (cache->B == 0 || cache->capacity == 0) return NOVA_OK;
+  if (!mass || (n > 0 && !lse)) return NOVA_ERR_INVALID_ARG;
+  const size_t mass_bytes = (size_t)cache->B * cache->capacity * 4;
+  if (mass_in != mass && overlap(mass_in, mass_bytes, mass, mass_bytes)) return NOVA_ERR_INVALID_ARG;
+  const size_t need = nova_fourbit_mass_workspace_bytes(cache, heads, n, kv_len);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace))) return NOVA_ERR_WORKSPACE;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  const nova_rows none = {};
+  return launch_fourbit_mass(ctx, static_cast<hipStream_t>(stream), dtype, *cache, heads, n,
+                             n > 0 ? settled(*q, cache->B, n, heads) : none, n_per_row, kv_len, kv_len_per_row,
+                             scale * kAttnLog2e, lse, mass_in, mass, workspace) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+int nova_fourbit_evict(nova_ctx* ctx, void* stream, const nova_fourbit_cache* src, const nova_fourbit_cache* dst, int k,
+                       const int32_t* kept_idx, const int32_t* k_per_row, int kv_len, const int32_t* kv_len_per_row,
+                       int32_t* kv_len_next, const float* mass_src, float* mass_dst) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  for (const nova_fourbit_cache* c : {src, dst})
+    if (int rc = fourbit_error(c)) return rc;
+  if (src->B != dst->B || src->kv_heads != dst->kv_heads || src->dh != dst->dh) return NOVA_ERR_INVALID_ARG;
+  if (k < 0 || k > dst->capacity || kv_len < 0 || kv_len > src->capacity || !mass_src != !mass_dst) return NOVA_ERR_INVALID_ARG;
+  if (int rc = counts_error({kept_idx, k_per_row, kv_len_per_row, kv_len_next, mass_src, mass_dst})) return rc;
+  const size_t B = (size_t)src->B, rows_src = B * src->kv_heads * src->capacity, rows_dst = B * src->kv_heads * dst->capacity;
+  if (B == 0) return NOVA_OK;
+  if (k > 0 && !kept_idx) return NOVA_ERR_INVALID_ARG;
+  for (const void* p : {k_per_row, kv_len_per_row})
+    if (overlap(kv_len_next, B * 4, p, B * 4)) return NOVA_ERR_INVALID_ARG;
+  if (overlap(kv_len_next, B * 4, kept_idx, B * k * 4) ||
+      overlap(mass_src, B * src->capacity * 4, mass_dst, B * dst->capacity * 4))
+    return NOVA_ERR_INVALID_ARG;
+  const size_t row_codes = src->dh / 2, row_scales = src->dh / 32;
+  for (const void* s : {src->k_codes, src->v_codes})
+    for (const void* d : {dst->k_codes, dst->v_codes})
+      if (overlap(s, rows_src * row_codes, d, rows_dst * row_codes)) return NOVA_ERR_INVALID_ARG;
+  for (const void* s : {src->k_scales, src->v_scales})
+    for (const void* d : {dst->k_scales, dst->v_scales})
+      if (overlap(s, rows_src * row_scales, d, rows_dst * row_scales)) return NOVA_ERR_INVALID_ARG;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  return launch_fourbit_evict(static_cast<hipStream_t>(stream), *src, *dst, k, kept_idx, k_per_row, kv_len, kv_len_per_row,
+                              kv_len_next, mass_src, mass_dst) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
 }
 
 }  // extern "C"

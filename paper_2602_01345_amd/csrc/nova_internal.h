@@ -165,3 +165,21 @@ hipError_t launch_block_bf16(nova_ctx* ctx, hipStream_t st, const nova_block_sha
                              const nova_block_weights& w, const nova_block_variant& var, const RowCounts& rc,
                              const void* x, const int32_t* idx, void* kc, void* vc, void* y,
                              const BlockWorkspace& ws);
+
+// fourbit_cache.hip: rows into, out of and between caches in 4 bits (include/nova.h: nova_fourbit_append, _unpack, _evict)
+hipError_t launch_fourbit_append(hipStream_t st, int dtype, const nova_fourbit_cache& c, int n, const nova_rows* k,
+                                 const nova_rows* v, const int32_t* n_rows, int P, const int32_t* kv_rows, int32_t* kv_next);
+hipError_t launch_fourbit_unpack(hipStream_t st, int dtype, const nova_fourbit_cache& c, int first, int n,
+                                 const int32_t* first_rows, const int32_t* n_rows, const nova_rows* k, const nova_rows* v);
+hipError_t launch_fourbit_evict(hipStream_t st, const nova_fourbit_cache& src, const nova_fourbit_cache& dst, int k,
+                                const int32_t* idx, const int32_t* k_rows, int P, const int32_t* kv_rows, int32_t* kv_next,
+                                const float* mass_src, float* mass_dst);
+// fourbit_attention.hip: attention over such a cache, and what its rows collect; scale_log2 = score scale * log2 e
+size_t fourbit_attention_workspace_bytes(const nova_fourbit_cache& c, int heads, int n, int kv_len);
+hipError_t launch_fourbit_attention(const nova_ctx* ctx, hipStream_t st, int dtype, const nova_fourbit_cache& c, int heads, int n,
+                                    const nova_rows& q, const int32_t* n_rows, int P, const int32_t* kv_rows, float scale_log2,
+                                    void* out, float* lse, void* workspace);
+size_t fourbit_mass_workspace_bytes(const nova_fourbit_cache& c, int heads, int n, int kv_len);
+hipError_t launch_fourbit_mass(const nova_ctx* ctx, hipStream_t st, int dtype, const nova_fourbit_cache& c, int heads, int n,
+                               const nova_rows& q, const int32_t* n_rows, int P, const int32_t* kv_rows, float scale_log2,
+                               const float* lse, const float* mass_in, float* mass, void* workspace);
