@@ -333,6 +333,7 @@ def _prepare_own(case, s):
         s["out"] = torch.empty((B, n, H, dh), dtype=dtype, device="cuda")
         s["lse"] = torch.empty((B, n, H), device="cuda")
     else:
+        s["lse"] = s["lse"].contiguous()                         # dense, as the attention call writes it
         need = _NOVA.fourbit_mass_workspace_bytes(s["own"], H, n, case["kv_len"])
         s["mass_out"] = torch.empty((B, case["kv_len"]), device="cuda")
     s["workspace"] = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
