@@ -1,0 +1,96 @@
+// What the attention kernels over the 4-bit cache share: arguments, the rows of a key head, operands, the joining of key runs.
+#pragma once
+#include "fourbit.h"
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// An operand of the caller's type as bf16 numbers whose sum it is.  Cached values are bf16 as they are, so a bf16 operand
+// takes one MFMA and an fp32 one three: 3 x 8 bits of significand are all 24 of it.
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+
+__device__ __forceinline__ void split(float x, bf16_t (&p)[1]) { p[0] = (bf16_t)x; }
+__device__ __forceinline__ void split(float x, bf16_t (&p)[3]) {
+  p[0] = (bf16_t)x;
+  const float r = x - (float)p[0];
+  p[1] = (bf16_t)r;
+  p[2] = (bf16_t)(r - (float)p[1]);
+}
+template <typename T>
+__device__ __forceinline__ void load_eight(const T* src, bf16x8 (&f)[kParts<T>]) {
+  if constexpr (kParts<T> == 1) {
+    f[0] = *reinterpret_cast<const bf16x8*>(src);
+  } else {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(src), b = *reinterpret_cast<const f32x4*>(src + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bf16_t p[3];
+      split(e < 4 ? a[e & 3] : b[e & 3], p);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) f[i][e] = p[i];
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_four(T* dst, f32x4 v, float f) {
+  if constexpr (kParts<T> == 1) {
+    *reinterpret_cast<bf16x4*>(dst) = bf16x4{(bf16_t)(v[0] * f), (bf16_t)(v[1] * f), (bf16_t)(v[2] * f), (bf16_t)(v[3] * f)};
+  } else {
+    *reinterpret_cast<f32x4*>(dst) = v * f;
+  }
+}
+
+// byte offset of 16-byte chunk c of row r in an LDS tile of rows of ROWB bytes: neighbouring rows' equal chunks lie in different
+// banks, for reads of 16 bytes along a row as for transposing reads of 8 bytes down the rows
+template <int ROWB>
+__device__ __forceinline__ int swz(int r, int c) {
+  if (ROWB == 256) return r * 256 + ((c ^ (r & 15)) << 4);
+  return r * 128 + ((c ^ ((r >> 1) & 7)) << 4);
+}
+
+// Four rows by sixteen channels of an LDS tile, transposed on the way: sixteen neighbouring lanes name four rows' 8-byte pieces
+// (lane i: row i / 4, piece i % 4) and get lane i's channel of the four rows.
+typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4_t;
+__device__ __forceinline__ bf16x4 read_transposed(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t)p);
+}
+__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+
+// The queries that read one key head are its rows: query s of head j G + g is row s G + g (G heads share a key head).
+template <typename T>
+struct AttentionArgs {
+  const T* q;
+  int64_t q_sb, q_sr, q_sh;
+  FourBitView c;
+  int heads, G, n, P;
+  const int32_t *n_rows, *kv_rows;
+  float scale_log2;
+  T* out;
+  float* lse;
+  // Pieces: item i (a block of rows of one key head) is one workgroup below n_whole and nsplit of them, runs of key tiles, from
+  // there on; the latter leave sums against their own reference to be joined: part_o [run][row of the block][dh] and part_ml
+  // [run][row of the block] (reference in log2 units, sum)
+  int blocks;            // of rows per key head
+  int n_whole, nsplit;
+  float* part_o;
+  float* part_ml;
+
+  __device__ __forceinline__ const T* query(int b, int j, int row) const {
+    const int s = row / G;
+    return q + b * q_sb + s * q_sr + (j * G + (row - s * G)) * q_sh;
+  }
+  __device__ __forceinline__ int64_t out_row(int b, int j, int row) const {
+    const int s = row / G;
+    return ((int64_t)b * n + s) * heads + j * G + (row - s * G);
+  }
+};
+
+// fourbit_few.hip: blocks of 16 MT rows, waves that each take key tiles of their own
+template <typename T>
+hipError_t launch_fourbit_few(hipStream_t st, int dh, int mt, unsigned grid, const AttentionArgs<T>& a);

@@ -1,133 +1,364 @@
-// Attention over the key/value cache in 4 bits.
-#include "fourbit.h"
+// Attention over the 4-bit cache for many rows per key head (whole scales, prompts); which kernel takes which shape; the
+// joining of key runs.
+//
+// As in attention_bf16.hip everything is computed transposed, a lane owning one row (query):
+//   S^T = K Q^T    A operand = key rows from LDS, B operand = the row's channels, held in registers
+//   O^T += V^T P^T A operand = value rows from LDS, read transposed, B operand = the probabilities as they come out of the
+//                  softmax: the order of the keys in that product is free, so the values follow the scores' lane layout
+// A workgroup is four waves of 32 rows.  Tiles of 64 keys are converted to bf16 (exactly: a level times a power of two) by
+// all of its threads on the way from registers into LDS, once for the 128 rows; the codes of the tile after next are
+// on the way meanwhile.  Two stages of LDS, two workgroups per CU, so that one wave's softmax runs next to another's MFMAs.
+#include <algorithm>
+
+#include "fourbit_attention.h"
 
 namespace {
 
-// One wave per (image, query, head): 64 keys at a time, a lane per key for the scores, a lane per two channels (or one) for
-// the output.
+constexpr int kWaves = 4, kTile = 64, kRows = kWaves * 32;
+
 template <typename T, int DH>
-__global__ __launch_bounds__(64) void attention_kernel(const T* __restrict__ q, int64_t q_sb, int64_t q_sr, int64_t q_sh, FourBitView c,
-                                                       int heads, int n, const int32_t* __restrict__ n_rows, int P,
-                                                       const int32_t* __restrict__ kv_rows, float scale_log2,
-                                                       T* __restrict__ out, float* __restrict__ lse) {
-  const int lane = threadIdx.x, h = blockIdx.x % heads;
-  const int64_t row = blockIdx.x / heads;
-  const int b = (int)(row / n), s = (int)(row % n);
-  const int len = s < image_count(n_rows, b, n) ? image_prior(kv_rows, b, P) : 0;
-  const int64_t bh = (int64_t)b * c.hk + h / (heads / c.hk);
-  const T* qp = q + b * q_sb + s * q_sr + h * q_sh;
-  constexpr int CPL = DH / 64, GPR = DH / kGroup;
-  float m = -INFINITY, l = 0.f, o[CPL] = {};
-  for (int j0 = 0; j0 < len; j0 += 64) {
-    float sc = -INFINITY;
-    if (j0 + lane < len) {
-      const int64_t r = bh * c.cap + j0 + lane;
-      sc = 0.f;
-      for (int g = 0; g < GPR; ++g) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(c.codes[0] + (r * GPR + g) * 16);
-        const float ks = fourbit_scale(c.scales[0][r * GPR + g]);
+__global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a) {
+  constexpr int NP = kParts<T>;
+  constexpr int GPR = DH / kGroup;
+  constexpr int ROWB = DH * 2;
+  constexpr int HALF = kTile * ROWB, STAGE = 2 * HALF;     // K rows, V rows
+  constexpr int KS = DH / 16;                  // MFMAs along dh for a score block
+  constexpr int DB = DH / 32;                  // 32-channel blocks of the output
+  constexpr int CW = DH / 32;                  // dwords of codes per thread and tile: a quarter of a row of K and of V
+  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  // whole items and key runs, either group dealt so that the row blocks of one key head run on one XCD and share its L2
+  auto xcd_contiguous = [](int i, int n) {
+    const int xcd = i & 7;
+    return xcd * (n >> 3) + min(xcd, n & 7) + (i >> 3);
+  };
+  const bool whole = (int)blockIdx.x < a.n_whole;
+  const int run = whole ? 0 : xcd_contiguous(blockIdx.x - a.n_whole, gridDim.x - a.n_whole);
+  const int item = whole ? xcd_contiguous(blockIdx.x, a.n_whole) : a.n_whole + run / a.nsplit;
+  const int split_i = whole ? 0 : run % a.nsplit;
+  const int nparts = whole ? 1 : a.nsplit;
+  const int bh = item / a.blocks, block = item - bh * a.blocks;
+  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  const int row0 = block * kRows;
+  const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
+  const int ntiles = row0 < live ? (len + kTile - 1) / kTile : 0;
+  const int per = (ntiles + nparts - 1) / nparts;
+  const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
+
+  const uint8_t* codes[2] = {a.c.codes[0] + (int64_t)bh * a.c.cap * (DH / 2), a.c.codes[1] + (int64_t)bh * a.c.cap * (DH / 2)};
+  const uint8_t* scales[2] = {a.c.scales[0] + (int64_t)bh * a.c.cap * GPR, a.c.scales[1] + (int64_t)bh * a.c.cap * GPR};
+
+  // this thread's quarter of row tid / 4 of a tile: rows past the last take the last one's place (their scores are set to
+  // -inf below, their values are those of a row that counts)
+  const int frow = tid >> 2, fq = tid & 3;
+  uint32_t cw[2][CW], cb[2];
+  auto request = [&](int t) {
+    const uint32_t r = min(t * kTile + frow, len - 1);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x8 kv = fourbit_eight(w[j], ks);
+    for (int w = 0; w < 2; ++w) {
+      if constexpr (DH == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(codes[w] + r * 64 + fq * 16);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sc = fmaf((float)qp[g * kGroup + j * 8 + e], (float)kv[e], sc);
+        for (int e = 0; e < 4; ++e) cw[w][e] = x[e];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(codes[w] + r * 32 + fq * 8);
+        cw[w][0] = x[0];
+        cw[w][1] = x[1];
+      }
+      cb[w] = scales[w][r * GPR + fq * GPR / 4];
+    }
+  };
+  auto convert = [&](int stage) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const float scale = fourbit_scale(cb[w]);
+#pragma unroll
+      for (int e = 0; e < CW; ++e)
+        *reinterpret_cast<bf16x8*>(lds + stage * STAGE + w * HALF + swz<ROWB>(frow, fq * CW + e)) = fourbit_eight(cw[w][e], scale);
+    }
+  };
+  // waits for this wave's LDS traffic only: requested codes stay on the way
+  auto barrier = [] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  if (t0 < t1) request(t0);
+  const int row = row0 + wave * 32 + col;
+  bf16x8 qf[KS][NP];                                       // channels 16 t + 8 half .. + 7 of this lane's row
+  {
+    const T* qp = a.query(b, j, min(row, rows - 1)) + half * 8;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) load_eight(qp + t * 16, qf[t]);
+  }
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  // probabilities are 2^(score - m_run); m_run is a reference, not necessarily the largest score (-inf: none yet)
+  float m_run = -INFINITY, l_run = 0.f;
+  const bool wave_live = row0 + wave * 32 < live;
+  // this lane's places in a tile: its key's chunks, and for transposed reads of values the 8-byte piece lane % 4 of 16 channels of
+  // key 4 half + (lane % 16) / 4 and of the one 8 behind it.  The swizzle repeats after 16 rows.
+  int ka[KS], va[DB][2];
+#pragma unroll
+  for (int t = 0; t < KS; ++t) ka[t] = swz<ROWB>(col, t * 2 + half);
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      va[d][x] = swz<ROWB>(4 * half + ((lane & 15) >> 2) + 8 * x, 4 * d + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+
+  if (t0 < t1) {
+    convert(0);
+    if (t0 + 1 < t1) request(t0 + 1);
+    barrier();
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int stage = (t - t0) & 1;
+    const char* sk = lds + stage * STAGE;
+    const char* sv = sk + HALF;
+    f32x16 s[2];
+    if (wave_live) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sk + kb * 32 * ROWB + ka[ks]);
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) s[kb] = mfma32(kf, qf[ks][p], s[kb]);
         }
       }
-      sc *= scale_log2;
     }
-    const float mn = fmaxf(m, wave_max(sc)), ref = mn == -INFINITY ? 0.f : mn;
-    const float p = __builtin_amdgcn_exp2f(sc - ref), alpha = __builtin_amdgcn_exp2f(m - ref);
-    l = l * alpha + wave_sum(p);
-    m = mn;
+    if (t + 1 < t1) {
+      convert(stage ^ 1);
+      if (t + 2 < t1) request(t + 2);
+    }
+    if (wave_live) {
+      // ---- softmax: register r of block kb is key 64 t + 32 kb + 8 (r / 4) + 4 half + r % 4
+      if ((t + 1) * kTile > len) {
+        const float dead = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
 #pragma unroll
-    for (int i = 0; i < CPL; ++i) o[i] *= alpha;
-    for (int jj = 0; jj < min(64, len - j0); ++jj) {
-      const int64_t r = bh * c.cap + j0 + jj;
-      const float pj = __shfl(p, jj, 64);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        const int d = lane * CPL + i;
-        const uint32_t code = c.codes[1][r * (DH / 2) + d / 2] >> (d % 2 * 4) & 15;
-        o[i] = fmaf(pj, (float)fourbit_pair<0>(code, fourbit_scale(c.scales[1][r * GPR + d / kGroup]))[0], o[i]);
+          for (int r = 0; r < 16; ++r)
+            if (t * kTile + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= len) s[kb][r] = dead;
+      }
+      constexpr float kBig = 1024.0f;
+      float e[2][16], psum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -m_run));
+          psum += e[kb][r];
+        }
+      if (__any(!(psum <= kBig))) {
+        // some score lies far above the reference, or there is none yet: it moves to the largest score, and the sums with it
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, s[kb][r] * a.scale_log2);
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
+        const float m_new = fmaxf(m_run, tmax);
+        const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+        m_run = m_new;
+        const float ref = m_new == -INFINITY ? 0.f : m_new;           // nothing but scores of -inf so far
+        psum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -ref));
+            psum += e[kb][r];
+          }
+      }
+      l_run += psum;
+      // ---- O^T += V^T P^T, 16 keys per MFMA: the lane's keys 16 u + 4 half .. + 3 and 8 behind them
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        bf16x8 pf[NP];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          bf16_t p[NP];
+          split(e[u >> 1][(u & 1) * 8 + i], p);
+#pragma unroll
+          for (int x = 0; x < NP; ++x) pf[x][i] = p[x];
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const char* at = sv + u * 16 * ROWB;
+          const bf16x8 vf = join(read_transposed(at + va[d][0]), read_transposed(at + va[d][1]));
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) o[d] = mfma32(vf, pf[p], o[d]);
+        }
       }
     }
+    barrier();
   }
-  const int64_t orow = ((int64_t)b * n + s) * heads + h;
-  const float inv = len > 0 ? 1.0f / l : 0.f;
+
+  if (row >= rows) return;
+  const float l = l_run + __shfl_xor(l_run, 32, NOVA_WAVE);
+  if (nparts == 1) {
+    const bool some = row < live && len > 0;
+    const int64_t to = a.out_row(b, j, row);
+    const float inv = some ? 1.0f / l : 0.f;
 #pragma unroll
-  for (int i = 0; i < CPL; ++i) out[orow * DH + lane * CPL + i] = (T)(o[i] * inv);
-  if (lse && lane == 0) lse[orow] = len > 0 ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (some) v = f32x4{o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]};
+        store_four(a.out + to * DH + d * 32 + r4 * 8 + half * 4, v, inv);
+      }
+    if (a.lse && half == 0)
+      a.lse[to] = some ? ((m_run == -INFINITY ? 0.f : m_run) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  } else {
+    const int64_t to = (int64_t)run * kRows + (row - row0);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(a.part_o + to * DH + d * 32 + r4 * 8 + half * 4) =
+            f32x4{o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]};
+    if (half == 0) {
+      a.part_ml[to * 2] = m_run;
+      a.part_ml[to * 2 + 1] = l;
+    }
+  }
 }
 
-// One thread per key.
+// The runs of the cut items joined: out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  A thread has four channels of
+// one row; block_rows rows per item.
 template <typename T, int DH>
-__global__ __launch_bounds__(64) void mass_kernel(const T* __restrict__ q, int64_t q_sb, int64_t q_sr, int64_t q_sh, FourBitView c,
-                                                  int heads, int n, const int32_t* __restrict__ n_rows, int P,
-                                                  const int32_t* __restrict__ kv_rows, float scale_log2,
-                                                  const float* __restrict__ lse, const float* __restrict__ mass_in,
-                                                  float* __restrict__ mass) {
-  const int b = blockIdx.y, lane = threadIdx.x, j = blockIdx.x;
-  const int len = image_prior(kv_rows, b, P), nq = image_count(n_rows, b, n);
-  constexpr int GPR = DH / kGroup;
-  const int64_t at = (int64_t)b * c.cap + j;
-  if (j >= len) {
-    if (lane == 0) mass[at] = -1.0f;
+__global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block_rows, int cut) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c4 = (int)(i % (DH / 4));
+  const int64_t r = i / (DH / 4);
+  const int ci = (int)(r / block_rows), rr = (int)(r - (int64_t)ci * block_rows);
+  if (ci >= cut) return;
+  const int item = a.n_whole + ci;
+  const int bh = item / a.blocks, block = item - bh * a.blocks;
+  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  const int row = block * block_rows + rr;
+  if (row >= a.n * a.G) return;
+  const int64_t to = a.out_row(b, j, row);
+  if (row >= image_count(a.n_rows, b, a.n) * a.G || image_prior(a.kv_rows, b, a.P) == 0) {
+    store_four(a.out + to * DH + c4 * 4, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f);
+    if (a.lse && c4 == 0) a.lse[to] = -INFINITY;
     return;
   }
-  float sum = 0.f;
-  for (int64_t i = lane; i < (int64_t)nq * heads; i += 64) {
-    const int s = (int)(i / heads), h = (int)(i % heads);
-    const T* qp = q + b * q_sb + s * q_sr + h * q_sh;
-    const int64_t r = ((int64_t)b * c.hk + h / (heads / c.hk)) * c.cap + j;
-    float sc = 0.f;
-    for (int g = 0; g < GPR; ++g) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(c.codes[0] + (r * GPR + g) * 16);
-      const float ks = fourbit_scale(c.scales[0][r * GPR + g]);
-#pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        const bf16x8 kv = fourbit_eight(w[jj], ks);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sc = fmaf((float)qp[g * kGroup + jj * 8 + e], (float)kv[e], sc);
-      }
+  const int64_t p0 = (int64_t)ci * a.nsplit * block_rows + rr;
+  float m = -INFINITY, l = 0.f;
+  for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, a.part_ml[(p0 + (int64_t)s * block_rows) * 2]);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.nsplit; ++s) {
+    const int64_t p = p0 + (int64_t)s * block_rows;
+    const float ms = a.part_ml[p * 2];
+    const float w = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - m);   // of a run without a finite score: 0 or NaN
+    l = fmaf(w, a.part_ml[p * 2 + 1], l);
+    acc += w * *reinterpret_cast<const f32x4*>(a.part_o + p * DH + c4 * 4);
+  }
+  store_four(a.out + to * DH + c4 * 4, acc, 1.0f / l);
+  if (a.lse && c4 == 0) a.lse[to] = ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// How a call is divided: mt > 0: blocks of 16 mt rows (fourbit_few.hip), else blocks of kRows; items below n_whole are one
+// workgroup each, the others nsplit.  The workspace is sized for either type and any number of CUs up to kMaxCus.
+struct Plan {
+  int mt, block_rows, blocks, items, n_whole, nsplit;
+  int64_t runs() const { return (int64_t)(items - n_whole) * (nsplit > 1 ? nsplit : 0); }
+};
+constexpr int kCus = 256;
+Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
+  const int rows = n * (heads / c.kv_heads), ntiles = (kv_len + kTile - 1) / kTile;
+  Plan p = {};
+  p.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+  p.block_rows = p.mt ? 16 * p.mt : kRows;
+  p.blocks = (rows + p.block_rows - 1) / p.block_rows;
+  p.items = c.B * c.kv_heads * p.blocks;
+  p.n_whole = p.items;
+  p.nsplit = 1;
+  if (p.mt) {
+    const int want = std::min((3 * kCus + p.items - 1) / p.items, ntiles / (4 * kWaves));
+    if (want >= 2) {
+      p.n_whole = 0;
+      p.nsplit = want;
     }
-    sum += __builtin_amdgcn_exp2f(fmaf(sc, scale_log2, -lse[((int64_t)b * n + s) * heads + h] * 1.4426950408889634f));
+    return p;
   }
-  sum = wave_sum(sum);
-  if (lane == 0) {
-    const float m0 = mass_in ? mass_in[at] : 0.f;
-    mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+  const int slots = 2 * kCus, rest = p.items % slots;
+  if (rest == 0) return p;
+  const int s = std::min(slots / rest, ntiles / 4);
+  if (s >= 2) {
+    p.n_whole = p.items - rest;
+    p.nsplit = s;
   }
+  return p;
+}
+
+size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+template <typename T>
+hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n, const nova_rows& q, const int32_t* n_rows, int P,
+                  const int32_t* kv_rows, float scale_log2, void* out, float* lse, void* workspace) {
+  const Plan p = plan(c, heads, n, P);
+  AttentionArgs<T> a = {};
+  a.q = static_cast<const T*>(q.data);
+  a.q_sb = q.stride_b; a.q_sr = q.stride_row; a.q_sh = q.stride_head;
+  a.c = fourbit_view(c);
+  a.heads = heads; a.G = heads / c.kv_heads; a.n = n; a.P = P;
+  a.n_rows = n_rows; a.kv_rows = kv_rows;
+  // a score of -inf stays one when it is multiplied (the rows past the last): scores times 1e-30 weigh alike to the last bit, too
+  a.scale_log2 = scale_log2 == 0.f ? 1e-30f : scale_log2;
+  a.out = static_cast<T*>(out);
+  a.lse = lse;
+  a.blocks = p.blocks; a.n_whole = p.n_whole; a.nsplit = p.nsplit;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
+  const unsigned grid = (unsigned)(p.n_whole + (p.nsplit > 1 ? p.runs() : 0));
+  hipError_t e;
+  if (p.mt) {
+    e = launch_fourbit_few<T>(st, c.dh, p.mt, grid, a);
+  } else {
+    if (c.dh == 64) many_kernel<T, 64><<<grid, kWaves * 64, 0, st>>>(a);
+    else many_kernel<T, 128><<<grid, kWaves * 64, 0, st>>>(a);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const int cut = p.items - p.n_whole;
+  const unsigned jg = (unsigned)(((int64_t)cut * p.block_rows * (c.dh / 4) + 255) / 256);
+  if (c.dh == 64) join_kernel<T, 64><<<jg, 256, 0, st>>>(a, p.block_rows, cut);
+  else join_kernel<T, 128><<<jg, 256, 0, st>>>(a, p.block_rows, cut);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t fourbit_attention_workspace_bytes(const nova_fourbit_cache&, int, int, int) { return 0; }
-size_t fourbit_mass_workspace_bytes(const nova_fourbit_cache&, int, int, int) { return 0; }
+size_t fourbit_attention_workspace_bytes(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
+  const Plan p = plan(c, heads, n, kv_len);
+  if (p.nsplit == 1) return 0;
+  const size_t rows = (size_t)p.runs() * p.block_rows;
+  return up256(rows * c.dh * 4) + up256(rows * 8);
+}
 
 hipError_t launch_fourbit_attention(const nova_ctx*, hipStream_t st, int dtype, const nova_fourbit_cache& c, int heads, int n,
                                     const nova_rows& q, const int32_t* n_rows, int P, const int32_t* kv_rows, float scale_log2,
-                                    void* out, float* lse, void*) {
-  const unsigned grid = (unsigned)((int64_t)c.B * n * heads);
-#define GO(T, DH)                                                                                                        \
-  attention_kernel<T, DH><<<grid, 64, 0, st>>>(static_cast<const T*>(q.data), q.stride_b, q.stride_row, q.stride_head, \
-                                               fourbit_view(c), heads, n, n_rows, P, kv_rows, scale_log2,              \
-                                               static_cast<T*>(out), lse)
-  if (dtype == NOVA_BF16) { if (c.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
-  else { if (c.dh == 64) GO(float, 64); else GO(float, 128); }
-#undef GO
-  return hipGetLastError();
-}
-
-hipError_t launch_fourbit_mass(const nova_ctx*, hipStream_t st, int dtype, const nova_fourbit_cache& c, int heads, int n,
-                               const nova_rows& q, const int32_t* n_rows, int P, const int32_t* kv_rows, float scale_log2,
-                               const float* lse, const float* mass_in, float* mass, void*) {
-  if (c.capacity == 0) return hipSuccess;
-  const dim3 grid(c.capacity, c.B);
-#define GO(T, DH)                                                                                                    \
-  mass_kernel<T, DH><<<grid, 64, 0, st>>>(static_cast<const T*>(q.data), q.stride_b, q.stride_row, q.stride_head, \
-                                          fourbit_view(c), heads, n, n_rows, P, kv_rows, scale_log2, lse, mass_in, mass)
-  if (dtype == NOVA_BF16) { if (c.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
-  else { if (c.dh == 64) GO(float, 64); else GO(float, 128); }
-#undef GO
-  return hipGetLastError();
+                                    void* out, float* lse, void* workspace) {
+  if (dtype == NOVA_BF16) return attend<bf16_t>(st, c, heads, n, q, n_rows, P, kv_rows, scale_log2, out, lse, workspace);
+  return attend<float>(st, c, heads, n, q, n_rows, P, kv_rows, scale_log2, out, lse, workspace);
 }

@@ -1,0 +1,257 @@
+// Attention over the 4-bit cache for few rows per key head (a row: a query of one of the heads that share it): single tokens,
+// a handful of queries, small scales.  What bounds it is reading the cache once.
+//
+// A workgroup is four waves and one block of up to 16 MT rows; tiles of 64 keys are dealt to the waves, which share nothing
+// until their results are joined at the end, so no tile waits at a barrier.  Everything is computed transposed, a lane owning
+// one row of 16 (col) and the four lane groups (grp) parts of the keys:
+//   S^T = K Q^T    16 keys x 16 rows per MFMA.  The order of the channels in that product is free, so a lane takes them as they
+//                  lie in the cache: dh / 4 neighbouring channels of one key, 16 bytes at dh = 128, in one load and with one
+//                  scale, four conversions to an operand and no trip through LDS.
+//   O^T += V^T P^T the order of the keys is free as well: the scores a lane holds after two S^T tiles, keys 4 grp .. + 3 of
+//                  either, are its operand as they are.  Values are converted as they come (a lane: 32 channels of a key),
+//                  laid into the wave's own LDS by rows and read back transposed.
+#include "fourbit_attention.h"
+
+namespace {
+
+constexpr int kWaves = 4, kTile = 64;
+
+template <typename T, int DH, int MT>
+__global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void few_kernel(AttentionArgs<T> a) {
+  constexpr int NP = kParts<T>;
+  constexpr int GPR = DH / kGroup;             // groups per row
+  constexpr int ROWB = DH * 2;                 // bytes of a converted row
+  constexpr int KW = DH / 32;                  // dwords of codes (MFMA steps) a lane holds per 16 keys
+  constexpr int VL = DH / 32;                  // 16-byte loads of value codes per lane and tile
+  constexpr int VR = 64 / GPR;                 // value rows per such load
+  constexpr int DT = DH / 16;                  // 16-channel blocks of the output
+  constexpr int HALF = 32 * ROWB;              // LDS of a wave: 32 converted value rows, then its 16 x DH results
+  __shared__ __attribute__((aligned(1024))) char lds[kWaves * HALF];
+  __shared__ float part_m[kWaves][16], part_l[kWaves][16];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int piece = blockIdx.x;
+  const int item = piece < a.n_whole ? piece : a.n_whole + (piece - a.n_whole) / a.nsplit;
+  const int split_i = piece < a.n_whole ? 0 : (piece - a.n_whole) % a.nsplit;
+  const int nparts = piece < a.n_whole ? 1 : a.nsplit;
+  const int bh = item / a.blocks, block = item - bh * a.blocks;
+  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  const int row0 = block * 16 * MT;
+  const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
+  const int ntiles = row0 < live ? (len + kTile - 1) / kTile : 0;
+  const int per = (ntiles + nparts - 1) / nparts;
+  const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
+
+  const uint8_t* kc = a.c.codes[0] + (int64_t)bh * a.c.cap * (DH / 2);
+  const uint8_t* vc = a.c.codes[1] + (int64_t)bh * a.c.cap * (DH / 2);
+  const uint8_t* ks = a.c.scales[0] + (int64_t)bh * a.c.cap * GPR;
+  const uint8_t* vs = a.c.scales[1] + (int64_t)bh * a.c.cap * GPR;
+
+  // Rows past the last take the last one's place: their scores are set to -inf, their values are those of a row that counts.
+  uint32_t kw[4][KW], vw[VL][4], kb[4], vb[VL];
+  auto load_k = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t r = min(t * kTile + i * 16 + col, len - 1);
+      if constexpr (DH == 128) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(kc + r * 64 + grp * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kw[i][e] = w[e];
+      } else {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(kc + r * 32 + grp * 8);
+        kw[i][0] = w[0];
+        kw[i][1] = w[1];
+      }
+      kb[i] = ks[r * GPR + grp * GPR / 4];
+    }
+  };
+  auto load_v = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const uint32_t r = min(t * kTile + i * VR + lane / GPR, len - 1);
+      const u32x4 w = *reinterpret_cast<const u32x4*>(vc + r * (DH / 2) + lane % GPR * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) vw[i][e] = w[e];
+      vb[i] = vs[r * GPR + lane % GPR];
+    }
+  };
+
+  const int first = t0 + wave;
+  if (first < t1) {
+    load_k(first);
+    load_v(first);
+  }
+  // operand of step e: channels grp dh / 4 + 8 e .. + 7 of row col
+  bf16x8 qf[MT][KW][NP];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const T* qp = a.query(b, j, min(row0 + mt * 16 + col, rows - 1)) + grp * (DH / 4);
+#pragma unroll
+    for (int e = 0; e < KW; ++e) load_eight(qp + e * 8, qf[mt][e]);
+  }
+  f32x4 o[MT][DT];
+  float m_run[MT], l_run[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m_run[mt] = -INFINITY;
+    l_run[mt] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  char* sv = lds + wave * HALF;
+  // transposed reads: lane i of a group of sixteen names row 4 grp + i / 4 and 8-byte piece i % 4 of 16 channels
+  int vaddr[DT];
+  {
+    const int r = 4 * grp + (col >> 2);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vaddr[d] = swz<ROWB>(r, 2 * d + ((col & 3) >> 1)) + (col & 1) * 8;
+  }
+
+  for (int t = first; t < t1; t += kWaves) {
+    const bool more = t + kWaves < t1;
+    // ---- scores: register r of tile i is key 16 i + 4 grp + r, for row col
+    f32x4 s[MT][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float scale = fourbit_scale(kb[i]);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) s[mt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < KW; ++e) {
+        const bf16x8 kf = fourbit_eight(kw[i][e], scale);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) s[mt][i] = mfma16(kf, qf[mt][e][p], s[mt][i]);
+      }
+    }
+    if (more) load_k(t + kWaves);
+
+    // ---- softmax against a reference that moves when a score lies above it
+    float pr[MT][4][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          pr[mt][i][r] = s[mt][i][r] * a.scale_log2;
+          if ((t + 1) * kTile > len && t * kTile + i * 16 + grp * 4 + r >= len) pr[mt][i][r] = -INFINITY;
+          tmax = fmaxf(tmax, pr[mt][i][r]);
+        }
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 16, NOVA_WAVE));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
+      if (__any(tmax > m_run[mt])) {
+        const float m_new = fmaxf(m_run[mt], tmax);
+        const float alpha = m_run[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[mt] - m_new);
+        l_run[mt] *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[mt][d] *= alpha;
+        m_run[mt] = m_new;
+      }
+      const float ref = m_run[mt] == -INFINITY ? 0.f : m_run[mt];      // nothing but scores of -inf so far
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          pr[mt][i][r] = __builtin_amdgcn_exp2f(pr[mt][i][r] - ref);
+          l_run[mt] += pr[mt][i][r];
+        }
+    }
+
+    // ---- values, 32 keys at a time through the wave's LDS (its reads and writes are done in order)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = u * VL / 2; i < (u + 1) * VL / 2; ++i) {
+        const float scale = fourbit_scale(vb[i]);
+        const int r = (i - u * VL / 2) * VR + lane / GPR, c = lane % GPR * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<bf16x8*>(sv + swz<ROWB>(r, c + e)) = fourbit_eight(vw[i][e], scale);
+      }
+      asm volatile("" ::: "memory");
+      if (u == 1 && more) load_v(t + kWaves);
+      bf16x8 pf[MT][NP];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          bf16_t p[NP];
+          split(pr[mt][2 * u + (e >> 2)][e & 3], p);
+#pragma unroll
+          for (int i = 0; i < NP; ++i) pf[mt][i][e] = p[i];
+        }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const bf16x8 vf = join(read_transposed(sv + vaddr[d]), read_transposed(sv + vaddr[d] + 16 * ROWB));
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) o[mt][d] = mfma16(vf, pf[mt][p], o[mt][d]);
+      }
+      asm volatile("" ::: "memory");
+    }
+  }
+
+  // ---- join the waves: [channel / 4][row] of four channels each in a wave's LDS
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float l = l_run[mt];
+    l += __shfl_xor(l, 16, NOVA_WAVE);
+    l += __shfl_xor(l, 32, NOVA_WAVE);
+    if (mt > 0) __syncthreads();
+    if (grp == 0) {
+      part_m[wave][col] = m_run[mt];
+      part_l[wave][col] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(sv + ((d * 4 + grp) * 16 + col) * 16) = o[mt][d];
+    __syncthreads();
+    for (int i = tid; i < 16 * (DH / 4); i += kWaves * 64) {
+      const int c4 = i % (DH / 4), rr = i / (DH / 4), row = row0 + mt * 16 + rr;
+      if (row >= rows) continue;
+      float m = -INFINITY, lt = 0.f;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, part_m[w][rr]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        // a wave without a finite score has reference -inf and sum 0 or NaN, and NaN or 0 in its results
+        const float f = part_m[w][rr] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(part_m[w][rr] - m);
+        lt = fmaf(f, part_l[w][rr], lt);
+        acc += f * *reinterpret_cast<const f32x4*>(lds + w * HALF + (c4 * 16 + rr) * 16);
+      }
+      if (nparts == 1) {
+        const bool some = row < live && len > 0;
+        const int64_t to = a.out_row(b, j, row);
+        store_four(a.out + to * DH + c4 * 4, some ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, some ? 1.0f / lt : 0.f);
+        if (a.lse && c4 == 0) a.lse[to] = some ? ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
+      } else {
+        const int64_t to = (int64_t)(piece - a.n_whole) * 16 * MT + mt * 16 + rr;
+        *reinterpret_cast<f32x4*>(a.part_o + to * DH + c4 * 4) = acc;
+        if (c4 == 0) {
+          a.part_ml[to * 2] = m;
+          a.part_ml[to * 2 + 1] = lt;
+        }
+      }
+    }
+  }
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_fourbit_few(hipStream_t st, int dh, int mt, unsigned grid, const AttentionArgs<T>& a) {
+#define GO(DH, MT) few_kernel<T, DH, MT><<<grid, kWaves * 64, 0, st>>>(a)
+  if (dh == 64) { if (mt == 1) GO(64, 1); else GO(64, 2); }
+  else { if (mt == 1) GO(128, 1); else GO(128, 2); }
+#undef GO
+  return hipGetLastError();
+}
+template hipError_t launch_fourbit_few<bf16_t>(hipStream_t, int, int, unsigned, const AttentionArgs<bf16_t>&);
+template hipError_t launch_fourbit_few<float>(hipStream_t, int, int, unsigned, const AttentionArgs<float>&);
