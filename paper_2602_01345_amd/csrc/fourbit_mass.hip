@@ -1,62 +1,234 @@
-// What the rows of the 4-bit cache collect of the queries' attention.
-#include "fourbit.h"
+// What the rows of the 4-bit cache collect of the queries' attention: mass_j = sum over rows of 2^(score - lse), a row being a
+// query of one of the heads that share a key head.  Half the products of the attention and as many exponentials, no values.
+//
+// S = Q K^T, 32 rows x 32 keys per MFMA, a lane owning one key of either of two blocks: the sum over rows stays in the lane.  A
+// wave has 64 keys, converted once into the operands it holds in registers (the order of the channels in the product is free:
+// a lane takes half a row of the cache as it lies); the rows come in tiles of 32 through LDS, shared by the four waves.
+// A launch leaves sums per key head (and run of rows, where there are few keys); a second one adds them up in a fixed order.
+#include <algorithm>
+
+#include "fourbit_attention.h"
 
 namespace {
 
-// One thread per key.
+constexpr int kWaves = 4, kKeys = kWaves * 64, kTileRows = 32;
+
+template <typename T>
+struct MassArgs {
+  const T* q;
+  int64_t q_sb, q_sr, q_sh;
+  FourBitView c;
+  int heads, G, n, P;
+  uint32_t G_inv;
+  const int32_t *n_rows, *kv_rows;
+  float scale_log2;
+  const float* lse;
+  int chunks, nsplit;    // key chunks per key head, runs of row tiles
+  float* part;           // [B][hk][nsplit][pitch]
+  int pitch;
+};
+
 template <typename T, int DH>
-__global__ __launch_bounds__(64) void mass_kernel(const T* __restrict__ q, int64_t q_sb, int64_t q_sr, int64_t q_sh, FourBitView c,
-                                                  int heads, int n, const int32_t* __restrict__ n_rows, int P,
-                                                  const int32_t* __restrict__ kv_rows, float scale_log2,
-                                                  const float* __restrict__ lse, const float* __restrict__ mass_in,
-                                                  float* __restrict__ mass) {
-  const int b = blockIdx.y, lane = threadIdx.x, j = blockIdx.x;
-  const int len = image_prior(kv_rows, b, P), nq = image_count(n_rows, b, n);
-  constexpr int GPR = DH / kGroup;
-  const int64_t at = (int64_t)b * c.cap + j;
-  if (j >= len) {
-    if (lane == 0) mass[at] = -1.0f;
-    return;
-  }
-  float sum = 0.f;
-  for (int64_t i = lane; i < (int64_t)nq * heads; i += 64) {
-    const int s = (int)(i / heads), h = (int)(i % heads);
-    const T* qp = q + b * q_sb + s * q_sr + h * q_sh;
-    const int64_t r = ((int64_t)b * c.hk + h / (heads / c.hk)) * c.cap + j;
-    float sc = 0.f;
-    for (int g = 0; g < GPR; ++g) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(c.codes[0] + (r * GPR + g) * 16);
-      const float ks = fourbit_scale(c.scales[0][r * GPR + g]);
+__global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
+  constexpr int NP = kParts<T>;
+  constexpr int GPR = DH / kGroup, ROWB = DH * 2, KS = DH / 16;
+  constexpr int PLANE = kTileRows * ROWB, STAGE = NP * PLANE;
+  constexpr int QL = kTileRows * DH / 8 / (kWaves * 64);       // runs of eight channels per thread and tile
+  constexpr int CPR = DH / 8;                                  // of them per row
+  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+  __shared__ __attribute__((aligned(16))) float neg_lse[2][kTileRows];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int split_i = blockIdx.x % a.nsplit, ic = blockIdx.x / a.nsplit;
+  const int chunk = ic % a.chunks, bh = ic / a.chunks;
+  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  const int live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
+  const int key0 = chunk * kKeys + wave * 64;
+  if (chunk * kKeys >= len) return;                            // the whole workgroup: nothing is read of these keys' sums
+  const int ntiles = (live + kTileRows - 1) / kTileRows, per = (ntiles + a.nsplit - 1) / a.nsplit;
+  const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
+
+  // ---- rows of a tile: past the last one its copies, which weigh nothing (lse = inf)
+  T qr[QL][8];
+  float lse_r = 0.f;
+  auto request = [&](int t) {
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        const bf16x8 kv = fourbit_eight(w[jj], ks);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sc = fmaf((float)qp[g * kGroup + jj * 8 + e], (float)kv[e], sc);
+    for (int i = 0; i < QL; ++i) {
+      const int x = tid + i * kWaves * 64;
+      int g;
+      const int s = div_by(min(t * kTileRows + x / CPR, live - 1), a.G, a.G_inv, g);
+      const T* p = a.q + b * a.q_sb + s * a.q_sr + (j * a.G + g) * a.q_sh + x % CPR * 8;
+      if constexpr (NP == 1) {
+        *reinterpret_cast<u32x4*>(qr[i]) = *reinterpret_cast<const u32x4*>(p);
+      } else {
+        *reinterpret_cast<f32x4*>(qr[i]) = *reinterpret_cast<const f32x4*>(p);
+        *reinterpret_cast<f32x4*>(qr[i] + 4) = *reinterpret_cast<const f32x4*>(p + 4);
       }
     }
-    sum += __builtin_amdgcn_exp2f(fmaf(sc, scale_log2, -lse[((int64_t)b * n + s) * heads + h] * 1.4426950408889634f));
+    if (tid < kTileRows) {
+      const int row = t * kTileRows + tid;
+      int g;
+      const int s = div_by(min(row, live - 1), a.G, a.G_inv, g);
+      lse_r = row < live ? -kAttnLog2e * a.lse[((int64_t)b * a.n + s) * a.heads + j * a.G + g] : -INFINITY;
+    }
+  };
+  auto place = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < QL; ++i) {
+      const int x = tid + i * kWaves * 64;
+      bf16x8 f[NP];
+      load_eight(qr[i], f);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8*>(lds + stage * STAGE + p * PLANE + swz<ROWB>(x / CPR, x % CPR)) = f[p];
+    }
+    if (tid < kTileRows) neg_lse[stage][tid] = lse_r;
+  };
+  auto barrier = [] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);                        // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  if (t0 < t1) request(t0);
+
+  // ---- this lane's keys: channels half dh / 2 + 8 t of key col of block kb
+  bf16x8 kf[2][KS];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int64_t r = (int64_t)bh * a.c.cap + min(key0 + kb * 32 + col, len - 1);
+    const uint8_t* w = a.c.codes[0] + r * (DH / 2) + half * (DH / 4);
+    const uint8_t* sc = a.c.scales[0] + r * GPR + half * (GPR / 2);
+#pragma unroll
+    for (int x = 0; x < GPR / 2; ++x) {
+      const u32x4 c = *reinterpret_cast<const u32x4*>(w + x * 16);
+      const float scale = fourbit_scale(sc[x]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) kf[kb][x * 4 + e] = fourbit_eight(c[e], scale);
+    }
   }
-  sum = wave_sum(sum);
-  if (lane == 0) {
-    const float m0 = mass_in ? mass_in[at] : 0.f;
-    mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+  int qa[KS];
+#pragma unroll
+  for (int t = 0; t < KS; ++t) qa[t] = swz<ROWB>(col, half * KS + t);
+
+  float acc[2] = {0.f, 0.f};
+  if (t0 < t1) {
+    place(0);
+    if (t0 + 1 < t1) request(t0 + 1);
+    barrier();
   }
+  for (int t = t0; t < t1; ++t) {
+    const int stage = (t - t0) & 1;
+    const char* sq = lds + stage * STAGE;
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) {
+        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(sq + p * PLANE + qa[ks]);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = mfma32(qf, kf[kb][ks], s[kb]);
+      }
+    if (t + 1 < t1) {
+      place(stage ^ 1);
+      if (t + 2 < t1) request(t + 2);
+    }
+    // register r is row 8 (r / 4) + 4 half + r % 4 of the tile
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const f32x4 nl = *reinterpret_cast<const f32x4*>(&neg_lse[stage][8 * r4 + 4 * half]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) sum[kb] += __builtin_amdgcn_exp2f(fmaf(s[kb][r4 * 4 + e], a.scale_log2, nl[e]));
+    }
+    acc[0] += sum[0];
+    acc[1] += sum[1];
+    barrier();
+  }
+  float* to = a.part + ((int64_t)bh * a.nsplit + split_i) * a.pitch;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const float v = acc[kb] + __shfl_xor(acc[kb], 32, NOVA_WAVE);
+    const int key = key0 + kb * 32 + col;
+    if (half == 0 && key < len) to[key] = v;
+  }
+}
+
+__global__ __launch_bounds__(256) void add_kernel(const float* __restrict__ part, int pitch, int parts, int cap, int P,
+                                                  const int32_t* __restrict__ kv_rows, const float* mass_in, float* mass) {
+  const int b = blockIdx.y, k = blockIdx.x * 256 + threadIdx.x;
+  if (k >= cap) return;
+  const int64_t at = (int64_t)b * cap + k;
+  if (k >= image_prior(kv_rows, b, P)) {
+    mass[at] = -1.0f;
+    return;
+  }
+  const float m0 = mass_in ? mass_in[at] : 0.f;
+  float sum = 0.f;
+  const float* p = part + (int64_t)b * parts * pitch + k;
+#pragma unroll 8
+  for (int i = 0; i < parts; ++i) sum += p[(int64_t)i * pitch];
+  mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+}
+
+struct Plan {
+  int chunks, nsplit, pitch;
+};
+constexpr int kCus = 256;
+Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
+  Plan p;
+  p.chunks = (kv_len + kKeys - 1) / kKeys;
+  p.pitch = (kv_len + 63) / 64 * 64;
+  const int64_t items = std::max((int64_t)c.B * c.kv_heads * p.chunks, (int64_t)1);
+  const int tiles = (int)(((int64_t)n * (heads / c.kv_heads) + kTileRows - 1) / kTileRows);
+  p.nsplit = (int)std::max((int64_t)1, std::min((int64_t)tiles, 2 * kCus / items));
+  return p;
+}
+
+template <typename T>
+hipError_t collect(hipStream_t st, const nova_fourbit_cache& c, int heads, int n, const nova_rows& q, const int32_t* n_rows, int P,
+                   const int32_t* kv_rows, float scale_log2, const float* lse, const float* mass_in, float* mass, void* workspace) {
+  const Plan p = plan(c, heads, n, P);
+  MassArgs<T> a = {};
+  a.q = static_cast<const T*>(q.data);
+  a.q_sb = q.stride_b; a.q_sr = q.stride_row; a.q_sh = q.stride_head;
+  a.c = fourbit_view(c);
+  a.heads = heads; a.G = heads / c.kv_heads; a.n = n; a.P = P;
+  a.G_inv = div_inv(a.G);
+  a.n_rows = n_rows; a.kv_rows = kv_rows;
+  a.scale_log2 = scale_log2;
+  a.lse = lse;
+  a.chunks = p.chunks; a.nsplit = p.nsplit; a.pitch = p.pitch;
+  a.part = static_cast<float*>(workspace);
+  int parts = 0;
+  if (n > 0 && P > 0) {
+    parts = c.kv_heads * p.nsplit;
+    const unsigned grid = (unsigned)((int64_t)c.B * c.kv_heads * p.chunks * p.nsplit);
+    if (c.dh == 64) mass_kernel<T, 64><<<grid, kWaves * 64, 0, st>>>(a);
+    else mass_kernel<T, 128><<<grid, kWaves * 64, 0, st>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  add_kernel<<<dim3((c.capacity + 255) / 256, c.B), 256, 0, st>>>(a.part, p.pitch, parts, c.capacity, P, kv_rows, mass_in, mass);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t fourbit_mass_workspace_bytes(const nova_fourbit_cache&, int, int, int) { return 0; }
+size_t fourbit_mass_workspace_bytes(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
+  const Plan p = plan(c, heads, n, kv_len);
+  return (size_t)c.B * c.kv_heads * p.nsplit * p.pitch * sizeof(float);
+}
 
 hipError_t launch_fourbit_mass(const nova_ctx*, hipStream_t st, int dtype, const nova_fourbit_cache& c, int heads, int n,
                                const nova_rows& q, const int32_t* n_rows, int P, const int32_t* kv_rows, float scale_log2,
-                               const float* lse, const float* mass_in, float* mass, void*) {
-  if (c.capacity == 0) return hipSuccess;
-  const dim3 grid(c.capacity, c.B);
-#define GO(T, DH)                                                                                                    \
-  mass_kernel<T, DH><<<grid, 64, 0, st>>>(static_cast<const T*>(q.data), q.stride_b, q.stride_row, q.stride_head, \
-                                          fourbit_view(c), heads, n, n_rows, P, kv_rows, scale_log2, lse, mass_in, mass)
-  if (dtype == NOVA_BF16) { if (c.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
-  else { if (c.dh == 64) GO(float, 64); else GO(float, 128); }
-#undef GO
-  return hipGetLastError();
+                               const float* lse, const float* mass_in, float* mass, void* workspace) {
+  if (dtype == NOVA_BF16) return collect<bf16_t>(st, c, heads, n, q, n_rows, P, kv_rows, scale_log2, lse, mass_in, mass, workspace);
+  return collect<float>(st, c, heads, n, q, n_rows, P, kv_rows, scale_log2, lse, mass_in, mass, workspace);
 }
