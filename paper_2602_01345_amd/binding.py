@@ -8,8 +8,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from dataclasses import dataclass
-from typing import Dict, Optional, Sequence, Union
+from dataclasses import dataclass, field
+from typing import Dict, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -50,7 +50,7 @@ class _Rows(C.Structure):
     _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("stride_b", "stride_row", "stride_head", "stride_channel")]
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class FourBitCache:
     """nova_fourbit_cache: keys and values of B images in 4 bits, uint8 device tensors: codes [B, kv_heads, capacity, dh / 2]
     and scales [B, kv_heads, capacity, dh / 32] of either."""
@@ -58,6 +58,7 @@ class FourBitCache:
     k_scales: torch.Tensor
     v_codes: torch.Tensor
     v_scales: torch.Tensor
+    _c: Optional["_FourBitCache"] = field(default=None, init=False, repr=False)
 
     @classmethod
     def empty(cls, B: int, kv_heads: int, capacity: int, dh: int, device: Union[str, int, torch.device] = "cuda") -> "FourBitCache":
@@ -76,14 +77,23 @@ class FourBitCache:
         return self.k_codes.shape[3] * 2
 
     def c_struct(self) -> "_FourBitCache":
-        codes, scales = self.k_codes.shape, self.k_scales.shape
-        if (self.v_codes.shape != codes or self.v_scales.shape != scales or codes[:3] != scales[:3]
-                or codes[3] != 16 * scales[3]):
-            raise ValueError(f"no cache in 4 bits: codes {tuple(codes)}, {tuple(self.v_codes.shape)}, "
-                             f"scales {tuple(scales)}, {tuple(self.v_scales.shape)}")
+        """The C structure: made and checked on the first call, and again only if a tensor has got other memory since."""
         ts = (self.k_codes, self.k_scales, self.v_codes, self.v_scales)
+        ptrs = (ts[0].data_ptr(), ts[1].data_ptr(), ts[2].data_ptr(), ts[3].data_ptr())
+        c = self._c
+        if c is not None and c.made_of == ptrs:
+            return c
+        codes, scales = ts[0].shape, ts[1].shape
+        if ts[2].shape != codes or ts[3].shape != scales or codes[:3] != scales[:3] or codes[3] != 16 * scales[3]:
+            raise ValueError(f"no cache in 4 bits: codes {tuple(codes)}, {tuple(ts[2].shape)}, scales {tuple(scales)}, "
+                             f"{tuple(ts[3].shape)}")
         assert all(t.dtype == torch.uint8 for t in ts), "codes and scales are uint8"
-        return _FourBitCache(*[_ptr(t) for t in ts], *codes[:3], codes[3] * 2)
+        c = _FourBitCache(*[_ptr(t) for t in ts], *codes[:3], codes[3] * 2)
+        c.made_of, c.device = ptrs, ts[0].get_device()
+        if any(t.get_device() != c.device for t in ts):
+            raise ValueError("the arrays of a cache lie on one device")
+        object.__setattr__(self, "_c", c)
+        return c
 
 
 @dataclass
@@ -232,11 +242,11 @@ def _rows(t: torch.Tensor, heads: int, dh: int, name: str) -> "_Rows":
     return _Rows(t.data_ptr(), *t.stride())
 
 
-def _shaped(name: str, t: Optional[torch.Tensor], shape: Sequence[int], dtype: torch.dtype) -> Optional[int]:
+def _shaped(name: str, t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype: torch.dtype) -> Optional[int]:
     """Pointer of an optional dense tensor that has to have this shape and type."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
     return _ptr(t)
 
@@ -506,68 +516,79 @@ class Nova:
     # These work on the context's device, on that device's current stream, whichever device is current.
     def _here(self, *ts: Optional[torch.Tensor]):
         for t in ts:
-            if t is not None and t.device.index != self.device:
+            if t is not None and t.get_device() != self.device:
                 raise ValueError(f"tensor on {t.device}, context on device {self.device}")
+
+    def _cache(self, cache: FourBitCache) -> "_FourBitCache":
+        c = cache.c_struct()
+        if c.device != self.device:
+            raise ValueError(f"cache on device {c.device}, context on device {self.device}")
+        return c
+
+    def _counts(self, B: int, name: str, t: Optional[torch.Tensor]) -> Optional[int]:
+        if t is None:
+            return None
+        self._here(t)
+        return _shaped(name, t, (B,), torch.int32)
 
     def fourbit_append(self, cache: FourBitCache, k: torch.Tensor, v: torch.Tensor, kv_len: int,
                        n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None,
                        kv_len_next: Optional[torch.Tensor] = None):
         """Quantises k, v [B, n, kv_heads, dh] (f32|bf16, any strides) behind the images' rows.  kv_len: rows every image
         has, or the upper bound of kv_len_per_row ([B] int32, like n_per_row and kv_len_next)."""
-        c = cache.c_struct()
+        c = self._cache(cache)
         if k.shape != v.shape or k.dtype != v.dtype or k.shape[0] != c.B:
             raise ValueError(f"k {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}, {c.B} images in the cache")
-        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, k, v, n_per_row, kv_len_per_row, kv_len_next)
-        kr, vr = _rows(k, c.kv_heads, c.dh, "k"), _rows(v, c.kv_heads, c.dh, "v")
+        self._here(k, v)
         rc = self.lib.nova_fourbit_append(
-            self.ctx, _stream(self.device), _dtype_code(k), C.byref(c), k.shape[1], C.byref(kr), C.byref(vr),
-            _shaped("n_per_row", n_per_row, (c.B,), torch.int32), int(kv_len),
-            _shaped("kv_len_per_row", kv_len_per_row, (c.B,), torch.int32),
-            _shaped("kv_len_next", kv_len_next, (c.B,), torch.int32))
-        self._check(rc, "nova_fourbit_append")
+            self.ctx, _stream(self.device), _dtype_code(k), c, k.shape[1], _rows(k, c.kv_heads, c.dh, "k"),
+            _rows(v, c.kv_heads, c.dh, "v"), self._counts(c.B, "n_per_row", n_per_row), kv_len,
+            self._counts(c.B, "kv_len_per_row", kv_len_per_row), self._counts(c.B, "kv_len_next", kv_len_next))
+        if rc:
+            self._check(rc, "nova_fourbit_append")
 
     def fourbit_unpack(self, cache: FourBitCache, first: int, k: Optional[torch.Tensor], v: Optional[torch.Tensor],
                        first_per_row: Optional[torch.Tensor] = None, n_per_row: Optional[torch.Tensor] = None):
         """Values of cached rows from row `first` on, into k and v [B, n, kv_heads, dh] (f32|bf16, any strides)."""
-        c = cache.c_struct()
-        out = [t for t in (k, v) if t is not None]
-        if not out:
+        c = self._cache(cache)
+        a = v if k is None else k
+        if a is None:
             return
-        if any(t.shape[:2] != out[0].shape[:2] or t.dtype != out[0].dtype or t.shape[0] != c.B for t in out):
-            raise ValueError(f"outputs {[(tuple(t.shape), t.dtype) for t in out]}, {c.B} images in the cache")
-        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, k, v, first_per_row, n_per_row)
-        kr, vr = (None if t is None else C.byref(_rows(t, c.kv_heads, c.dh, "output")) for t in (k, v))
+        if v is not None and (v.shape != a.shape or v.dtype != a.dtype) or a.shape[0] != c.B:
+            raise ValueError(f"outputs {[None if t is None else (tuple(t.shape), t.dtype) for t in (k, v)]}, {c.B} images in the "
+                             "cache")
+        self._here(k, v)
         rc = self.lib.nova_fourbit_unpack(
-            self.ctx, _stream(self.device), _dtype_code(out[0]), C.byref(c), int(first), out[0].shape[1],
-            _shaped("first_per_row", first_per_row, (c.B,), torch.int32),
-            _shaped("n_per_row", n_per_row, (c.B,), torch.int32), kr, vr)
-        self._check(rc, "nova_fourbit_unpack")
+            self.ctx, _stream(self.device), _dtype_code(a), c, first, a.shape[1],
+            self._counts(c.B, "first_per_row", first_per_row), self._counts(c.B, "n_per_row", n_per_row),
+            None if k is None else _rows(k, c.kv_heads, c.dh, "k"), None if v is None else _rows(v, c.kv_heads, c.dh, "v"))
+        if rc:
+            self._check(rc, "nova_fourbit_unpack")
 
     def fourbit_attention_workspace_bytes(self, cache: FourBitCache, heads: int, n: int, kv_len: int) -> int:
-        return int(self.lib.nova_fourbit_attention_workspace_bytes(C.byref(cache.c_struct()), heads, n, kv_len))
+        return self.lib.nova_fourbit_attention_workspace_bytes(cache.c_struct(), heads, n, kv_len)
 
     def fourbit_attention(self, cache: FourBitCache, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor],
                           kv_len: int, scale: Optional[float] = None, lse: Optional[torch.Tensor] = None,
                           n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None):
         """out [B, n, heads, dh] = attention of q [B, n, heads, dh] (f32|bf16, channels dense) over the cached rows; lse
         [B, n, heads] f32 or None.  scale: 1 / sqrt(dh) where None."""
-        c = cache.c_struct()
-        B, n, heads, dh = q.shape
+        c = self._cache(cache)
+        shape = q.shape
+        B, n, heads, dh = shape
         if B != c.B:
             raise ValueError(f"{B} images of queries, {c.B} in the cache")
-        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, q, out, lse, workspace, n_per_row,
-                   kv_len_per_row)
-        qr = _rows(q, heads, c.dh, "q")
+        self._here(q, out, lse, workspace)
         rc = self.lib.nova_fourbit_attention(
-            self.ctx, _stream(self.device), _dtype_code(q), C.byref(c), heads, n, C.byref(qr),
-            _shaped("n_per_row", n_per_row, (B,), torch.int32), int(kv_len),
-            _shaped("kv_len_per_row", kv_len_per_row, (B,), torch.int32), dh ** -0.5 if scale is None else float(scale),
-            _shaped("out", out, q.shape, q.dtype), _shaped("lse", lse, (B, n, heads), torch.float32),
-            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
-        self._check(rc, "nova_fourbit_attention")
+            self.ctx, _stream(self.device), _dtype_code(q), c, heads, n, _rows(q, heads, c.dh, "q"),
+            self._counts(B, "n_per_row", n_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
+            dh ** -0.5 if scale is None else scale, _shaped("out", out, shape, q.dtype),
+            _shaped("lse", lse, (B, n, heads), torch.float32), _ptr(workspace), 0 if workspace is None else workspace.nbytes)
+        if rc:
+            self._check(rc, "nova_fourbit_attention")
 
     def fourbit_mass_workspace_bytes(self, cache: FourBitCache, heads: int, n: int, kv_len: int) -> int:
-        return int(self.lib.nova_fourbit_mass_workspace_bytes(C.byref(cache.c_struct()), heads, n, kv_len))
+        return self.lib.nova_fourbit_mass_workspace_bytes(cache.c_struct(), heads, n, kv_len)
 
     def fourbit_mass(self, cache: FourBitCache, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor,
                      workspace: Optional[torch.Tensor], kv_len: int, scale: Optional[float] = None,
@@ -575,39 +596,35 @@ class Nova:
                      kv_len_per_row: Optional[torch.Tensor] = None):
         """mass [B, capacity] f32: mass_in (may be the same tensor; None: zeros) plus what the cached rows collect from q; lse
         as fourbit_attention wrote it."""
-        c = cache.c_struct()
+        c = self._cache(cache)
         B, n, heads, dh = q.shape
         if B != c.B:
             raise ValueError(f"{B} images of queries, {c.B} in the cache")
-        self._here(cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales, q, lse, mass, mass_in, workspace, n_per_row,
-                   kv_len_per_row)
-        qr = _rows(q, heads, c.dh, "q")
+        self._here(q, lse, mass, mass_in, workspace)
         rc = self.lib.nova_fourbit_mass(
-            self.ctx, _stream(self.device), _dtype_code(q), C.byref(c), heads, n, C.byref(qr),
-            _shaped("n_per_row", n_per_row, (B,), torch.int32), int(kv_len),
-            _shaped("kv_len_per_row", kv_len_per_row, (B,), torch.int32), dh ** -0.5 if scale is None else float(scale),
-            _shaped("lse", lse, (B, n, heads), torch.float32), _shaped("mass_in", mass_in, (B, c.capacity), torch.float32),
-            _shaped("mass", mass, (B, c.capacity), torch.float32),
-            _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
-        self._check(rc, "nova_fourbit_mass")
+            self.ctx, _stream(self.device), _dtype_code(q), c, heads, n, _rows(q, heads, c.dh, "q"),
+            self._counts(B, "n_per_row", n_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
+            dh ** -0.5 if scale is None else scale, _shaped("lse", lse, (B, n, heads), torch.float32),
+            _shaped("mass_in", mass_in, (B, c.capacity), torch.float32), _shaped("mass", mass, (B, c.capacity), torch.float32),
+            _ptr(workspace), 0 if workspace is None else workspace.nbytes)
+        if rc:
+            self._check(rc, "nova_fourbit_mass")
 
     def fourbit_evict(self, src: FourBitCache, dst: FourBitCache, kept_idx: torch.Tensor, kv_len: int,
                       k_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None,
                       kv_len_next: Optional[torch.Tensor] = None, mass_src: Optional[torch.Tensor] = None,
                       mass_dst: Optional[torch.Tensor] = None):
         """Rows kept_idx [B, k] of src to the front of dst, with their masses."""
-        s, d = src.c_struct(), dst.c_struct()
-        k = kept_idx.shape[1]
-        self._here(src.k_codes, src.k_scales, src.v_codes, src.v_scales, dst.k_codes, dst.k_scales, dst.v_codes, dst.v_scales,
-                   kept_idx, k_per_row, kv_len_per_row, kv_len_next, mass_src, mass_dst)
+        s, d = self._cache(src), self._cache(dst)
+        B, k = s.B, kept_idx.shape[1]
+        self._here(kept_idx, mass_src, mass_dst)
         rc = self.lib.nova_fourbit_evict(
-            self.ctx, _stream(self.device), C.byref(s), C.byref(d), k, _shaped("kept_idx", kept_idx, (s.B, k), torch.int32),
-            _shaped("k_per_row", k_per_row, (s.B,), torch.int32), int(kv_len),
-            _shaped("kv_len_per_row", kv_len_per_row, (s.B,), torch.int32),
-            _shaped("kv_len_next", kv_len_next, (s.B,), torch.int32),
-            _shaped("mass_src", mass_src, (s.B, s.capacity), torch.float32),
-            _shaped("mass_dst", mass_dst, (s.B, d.capacity), torch.float32))
-        self._check(rc, "nova_fourbit_evict")
+            self.ctx, _stream(self.device), s, d, k, _shaped("kept_idx", kept_idx, (B, k), torch.int32),
+            self._counts(B, "k_per_row", k_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
+            self._counts(B, "kv_len_next", kv_len_next), _shaped("mass_src", mass_src, (B, s.capacity), torch.float32),
+            _shaped("mass_dst", mass_dst, (B, d.capacity), torch.float32))
+        if rc:
+            self._check(rc, "nova_fourbit_evict")
 
 
 # ------------------------------------------------------------------------------------
