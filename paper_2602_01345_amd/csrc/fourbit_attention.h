@@ -46,12 +46,15 @@ __device__ __forceinline__ void store_four(T* dst, f32x4 v, float f) {
   }
 }
 
-// byte offset of 16-byte chunk c of row r in an LDS tile of rows of ROWB bytes: neighbouring rows' equal chunks lie in different
-// banks, for reads of 16 bytes along a row as for transposing reads of 8 bytes down the rows
+// Byte offset of 16-byte chunk c of row r in an LDS tile of rows of ROWB bytes: chunk c lies in place c ^ f(r).  f is a sum of
+// r's bits chosen so that none of these meets a bank twice, whether 128 or 256 bytes are served at a time: one chunk of 8 or 16
+// rows running (operands read along the rows, rows written); two neighbouring chunks of rows 4 i .. 4 i + 3 and of the 4 behind
+// them, four chunks of 4 rows (transposing reads by 16 or 32 lanes).  With the usual f(r) = r mod 16 transposing reads take
+// twice the time: 57 % of the LDS cycles of attend many, 128 channels, were conflicts.  f repeats after 16 rows.
 template <int ROWB>
 __device__ __forceinline__ int swz(int r, int c) {
-  if (ROWB == 256) return r * 256 + ((c ^ (r & 15)) << 4);
-  return r * 128 + ((c ^ ((r >> 1) & 7)) << 4);
+  const int f = 2 * (r & 3) ^ 3 * ((r >> 2) & 1) ^ (ROWB == 256 ? 8 * ((r ^ (r >> 3)) & 1) : (r >> 3) & 1);
+  return r * ROWB + ((c ^ f) << 4);
 }
 
 // Four rows by sixteen channels of an LDS tile, transposed on the way: sixteen neighbouring lanes name four rows' 8-byte pieces

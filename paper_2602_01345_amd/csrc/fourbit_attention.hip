@@ -51,9 +51,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a
   const uint8_t* codes[2] = {a.c.codes[0] + (int64_t)bh * a.c.cap * (DH / 2), a.c.codes[1] + (int64_t)bh * a.c.cap * (DH / 2)};
   const uint8_t* scales[2] = {a.c.scales[0] + (int64_t)bh * a.c.cap * GPR, a.c.scales[1] + (int64_t)bh * a.c.cap * GPR};
 
-  // this thread's quarter of row tid / 4 of a tile: rows past the last take the last one's place (their scores are set to
+  // this thread's quarter (the wave's) of row lane of a tile, so that neighbouring lanes write one chunk of neighbouring rows: rows past the last take the last one's place (their scores are set to
   // -inf below, their values are those of a row that counts)
-  const int frow = tid >> 2, fq = tid & 3;
+  const int frow = lane, fq = wave;
   uint32_t cw[2][CW], cb[2];
   auto request = [&](int t) {
     const uint32_t r = min(t * kTile + frow, len - 1);
