@@ -7,7 +7,9 @@
 //                  softmax: the order of the keys in that product is free, so the values follow the scores' lane layout
 // A workgroup is four waves of 32 rows.  Tiles of 64 keys are converted to bf16 (exactly: a level times a power of two) by
 // all of its threads on the way from registers into LDS, once for the 128 rows; the codes of the tile after next are
-// on the way meanwhile.  Two stages of LDS, two workgroups per CU, so that one wave's softmax runs next to another's MFMAs.
+// on the way meanwhile.  Two stages of LDS, two workgroups per CU, so that one wave's softmax runs next to another's MFMAs; a
+// wave asks for priority while it issues MFMAs, or two waves of a SIMD fall into step and take turns at everything (385 us
+// without, 340 with: 2458 queries of 2 images, 16 heads of 128, 8883 keys).
 #include <algorithm>
 
 #include "fourbit_attention.h"
@@ -126,6 +128,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a
     const char* sv = sk + HALF;
     f32x16 s[2];
     if (wave_live) {
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
@@ -138,6 +141,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if (t + 1 < t1) {
       convert(stage ^ 1);
       if (t + 2 < t1) request(t + 2);
@@ -188,6 +192,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a
           }
       }
       l_run += psum;
+      __builtin_amdgcn_s_setprio(1);
       // ---- O^T += V^T P^T, 16 keys per MFMA: the lane's keys 16 u + 4 half .. + 3 and 8 behind them
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -208,6 +213,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     barrier();
   }
 
