@@ -79,11 +79,25 @@ struct AttentionArgs {
   // Pieces: item i (a block of rows of one key head) is one workgroup below n_whole and nsplit of them, runs of key tiles, from
   // there on; the latter leave sums against their own reference to be joined: part_o [run][row of the block][dh] and part_ml
   // [run][row of the block] (reference in log2 units, sum)
-  int blocks;            // of rows per key head
+  int blocks, items;     // of rows per key head; in all
   int n_whole, nsplit;
   float* part_o;
   float* part_ml;
 
+  // Key head (of all images') and block of rows of an item.  Workgroups are dealt to the 8 XCDs in turn: the blocks of one key
+  // head go to one XCD and share its L2, eight key heads running to the eight XCDs, so that images of different lengths load
+  // them alike.  What is left of the key heads goes as it comes.
+  __device__ __forceinline__ void place(int item, int& bh, int& block) const {
+    const int dealt = items / (8 * blocks) * 8 * blocks;
+    if (item < dealt) {
+      const int i = item >> 3, g = i / blocks;
+      bh = g * 8 + (item & 7);
+      block = i - g * blocks;
+    } else {
+      bh = item / blocks;
+      block = item - bh * blocks;
+    }
+  }
   __device__ __forceinline__ const T* query(int b, int j, int row) const {
     const int s = row / G;
     return q + b * q_sb + s * q_sr + (j * G + (row - s * G)) * q_sh;

@@ -19,7 +19,7 @@ namespace {
 constexpr int kWaves = 4, kTile = 64, kRows = kWaves * 32;
 
 template <typename T, int DH>
-__global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a) {
+__global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) void many_kernel(AttentionArgs<T> a) {
   constexpr int NP = kParts<T>;
   constexpr int GPR = DH / kGroup;
   constexpr int ROWB = DH * 2;
@@ -32,17 +32,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void many_kernel(AttentionArgs<T> a
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
-  // whole items and key runs, either group dealt so that the row blocks of one key head run on one XCD and share its L2
-  auto xcd_contiguous = [](int i, int n) {
-    const int xcd = i & 7;
-    return xcd * (n >> 3) + min(xcd, n & 7) + (i >> 3);
-  };
   const bool whole = (int)blockIdx.x < a.n_whole;
-  const int run = whole ? 0 : xcd_contiguous(blockIdx.x - a.n_whole, gridDim.x - a.n_whole);
-  const int item = whole ? xcd_contiguous(blockIdx.x, a.n_whole) : a.n_whole + run / a.nsplit;
+  const int run = blockIdx.x - a.n_whole;
   const int split_i = whole ? 0 : run % a.nsplit;
   const int nparts = whole ? 1 : a.nsplit;
-  const int bh = item / a.blocks, block = item - bh * a.blocks;
+  int bh, block;
+  a.place(whole ? blockIdx.x : a.n_whole + run / a.nsplit, bh, block);
   const int b = bh / a.c.hk, j = bh - b * a.c.hk;
   const int row0 = block * kRows;
   const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
@@ -257,8 +252,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block
   const int64_t r = i / (DH / 4);
   const int ci = (int)(r / block_rows), rr = (int)(r - (int64_t)ci * block_rows);
   if (ci >= cut) return;
-  const int item = a.n_whole + ci;
-  const int bh = item / a.blocks, block = item - bh * a.blocks;
+  int bh, block;
+  a.place(a.n_whole + ci, bh, block);
   const int b = bh / a.c.hk, j = bh - b * a.c.hk;
   const int row = block * block_rows + rr;
   if (row >= a.n * a.G) return;
@@ -333,7 +328,7 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
   a.scale_log2 = scale_log2 == 0.f ? 1e-30f : scale_log2;
   a.out = static_cast<T*>(out);
   a.lse = lse;
-  a.blocks = p.blocks; a.n_whole = p.n_whole; a.nsplit = p.nsplit;
+  a.blocks = p.blocks; a.items = p.items; a.n_whole = p.n_whole; a.nsplit = p.nsplit;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
   const unsigned grid = (unsigned)(p.n_whole + (p.nsplit > 1 ? p.runs() : 0));

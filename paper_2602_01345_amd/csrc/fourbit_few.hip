@@ -36,7 +36,8 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
   const int item = piece < a.n_whole ? piece : a.n_whole + (piece - a.n_whole) / a.nsplit;
   const int split_i = piece < a.n_whole ? 0 : (piece - a.n_whole) % a.nsplit;
   const int nparts = piece < a.n_whole ? 1 : a.nsplit;
-  const int bh = item / a.blocks, block = item - bh * a.blocks;
+  int bh, block;
+  a.place(item, bh, block);
   const int b = bh / a.c.hk, j = bh - b * a.c.hk;
   const int row0 = block * 16 * MT;
   const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
