@@ -3,6 +3,7 @@
 #include "fourbit.h"
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kBig = 1024.0f;          // sum of a lane's probabilities of one tile above which the softmax reference moves
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -81,6 +82,7 @@ struct AttentionArgs {
   // [run][row of the block] (reference in log2 units, sum)
   int blocks, items;     // of rows per key head; in all
   int n_whole, nsplit;
+  int run_tiles;         // tiles per run; 0: an item's tiles divided by nsplit
   float* part_o;
   float* part_ml;
 
@@ -108,6 +110,6 @@ struct AttentionArgs {
   }
 };
 
-// fourbit_few.hip: blocks of 16 MT rows, waves that each take key tiles of their own
+// fourbit_few.hip: blocks of 16 mt rows, 4 or 8 waves that each take key tiles of their own (8: mt 1)
 template <typename T>
-hipError_t launch_fourbit_few(hipStream_t st, int dh, int mt, unsigned grid, const AttentionArgs<T>& a);
+hipError_t launch_fourbit_few(hipStream_t st, int dh, int mt, int waves, unsigned grid, const AttentionArgs<T>& a);

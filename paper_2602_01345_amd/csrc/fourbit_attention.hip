@@ -151,7 +151,6 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
           for (int r = 0; r < 16; ++r)
             if (t * kTile + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= len) s[kb][r] = dead;
       }
-      constexpr float kBig = 1024.0f;
       float e[2][16], psum = 0.f;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -244,61 +243,91 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
 }
 
 // The runs of the cut items joined: out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  A thread has four channels of
-// one row; block_rows rows per item.
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block_rows, int cut) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int c4 = (int)(i % (DH / 4));
-  const int64_t r = i / (DH / 4);
-  const int ci = (int)(r / block_rows), rr = (int)(r - (int64_t)ci * block_rows);
-  if (ci >= cut) return;
+// one row and every SL-th run; with many runs per row (SL = 8: from five on) the threads of a row join through LDS.
+template <typename T, int DH, int SL>
+__global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block_rows, int used_rows) {
+  constexpr int C4 = DH / 4, RPW = 256 / (C4 * SL);
+  __shared__ f32x4 part_o[SL > 1 ? 256 : 1];
+  __shared__ float part_m[SL > 1 ? 256 / C4 : 1], part_l[SL > 1 ? 256 / C4 : 1];
+  const int tid = threadIdx.x, c4 = tid % C4, sl = tid / C4 % SL;
+  const int64_t r = (int64_t)blockIdx.x * RPW + tid / (C4 * SL);
+  const int ci = (int)(r / used_rows), rr = (int)(r - (int64_t)ci * used_rows);
   int bh, block;
-  a.place(a.n_whole + ci, bh, block);
+  a.place(min(a.n_whole + ci, a.items - 1), bh, block);
   const int b = bh / a.c.hk, j = bh - b * a.c.hk;
   const int row = block * block_rows + rr;
-  if (row >= a.n * a.G) return;
-  const int64_t to = a.out_row(b, j, row);
-  if (row >= image_count(a.n_rows, b, a.n) * a.G || image_prior(a.kv_rows, b, a.P) == 0) {
-    store_four(a.out + to * DH + c4 * 4, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f);
-    if (a.lse && c4 == 0) a.lse[to] = -INFINITY;
-    return;
-  }
+  const int len = image_prior(a.kv_rows, b, a.P);
+  const bool there = a.n_whole + ci < a.items && row < a.n * a.G;
+  const bool some = there && row < image_count(a.n_rows, b, a.n) * a.G && len > 0;
+  const int runs = !some ? 0 : a.run_tiles ? min(a.nsplit, ((len + kTile - 1) / kTile + a.run_tiles - 1) / a.run_tiles) : a.nsplit;
   const int64_t p0 = (int64_t)ci * a.nsplit * block_rows + rr;
+  // a run without a finite score has reference -inf and sum 0 or NaN, and 0 or NaN in its results: it is added as it is
   float m = -INFINITY, l = 0.f;
-  for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, a.part_ml[(p0 + (int64_t)s * block_rows) * 2]);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.nsplit; ++s) {
+#pragma unroll 2
+  for (int s = sl; s < runs; s += SL) {
     const int64_t p = p0 + (int64_t)s * block_rows;
-    const float ms = a.part_ml[p * 2];
-    const float w = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - m);   // of a run without a finite score: 0 or NaN
-    l = fmaf(w, a.part_ml[p * 2 + 1], l);
-    acc += w * *reinterpret_cast<const f32x4*>(a.part_o + p * DH + c4 * 4);
+    const float ms = a.part_ml[p * 2], ls = a.part_ml[p * 2 + 1];
+    const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + p * DH + c4 * 4);
+    const float mn = fmaxf(m, ms);
+    const float w0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn), w1 = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - mn);
+    l = l * w0 + ls * w1;
+    acc = acc * w0 + o * w1;
+    m = mn;
   }
-  store_four(a.out + to * DH + c4 * 4, acc, 1.0f / l);
-  if (a.lse && c4 == 0) a.lse[to] = ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+  if constexpr (SL > 1) {
+    part_o[tid] = acc;
+    if (c4 == 0) {
+      part_m[tid / C4] = m;
+      part_l[tid / C4] = l;
+    }
+    __syncthreads();
+    if (sl > 0 || !there) return;
+    const int g = tid / C4;
+    for (int s = 1; s < SL; ++s) m = fmaxf(m, part_m[g + s]);
+    l = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < SL; ++s) {
+      const float w = part_m[g + s] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(part_m[g + s] - m);
+      l = fmaf(w, part_l[g + s], l);
+      acc += w * part_o[tid + s * C4];
+    }
+  }
+  if (!there) return;
+  const int64_t to = a.out_row(b, j, row);
+  store_four(a.out + to * DH + c4 * 4, acc, some ? 1.0f / l : 0.f);
+  if (a.lse && c4 == 0) a.lse[to] = some ? ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // How a call is divided: mt > 0: blocks of 16 mt rows (fourbit_few.hip), else blocks of kRows; items below n_whole are one
-// workgroup each, the others nsplit.  The workspace is sized for either type and any number of CUs up to kMaxCus.
+// workgroup each, the others nsplit.
 struct Plan {
-  int mt, block_rows, blocks, items, n_whole, nsplit;
-  int64_t runs() const { return (int64_t)(items - n_whole) * (nsplit > 1 ? nsplit : 0); }
+  int mt, waves, block_rows, blocks, items, n_whole, nsplit, run_tiles;
+  int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
 };
 constexpr int kCus = 256;
+constexpr int kFewWhole = 24;
 Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
   const int rows = n * (heads / c.kv_heads), ntiles = (kv_len + kTile - 1) / kTile;
   Plan p = {};
   p.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+  p.waves = 4;
   p.block_rows = p.mt ? 16 * p.mt : kRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;
   p.items = c.B * c.kv_heads * p.blocks;
   p.n_whole = p.items;
   p.nsplit = 1;
+  p.run_tiles = 0;
   if (p.mt) {
-    const int want = std::min((3 * kCus + p.items - 1) / p.items, ntiles / (4 * kWaves));
-    if (want >= 2) {
+    const int want = std::min((12 * kCus + p.items - 1) / p.items, ntiles);      // waves per item: twelve per CU, a tile each
+    p.run_tiles = ntiles;
+    if (want > 4 && p.mt == 1 && ntiles <= kFewWhole) {
+      p.waves = 8;
+    } else if (want > 4) {
       p.n_whole = 0;
-      p.nsplit = want;
+      p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
+      p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
     }
     return p;
   }
@@ -328,23 +357,25 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
   a.scale_log2 = scale_log2 == 0.f ? 1e-30f : scale_log2;
   a.out = static_cast<T*>(out);
   a.lse = lse;
-  a.blocks = p.blocks; a.items = p.items; a.n_whole = p.n_whole; a.nsplit = p.nsplit;
+  a.blocks = p.blocks; a.items = p.items; a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
-  const unsigned grid = (unsigned)(p.n_whole + (p.nsplit > 1 ? p.runs() : 0));
+  const unsigned grid = (unsigned)(p.n_whole + p.runs());
   hipError_t e;
   if (p.mt) {
-    e = launch_fourbit_few<T>(st, c.dh, p.mt, grid, a);
+    e = launch_fourbit_few<T>(st, c.dh, p.mt, p.waves, grid, a);
   } else {
     if (c.dh == 64) many_kernel<T, 64><<<grid, kWaves * 64, 0, st>>>(a);
     else many_kernel<T, 128><<<grid, kWaves * 64, 0, st>>>(a);
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.nsplit == 1) return e;
-  const int cut = p.items - p.n_whole;
-  const unsigned jg = (unsigned)(((int64_t)cut * p.block_rows * (c.dh / 4) + 255) / 256);
-  if (c.dh == 64) join_kernel<T, 64><<<jg, 256, 0, st>>>(a, p.block_rows, cut);
-  else join_kernel<T, 128><<<jg, 256, 0, st>>>(a, p.block_rows, cut);
+  const int used = std::min(p.block_rows, n * a.G);            // rows of a block that there are, where it is the only one
+  const int64_t rows = (int64_t)(p.items - p.n_whole) * used;
+#define GO(DH, SL) join_kernel<T, DH, SL><<<(unsigned)((rows * (DH / 4 * SL) + 255) / 256), 256, 0, st>>>(a, p.block_rows, used)
+  if (c.dh == 64) { if (p.nsplit > 4) GO(64, 8); else GO(64, 1); }
+  else { if (p.nsplit > 4) GO(128, 8); else GO(128, 1); }
+#undef GO
   return hipGetLastError();
 }
 

@@ -1,7 +1,7 @@
 // Attention over the 4-bit cache for few rows per key head (a row: a query of one of the heads that share it): single tokens,
 // a handful of queries, small scales.  What bounds it is reading the cache once.
 //
-// A workgroup is four waves and one block of up to 16 MT rows; tiles of 64 keys are dealt to the waves, which share nothing
+// A workgroup is four or eight waves and one block of up to 16 MT rows; tiles of 64 keys are dealt to the waves, which share nothing
 // until their results are joined at the end, so no tile waits at a barrier.  Everything is computed transposed, a lane owning
 // one row of 16 (col) and the four lane groups (grp) parts of the keys:
 //   S^T = K Q^T    16 keys x 16 rows per MFMA.  The order of the channels in that product is free, so a lane takes them as they
@@ -14,10 +14,10 @@
 
 namespace {
 
-constexpr int kWaves = 4, kTile = 64;
+constexpr int kTile = 64;
 
-template <typename T, int DH, int MT>
-__global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void few_kernel(AttentionArgs<T> a) {
+template <typename T, int DH, int MT, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 512 ? 2 : 3) void few_kernel(AttentionArgs<T> a) {
   constexpr int NP = kParts<T>;
   constexpr int GPR = DH / kGroup;             // groups per row
   constexpr int ROWB = DH * 2;                 // bytes of a converted row
@@ -26,24 +26,23 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
   constexpr int VR = 64 / GPR;                 // value rows per such load
   constexpr int DT = DH / 16;                  // 16-channel blocks of the output
   constexpr int HALF = 32 * ROWB;              // LDS of a wave: 32 converted value rows, then its 16 x DH results
-  __shared__ __attribute__((aligned(1024))) char lds[kWaves * HALF];
-  __shared__ float part_m[kWaves][16], part_l[kWaves][16];
+  __shared__ __attribute__((aligned(1024))) char lds[NW * HALF];
+  __shared__ float part_m[NW][16], part_l[NW][16];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  const int piece = blockIdx.x;
-  const int item = piece < a.n_whole ? piece : a.n_whole + (piece - a.n_whole) / a.nsplit;
-  const int split_i = piece < a.n_whole ? 0 : (piece - a.n_whole) % a.nsplit;
-  const int nparts = piece < a.n_whole ? 1 : a.nsplit;
+  const int piece = blockIdx.x, nparts = a.nsplit;
+  const int item = piece / nparts, split_i = piece - item * nparts;
   int bh, block;
   a.place(item, bh, block);
   const int b = bh / a.c.hk, j = bh - b * a.c.hk;
   const int row0 = block * 16 * MT;
   const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
   const int ntiles = row0 < live ? (len + kTile - 1) / kTile : 0;
-  const int per = (ntiles + nparts - 1) / nparts;
-  const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
+  // runs of one length whatever the image has, so that an image of any length is spread like the others; what none needs leaves
+  const int t0 = split_i * a.run_tiles, t1 = min(ntiles, t0 + a.run_tiles);
+  if (nparts > 1 && t0 >= t1) return;
 
   const uint8_t* kc = a.c.codes[0] + (int64_t)bh * a.c.cap * (DH / 2);
   const uint8_t* vc = a.c.codes[1] + (int64_t)bh * a.c.cap * (DH / 2);
@@ -110,8 +109,8 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
     for (int d = 0; d < DT; ++d) vaddr[d] = swz<ROWB>(r, 2 * d + ((col & 3) >> 1)) + (col & 1) * 8;
   }
 
-  for (int t = first; t < t1; t += kWaves) {
-    const bool more = t + kWaves < t1;
+  for (int t = first; t < t1; t += NW) {
+    const bool more = t + NW < t1;
     // ---- scores: register r of tile i is key 16 i + 4 grp + r, for row col
     f32x4 s[MT][4];
 #pragma unroll
@@ -128,39 +127,56 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
           for (int p = NP - 1; p >= 0; --p) s[mt][i] = mfma16(kf, qf[mt][e][p], s[mt][i]);
       }
     }
-    if (more) load_k(t + kWaves);
+    if (more) load_k(t + NW);
 
-    // ---- softmax against a reference that moves when a score lies above it
+    // ---- softmax: probabilities are 2^(score - m_run) against a reference that moves only when a sum of them says that some
+    // score lies far above it, or there is none yet (-inf): no largest score, no lanes asked in the common case
+    if ((t + 1) * kTile > len) {
+      const float dead = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (t * kTile + i * 16 + grp * 4 + r >= len)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) s[mt][i][r] = dead;
+    }
     float pr[MT][4][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      float tmax = -INFINITY;
+      float psum = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          pr[mt][i][r] = s[mt][i][r] * a.scale_log2;
-          if ((t + 1) * kTile > len && t * kTile + i * 16 + grp * 4 + r >= len) pr[mt][i][r] = -INFINITY;
-          tmax = fmaxf(tmax, pr[mt][i][r]);
+          pr[mt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][i][r], a.scale_log2, -m_run[mt]));
+          psum += pr[mt][i][r];
         }
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 16, NOVA_WAVE));
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
-      if (__any(tmax > m_run[mt])) {
+      if (__any(!(psum <= kBig))) {
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) tmax = fmaxf(tmax, s[mt][i][r] * a.scale_log2);
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 16, NOVA_WAVE));
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
         const float m_new = fmaxf(m_run[mt], tmax);
         const float alpha = m_run[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[mt] - m_new);
         l_run[mt] *= alpha;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[mt][d] *= alpha;
         m_run[mt] = m_new;
+        const float ref = m_new == -INFINITY ? 0.f : m_new;            // nothing but scores of -inf so far
+        psum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            pr[mt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][i][r], a.scale_log2, -ref));
+            psum += pr[mt][i][r];
+          }
       }
-      const float ref = m_run[mt] == -INFINITY ? 0.f : m_run[mt];      // nothing but scores of -inf so far
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          pr[mt][i][r] = __builtin_amdgcn_exp2f(pr[mt][i][r] - ref);
-          l_run[mt] += pr[mt][i][r];
-        }
+      l_run[mt] += psum;
     }
 
     // ---- values, 32 keys at a time through the wave's LDS (its reads and writes are done in order)
@@ -176,7 +192,7 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
           *reinterpret_cast<bf16x8*>(sv + swz<ROWB>(r, c + e)) = fourbit_eight(vw[i][e], scale);
       }
       asm volatile("" ::: "memory");
-      if (u == 1 && more) load_v(t + kWaves);
+      if (u == 1 && more) load_v(t + NW);
       bf16x8 pf[MT][NP];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -213,15 +229,15 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
 #pragma unroll
     for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(sv + ((d * 4 + grp) * 16 + col) * 16) = o[mt][d];
     __syncthreads();
-    for (int i = tid; i < 16 * (DH / 4); i += kWaves * 64) {
+    for (int i = tid; i < 16 * (DH / 4); i += NW * 64) {
       const int c4 = i % (DH / 4), rr = i / (DH / 4), row = row0 + mt * 16 + rr;
       if (row >= rows) continue;
       float m = -INFINITY, lt = 0.f;
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, part_m[w][rr]);
+      for (int w = 0; w < NW; ++w) m = fmaxf(m, part_m[w][rr]);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < NW; ++w) {
         // a wave without a finite score has reference -inf and sum 0 or NaN, and NaN or 0 in its results
         const float f = part_m[w][rr] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(part_m[w][rr] - m);
         lt = fmaf(f, part_l[w][rr], lt);
@@ -233,7 +249,7 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
         store_four(a.out + to * DH + c4 * 4, some ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, some ? 1.0f / lt : 0.f);
         if (a.lse && c4 == 0) a.lse[to] = some ? ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;
       } else {
-        const int64_t to = (int64_t)(piece - a.n_whole) * 16 * MT + mt * 16 + rr;
+        const int64_t to = (int64_t)piece * 16 * MT + mt * 16 + rr;
         *reinterpret_cast<f32x4*>(a.part_o + to * DH + c4 * 4) = acc;
         if (c4 == 0) {
           a.part_ml[to * 2] = m;
@@ -247,12 +263,12 @@ __global__ __launch_bounds__(kWaves * 64, MT == 1 ? 3 : MT == 2 ? 2 : 1) void fe
 }  // namespace
 
 template <typename T>
-hipError_t launch_fourbit_few(hipStream_t st, int dh, int mt, unsigned grid, const AttentionArgs<T>& a) {
-#define GO(DH, MT) few_kernel<T, DH, MT><<<grid, kWaves * 64, 0, st>>>(a)
-  if (dh == 64) { if (mt == 1) GO(64, 1); else GO(64, 2); }
-  else { if (mt == 1) GO(128, 1); else GO(128, 2); }
+hipError_t launch_fourbit_few(hipStream_t st, int dh, int mt, int waves, unsigned grid, const AttentionArgs<T>& a) {
+#define GO(DH, MT, NW) few_kernel<T, DH, MT, NW><<<grid, NW * 64, 0, st>>>(a)
+  if (dh == 64) { if (mt == 2) GO(64, 2, 4); else if (waves == 8) GO(64, 1, 8); else GO(64, 1, 4); }
+  else { if (mt == 2) GO(128, 2, 4); else if (waves == 8) GO(128, 1, 8); else GO(128, 1, 4); }
 #undef GO
   return hipGetLastError();
 }
-template hipError_t launch_fourbit_few<bf16_t>(hipStream_t, int, int, unsigned, const AttentionArgs<bf16_t>&);
-template hipError_t launch_fourbit_few<float>(hipStream_t, int, int, unsigned, const AttentionArgs<float>&);
+template hipError_t launch_fourbit_few<bf16_t>(hipStream_t, int, int, int, unsigned, const AttentionArgs<bf16_t>&);
+template hipError_t launch_fourbit_few<float>(hipStream_t, int, int, int, unsigned, const AttentionArgs<float>&);
