@@ -21,6 +21,11 @@ __device__ __forceinline__ bf16x8 fourbit_eight(uint32_t codes, float scale) {
 }
 __device__ __forceinline__ float fourbit_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Rows of one head as a buffer of `bytes`: loads from there on give zeros, codes and scales that read as zero.
+__device__ __forceinline__ auto head_buffer(const uint8_t* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, bytes, 0x00020000);
+}
+
 // A cache as the kernels take it.  Rows of K and of V lie alike: row j of head bh has its codes at (bh * cap + j) * dh / 2.
 struct FourBitView {
   const uint8_t* codes[2];               // K, V

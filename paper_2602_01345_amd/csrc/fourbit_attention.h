@@ -50,11 +50,12 @@ __device__ __forceinline__ void store_four(T* dst, f32x4 v, float f) {
 // Byte offset of 16-byte chunk c of row r in an LDS tile of rows of ROWB bytes: chunk c lies in place c ^ f(r).  f is a sum of
 // r's bits chosen so that none of these meets a bank twice, whether 128 or 256 bytes are served at a time: one chunk of 8 or 16
 // rows running (operands read along the rows, rows written); two neighbouring chunks of rows 4 i .. 4 i + 3 and of the 4 behind
-// them, four chunks of 4 rows (transposing reads by 16 or 32 lanes).  With the usual f(r) = r mod 16 transposing reads take
-// twice the time: 57 % of the LDS cycles of attend many, 128 channels, were conflicts.  f repeats after 16 rows.
+// them, four chunks of 4 rows (transposing reads by 16 or 32 lanes).  The top bit of c goes into the lowest place bit, for eight
+// lanes that write a chunk each of the groups of two or four rows.  With the usual f(r) = r mod 16 transposing reads take
+// twice the time: 57 % of the LDS cycles with many rows of 128 channels were conflicts.  f repeats after 16 rows.
 template <int ROWB>
 __device__ __forceinline__ int swz(int r, int c) {
-  const int f = 2 * (r & 3) ^ 3 * ((r >> 2) & 1) ^ (ROWB == 256 ? 8 * ((r ^ (r >> 3)) & 1) : (r >> 3) & 1);
+  const int f = 2 * (r & 3) ^ 3 * ((r >> 2) & 1) ^ (ROWB == 256 ? 8 * ((r ^ (r >> 3)) & 1) ^ c >> 3 : ((r >> 3) & 1) ^ c >> 2);
   return r * ROWB + ((c ^ f) << 4);
 }
 
@@ -81,6 +82,8 @@ struct AttentionArgs {
   // there on; the latter leave sums against their own reference to be joined: part_o [run][row of the block][dh] and part_ml
   // [run][row of the block] (reference in log2 units, sum)
   int blocks, items;     // of rows per key head; in all
+  int dealt;             // items of key heads that come in eights
+  uint32_t blocks_inv, hk_inv, G_inv, nsplit_inv;
   int n_whole, nsplit;
   int run_tiles;         // tiles per run; 0: an item's tiles divided by nsplit
   float* part_o;
@@ -89,24 +92,24 @@ struct AttentionArgs {
   // Key head (of all images') and block of rows of an item.  Workgroups are dealt to the 8 XCDs in turn: the blocks of one key
   // head go to one XCD and share its L2, eight key heads running to the eight XCDs, so that images of different lengths load
   // them alike.  What is left of the key heads goes as it comes.
-  __device__ __forceinline__ void place(int item, int& bh, int& block) const {
-    const int dealt = items / (8 * blocks) * 8 * blocks;
+  __device__ __forceinline__ void place(int item, int& b, int& j, int& block) const {
+    int bh;
     if (item < dealt) {
-      const int i = item >> 3, g = i / blocks;
-      bh = g * 8 + (item & 7);
-      block = i - g * blocks;
+      bh = div_by(item >> 3, blocks, blocks_inv, block) * 8 + (item & 7);
     } else {
-      bh = item / blocks;
-      block = item - bh * blocks;
+      bh = div_by(item, blocks, blocks_inv, block);
     }
+    b = div_by(bh, c.hk, hk_inv, j);
   }
   __device__ __forceinline__ const T* query(int b, int j, int row) const {
-    const int s = row / G;
-    return q + b * q_sb + s * q_sr + (j * G + (row - s * G)) * q_sh;
+    int g;
+    const int s = div_by(row, G, G_inv, g);
+    return q + b * q_sb + s * q_sr + (j * G + g) * q_sh;
   }
   __device__ __forceinline__ int64_t out_row(int b, int j, int row) const {
-    const int s = row / G;
-    return ((int64_t)b * n + s) * heads + j * G + (row - s * G);
+    int g;
+    const int s = div_by(row, G, G_inv, g);
+    return ((int64_t)b * n + s) * heads + j * G + g;
   }
 };
 

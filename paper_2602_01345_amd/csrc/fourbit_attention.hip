@@ -36,17 +36,17 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
   const int run = blockIdx.x - a.n_whole;
   const int split_i = whole ? 0 : run % a.nsplit;
   const int nparts = whole ? 1 : a.nsplit;
-  int bh, block;
-  a.place(whole ? blockIdx.x : a.n_whole + run / a.nsplit, bh, block);
-  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  int b, j, block;
+  a.place(whole ? blockIdx.x : a.n_whole + run / a.nsplit, b, j, block);
+  const int64_t bh = (int64_t)b * a.c.hk + j;
   const int row0 = block * kRows;
   const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
   const int ntiles = row0 < live ? (len + kTile - 1) / kTile : 0;
   const int per = (ntiles + nparts - 1) / nparts;
   const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
 
-  const uint8_t* codes[2] = {a.c.codes[0] + (int64_t)bh * a.c.cap * (DH / 2), a.c.codes[1] + (int64_t)bh * a.c.cap * (DH / 2)};
-  const uint8_t* scales[2] = {a.c.scales[0] + (int64_t)bh * a.c.cap * GPR, a.c.scales[1] + (int64_t)bh * a.c.cap * GPR};
+  const uint8_t* codes[2] = {a.c.codes[0] + bh * a.c.cap * (DH / 2), a.c.codes[1] + bh * a.c.cap * (DH / 2)};
+  const uint8_t* scales[2] = {a.c.scales[0] + bh * a.c.cap * GPR, a.c.scales[1] + bh * a.c.cap * GPR};
 
   // this thread's quarter (the wave's) of row lane of a tile, so that neighbouring lanes write one chunk of neighbouring rows: rows past the last take the last one's place (their scores are set to
   // -inf below, their values are those of a row that counts)
@@ -252,9 +252,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block
   const int tid = threadIdx.x, c4 = tid % C4, sl = tid / C4 % SL;
   const int64_t r = (int64_t)blockIdx.x * RPW + tid / (C4 * SL);
   const int ci = (int)(r / used_rows), rr = (int)(r - (int64_t)ci * used_rows);
-  int bh, block;
-  a.place(min(a.n_whole + ci, a.items - 1), bh, block);
-  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  int b, j, block;
+  a.place(min(a.n_whole + ci, a.items - 1), b, j, block);
   const int row = block * block_rows + rr;
   const int len = image_prior(a.kv_rows, b, a.P);
   const bool there = a.n_whole + ci < a.items && row < a.n * a.G;
@@ -325,9 +324,9 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
     if (want > 4 && p.mt == 1 && ntiles <= kFewWhole) {
       p.waves = 8;
     } else if (want > 4) {
-      p.n_whole = 0;
       p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
       p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
+      if (p.nsplit > 1) p.n_whole = 0;
     }
     return p;
   }
@@ -357,7 +356,9 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
   a.scale_log2 = scale_log2 == 0.f ? 1e-30f : scale_log2;
   a.out = static_cast<T*>(out);
   a.lse = lse;
-  a.blocks = p.blocks; a.items = p.items; a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles;
+  a.blocks = p.blocks; a.items = p.items; a.dealt = p.items / (8 * p.blocks) * 8 * p.blocks;
+  a.blocks_inv = div_inv(p.blocks); a.hk_inv = div_inv(c.kv_heads); a.G_inv = div_inv(a.G); a.nsplit_inv = div_inv(p.nsplit);
+  a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
   const unsigned grid = (unsigned)(p.n_whole + p.runs());

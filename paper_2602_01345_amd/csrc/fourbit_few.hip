@@ -33,10 +33,8 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
   const int piece = blockIdx.x, nparts = a.nsplit;
-  const int item = piece / nparts, split_i = piece - item * nparts;
-  int bh, block;
-  a.place(item, bh, block);
-  const int b = bh / a.c.hk, j = bh - b * a.c.hk;
+  int split_i, b, j, block;
+  a.place(div_by(piece, nparts, a.nsplit_inv, split_i), b, j, block);
   const int row0 = block * 16 * MT;
   const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
   const int ntiles = row0 < live ? (len + kTile - 1) / kTile : 0;
@@ -44,37 +42,35 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
   const int t0 = split_i * a.run_tiles, t1 = min(ntiles, t0 + a.run_tiles);
   if (nparts > 1 && t0 >= t1) return;
 
-  const uint8_t* kc = a.c.codes[0] + (int64_t)bh * a.c.cap * (DH / 2);
-  const uint8_t* vc = a.c.codes[1] + (int64_t)bh * a.c.cap * (DH / 2);
-  const uint8_t* ks = a.c.scales[0] + (int64_t)bh * a.c.cap * GPR;
-  const uint8_t* vs = a.c.scales[1] + (int64_t)bh * a.c.cap * GPR;
-
-  // Rows past the last take the last one's place: their scores are set to -inf, their values are those of a row that counts.
+  const int64_t base = ((int64_t)b * a.c.hk + j) * a.c.cap;
+  const auto kc = head_buffer(a.c.codes[0] + base * (DH / 2), len * (DH / 2)), ks = head_buffer(a.c.scales[0] + base * GPR, len * GPR);
+  const auto vc = head_buffer(a.c.codes[1] + base * (DH / 2), len * (DH / 2)), vs = head_buffer(a.c.scales[1] + base * GPR, len * GPR);
+  const uint32_t k_lane = col * (DH / 2) + grp * (DH / 8), ks_lane = col * GPR + grp * GPR / 4;
   uint32_t kw[4][KW], vw[VL][4], kb[4], vb[VL];
   auto load_k = [&](int t) {
+    const uint32_t o = k_lane + t * (kTile * DH / 2), os = ks_lane + t * (kTile * GPR);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t r = min(t * kTile + i * 16 + col, len - 1);
       if constexpr (DH == 128) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(kc + r * 64 + grp * 16);
+        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(kc, o + i * 16 * (DH / 2), 0, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) kw[i][e] = w[e];
       } else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(kc + r * 32 + grp * 8);
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(kc, o + i * 16 * (DH / 2), 0, 0);
         kw[i][0] = w[0];
         kw[i][1] = w[1];
       }
-      kb[i] = ks[r * GPR + grp * GPR / 4];
+      kb[i] = __builtin_amdgcn_raw_buffer_load_b8(ks, os + i * 16 * GPR, 0, 0);
     }
   };
   auto load_v = [&](int t) {
+    const uint32_t o = lane * 16 + t * (kTile * DH / 2), os = lane + t * (kTile * GPR);
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const uint32_t r = min(t * kTile + i * VR + lane / GPR, len - 1);
-      const u32x4 w = *reinterpret_cast<const u32x4*>(vc + r * (DH / 2) + lane % GPR * 16);
+      const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(vc, o + i * 1024, 0, 0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) vw[i][e] = w[e];
-      vb[i] = vs[r * GPR + lane % GPR];
+      vb[i] = __builtin_amdgcn_raw_buffer_load_b8(vs, os + i * 64, 0, 0);
     }
   };
 
@@ -109,6 +105,21 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
     for (int d = 0; d < DT; ++d) vaddr[d] = swz<ROWB>(r, 2 * d + ((col & 3) >> 1)) + (col & 1) * 8;
   }
 
+  // values of 32 keys through the wave's LDS (its reads and writes are done in order): a lane's groups of channels
+  char* lay_at[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) lay_at[e] = sv + swz<ROWB>(lane / GPR, lane % GPR * 4 + e);
+  auto lay = [&](int u) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < VL / 2; ++i) {
+      const float scale = fourbit_scale(vb[u * VL / 2 + i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)        // the swizzle repeats after 16 rows
+        *reinterpret_cast<bf16x8*>(lay_at[e] + i * VR * ROWB) = fourbit_eight(vw[u * VL / 2 + i][e], scale);
+    }
+    asm volatile("" ::: "memory");
+  };
   for (int t = first; t < t1; t += NW) {
     const bool more = t + NW < t1;
     // ---- scores: register r of tile i is key 16 i + 4 grp + r, for row col
@@ -128,6 +139,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
       }
     }
     if (more) load_k(t + NW);
+    lay(0);
 
     // ---- softmax: probabilities are 2^(score - m_run) against a reference that moves only when a sum of them says that some
     // score lies far above it, or there is none yet (-inf): no largest score, no lanes asked in the common case
@@ -179,20 +191,13 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
       l_run[mt] += psum;
     }
 
-    // ---- values, 32 keys at a time through the wave's LDS (its reads and writes are done in order)
+    // ---- O^T += V^T P^T, 32 keys at a time
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int i = u * VL / 2; i < (u + 1) * VL / 2; ++i) {
-        const float scale = fourbit_scale(vb[i]);
-        const int r = (i - u * VL / 2) * VR + lane / GPR, c = lane % GPR * 4;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<bf16x8*>(sv + swz<ROWB>(r, c + e)) = fourbit_eight(vw[i][e], scale);
+      if (u == 1) {
+        lay(1);
+        if (more) load_v(t + NW);
       }
-      asm volatile("" ::: "memory");
-      if (u == 1 && more) load_v(t + NW);
       bf16x8 pf[MT][NP];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -211,7 +216,6 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
 #pragma unroll
           for (int p = NP - 1; p >= 0; --p) o[mt][d] = mfma16(vf, pf[mt][p], o[mt][d]);
       }
-      asm volatile("" ::: "memory");
     }
   }
 
