@@ -466,6 +466,21 @@ int nova_fourbit_evict(nova_ctx* ctx, void* stream, const nova_fourbit_cache* sr
                        int32_t* kv_len_next, const float* mass_src, float* mass_dst);
 
 /*
+ * nova_pruned_block_rows with the block's cache in 4 bits: the kept rows' keys and values are quantised and appended to `cache`,
+ * and attention reads prior and kept rows from there.  Everything else, variants and per-image counts included, as there, with
+ *   shape    kv_capacity is cache->capacity (no multiple needed); heads of 64 or 128 channels in either dtype
+ *   cache    B, kv_heads = heads, dh of the shape
+ *   mass     fp32 [B, capacity] or NULL: the weight that the rows have collected after this block, from mass_in [B, capacity]
+ *            (NULL: none before; may be the mass array itself) and the kept queries of this call, as nova_fourbit_mass
+ *   workspace  of at least nova_fourbit_block_workspace_bytes(shape), 256-byte aligned
+ */
+size_t nova_fourbit_block_workspace_bytes(const nova_block_shape* shape);
+int nova_pruned_block_fourbit(nova_ctx* ctx, void* stream, const nova_block_shape* shape, const nova_block_weights* weights,
+                              const nova_block_variant* variant, const int32_t* k_per_row, const int32_t* kv_len_per_row,
+                              int32_t* kv_len_next, const void* x, const int32_t* kept_idx, const nova_fourbit_cache* cache,
+                              const float* mass_in, float* mass, void* y_kept, void* workspace, size_t workspace_bytes);
+
+/*
  * Instrumentation (not part of the hot path): per-kernel device timing with HIP events on
  * the caller's stream.  While a stage's bit is set in `stage_mask`, every launch of that
  * stage by the four entry points is bracketed by a pair of events (created on the host as

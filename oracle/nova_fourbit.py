@@ -107,3 +107,44 @@ def evict(half: Tuple[np.ndarray, np.ndarray], dst: Tuple[np.ndarray, np.ndarray
             else:
                 codes[b, :, s], scales[b, :, s] = 0, 127
     return codes, scales
+
+
+def block(x: np.ndarray, idx: np.ndarray, weights, K: np.ndarray, V: np.ndarray, heads: int, lens: Sequence[int],
+          counts: Sequence[int], gelu_form: str = "erf", qk_scale=None, ada=None):
+    """The pruned block on cached rows as they read: K, V values [B, heads, capacity, dh], image b's kept tokens
+    idx[b, :counts[b]] among its lens[b] rows (prior ones first, its own behind them).  Returns y_kept [B, k, C], the keys and
+    values [B, k, C] of the kept tokens before they are quantised, and the weight the rows collect [B, capacity]."""
+    from . import nova_oracle as O
+    x = np.asarray(x, dtype=np.float64)
+    W = {n: np.asarray(a, dtype=np.float64) for n, a in weights.items() if a is not None}
+    B, _, C = x.shape
+    k, dh = idx.shape[1], C // heads
+    y, kn, vn = (np.zeros((B, k, C)) for _ in range(3))
+    got = np.zeros((B, K.shape[2]))
+    act = {"erf": O.gelu, "tanh": O.gelu_tanh}[gelu_form]
+    for b in range(B):
+        c, L = int(counts[b]), int(lens[b])
+        if c == 0:
+            continue
+        s1 = b1 = s2 = b2 = 0.0
+        g1 = g2 = 1.0
+        if ada is not None:
+            b1, s1, g1, b2, s2, g2 = np.asarray(ada, dtype=np.float64)[b]
+        xs = x[b, idx[b, :c]]
+        qkv = (O.layer_norm(xs) * (1 + s1) + b1) @ W["w_qkv"].T + W.get("b_qkv", 0.0)
+        q, kn[b, :c], vn[b, :c] = qkv[:, :C], qkv[:, C:2 * C], qkv[:, 2 * C:]
+        a = np.zeros((c, C))
+        for h in range(heads):
+            sl = slice(h * dh, (h + 1) * dh)
+            scale = 1 / np.sqrt(dh)
+            qh = q[:, sl]
+            if qk_scale is not None:
+                qh, scale = O.unit_rows(qh), float(qk_scale[h])
+                kn[b, :c, sl] = O.unit_rows(kn[b, :c, sl])
+            p = O.softmax(scale * (qh @ K[b, h, :L].T))
+            got[b, :L] += p.sum(0)
+            a[:, sl] = p @ V[b, h, :L]
+        x1 = xs + g1 * (a @ W["w_o"].T + W.get("b_o", 0.0))
+        hid = act((O.layer_norm(x1) * (1 + s2) + b2) @ W["w_fc1"].T + W.get("b_fc1", 0.0))
+        y[b, :c] = x1 + g2 * (hid @ W["w_fc2"].T + W.get("b_fc2", 0.0))
+    return y, kn, vn, got

@@ -199,8 +199,11 @@ def load_library() -> C.CDLL:
     lib.nova_fourbit_attention.argtypes = [vp, vp, i32, cache, i32, i32, rows, vp, i32, vp, C.c_float, vp, vp, vp, sz]
     lib.nova_fourbit_mass.argtypes = [vp, vp, i32, cache, i32, i32, rows, vp, i32, vp, C.c_float, vp, vp, vp, vp, sz]
     lib.nova_fourbit_evict.argtypes = [vp, vp, cache, cache, i32, vp, vp, i32, vp, vp, vp, vp]
+    lib.nova_fourbit_block_workspace_bytes.argtypes, lib.nova_fourbit_block_workspace_bytes.restype = [C.POINTER(_Shape)], sz
+    lib.nova_pruned_block_fourbit.argtypes = [vp, vp, C.POINTER(_Shape), C.POINTER(_Weights), C.POINTER(_Variant), vp, vp, vp, vp,
+                                              vp, cache, vp, vp, vp, vp, sz]
     for f in (lib.nova_fourbit_append, lib.nova_fourbit_unpack, lib.nova_fourbit_attention, lib.nova_fourbit_mass,
-              lib.nova_fourbit_evict):
+              lib.nova_fourbit_evict, lib.nova_pruned_block_fourbit):
         f.restype = i32
     for f in (lib.nova_fourbit_attention_workspace_bytes, lib.nova_fourbit_mass_workspace_bytes):
         f.argtypes, f.restype = [cache, i32, i32, i32], sz
@@ -625,6 +628,31 @@ class Nova:
             _shaped("mass_dst", mass_dst, (B, d.capacity), torch.float32))
         if rc:
             self._check(rc, "nova_fourbit_evict")
+
+    def fourbit_block_workspace_bytes(self, shape: BlockShape) -> int:
+        return self.lib.nova_fourbit_block_workspace_bytes(C.byref(shape.c_struct()))
+
+    def pruned_block_fourbit(self, shape: BlockShape, weights: Dict[str, Optional[torch.Tensor]],
+                             variant: Optional[BlockVariant], k_per_row: Optional[torch.Tensor],
+                             kv_len_per_row: Optional[torch.Tensor], kv_len_next: Optional[torch.Tensor],
+                             x: torch.Tensor, kept_idx: torch.Tensor, cache: FourBitCache, y_kept: torch.Tensor,
+                             workspace: torch.Tensor, mass: Optional[torch.Tensor] = None,
+                             mass_in: Optional[torch.Tensor] = None):
+        """nova_pruned_block_fourbit: pruned_block_rows with the block's cache in 4 bits; mass [B, capacity] f32 (and mass_in,
+        what the rows had before) where the weight they collect is wanted."""
+        c = self._cache(cache)
+        B = shape.B
+        self._here(x, kept_idx, y_kept, workspace, mass, mass_in)
+        s = shape.c_struct()
+        w = _Weights(*[_ptr(weights.get(n)) for n, _ in _Weights._fields_])
+        rc = self.lib.nova_pruned_block_fourbit(
+            self.ctx, _stream(self.device), C.byref(s), C.byref(w), None if variant is None else C.byref(variant.c_struct()),
+            self._counts(B, "k_per_row", k_per_row), self._counts(B, "kv_len_per_row", kv_len_per_row),
+            self._counts(B, "kv_len_next", kv_len_next), _ptr(x), _ptr(kept_idx), c,
+            _shaped("mass_in", mass_in, (B, c.capacity), torch.float32), _shaped("mass", mass, (B, c.capacity), torch.float32),
+            _ptr(y_kept), _ptr(workspace), workspace.nbytes)
+        if rc:
+            self._check(rc, "nova_pruned_block_fourbit")
 
 
 # ------------------------------------------------------------------------------------

@@ -117,6 +117,78 @@ int fourbit_query_error(int dtype, const nova_fourbit_cache* cache, int heads, i
   return rows_error(q, dtype, cache->B, n, heads, true);
 }
 
+// What the block calls check of everything but the cache and the workspace; `plain`: the shape to hold against the kernels'
+// limits.  Sets `var`.  Returns 1 where there is nothing to do.
+int block_error(const nova_block_shape* plain, const nova_block_weights* weights, const nova_block_variant* variant,
+                const RowCounts& rows, const void* x, const int32_t* kept_idx, const void* y_kept, nova_block_variant* var) {
+  if (!weights) return NOVA_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)rows.k_rows, (const void*)rows.kv_rows, (const void*)rows.kv_next})
+    if (reinterpret_cast<uintptr_t>(p) & 3) return NOVA_ERR_INVALID_ARG;
+  *var = {};
+  if (variant) *var = *variant;
+  if ((var->gelu_tanh != 0 && var->gelu_tanh != 1) || (var->qk_norm != 0 && var->qk_norm != 1))
+    return NOVA_ERR_INVALID_ARG;
+  if (var->qk_norm && (!var->qk_scale || (reinterpret_cast<uintptr_t>(var->qk_scale) & 3) != 0))
+    return NOVA_ERR_INVALID_ARG;
+  if (var->ada && !aligned16(var->ada)) return NOVA_ERR_INVALID_ARG;
+  if (int rc = shape_error(plain)) return rc;
+  if (var->w_cq) {
+    if (!var->w_co || !var->k_text || !var->v_text) return NOVA_ERR_INVALID_ARG;
+    if (var->text_len < 1 || var->text_len > var->text_capacity) return NOVA_ERR_INVALID_ARG;
+    const void* cptrs[] = {var->w_cq, var->b_cq, var->w_co, var->b_co, var->k_text, var->v_text};
+    for (const void* p : cptrs)
+      if (p && !aligned16(p)) return NOVA_ERR_INVALID_ARG;
+    const int dh = plain->C / plain->heads;
+    if (plain->dtype == NOVA_BF16 ? var->text_capacity % 64 != 0 : (int64_t)var->text_len + dh > 16384)
+      return NOVA_ERR_UNSUPPORTED;
+  }
+  if (plain->k == 0 || plain->B == 0) return 1;
+  if (!x || !kept_idx || !y_kept) return NOVA_ERR_INVALID_ARG;
+  if (!weights->w_qkv || !weights->w_o || !weights->w_fc1 || !weights->w_fc2) return NOVA_ERR_INVALID_ARG;
+  const void* ptrs[] = {x, y_kept, weights->w_qkv, weights->w_o, weights->w_fc1, weights->w_fc2,
+                        weights->b_qkv, weights->b_o, weights->b_fc1, weights->b_fc2};
+  for (const void* p : ptrs)
+    if (p && !aligned16(p)) return NOVA_ERR_INVALID_ARG;
+  return NOVA_OK;
+}
+
+// The shape of a block whose cache is held in 4 bits as the other kernels see it: kept rows in a cache of their own.
+nova_block_shape fourbit_plain_shape(const nova_block_shape& s) {
+  nova_block_shape p = s;
+  p.kv_len = 0;
+  p.kv_capacity = s.k > 0 && s.k <= INT32_MAX - 63 ? (s.k + 63) / 64 * 64 : 64;
+  return p;
+}
+int fourbit_shape_error(const nova_block_shape* s) {
+  if (!s) return NOVA_ERR_INVALID_ARG;
+  const nova_block_shape p = fourbit_plain_shape(*s);
+  if (int rc = shape_error(&p)) return rc;
+  if (s->kv_len < 0 || (int64_t)s->kv_len + s->k > s->kv_capacity) return NOVA_ERR_INVALID_ARG;
+  const int dh = s->C / s->heads;
+  if ((dh != 64 && dh != 128) || s->kv_capacity > 1 << 24 || s->B > 65535 || s->heads > 32767 ||
+      (int64_t)s->B * s->heads * std::max(s->k, 1) > (int64_t)1 << 30)
+    return NOVA_ERR_UNSUPPORTED;
+  return NOVA_OK;
+}
+// Its workspace: that of the block, then the kept rows' keys and values, lengths, logarithms, and the attention's own.
+size_t carve_fourbit(const nova_block_shape& s, void* base, FourBitBlock* fb) {
+  const nova_block_shape p = fourbit_plain_shape(s);
+  const size_t rows = (size_t)s.B * s.heads, dh = s.C / s.heads, total = (size_t)s.kv_len + s.k;
+  const nova_fourbit_cache c = {nullptr, nullptr, nullptr, nullptr, s.B, s.heads, s.kv_capacity, (int32_t)dh};
+  size_t off = up256(carve_workspace(p, nullptr).total);
+  char* b = static_cast<char*>(base);
+  const size_t half = up256(rows * p.kv_capacity * dh * esize(s.dtype));
+  fb->pitch = p.kv_capacity;
+  fb->k_new = b + off; off += half;
+  fb->v_new = b + off; off += half;
+  fb->kv_after = reinterpret_cast<int32_t*>(b + off); off += up256((size_t)s.B * 4);
+  fb->lse = reinterpret_cast<float*>(b + off); off += up256(rows * s.k * 4);
+  fb->work = b + off;
+  off += up256(std::max(fourbit_attention_workspace_bytes(c, s.heads, s.k, (int)total),
+                        fourbit_mass_workspace_bytes(c, s.heads, s.k, (int)total)));
+  return off;
+}
+
 }  // namespace
 
 BlockWorkspace carve_workspace(const nova_block_shape& s, void* base) {
@@ -428,35 +500,11 @@ int nova_pruned_block_rows(nova_ctx* ctx, void* stream, const nova_block_shape* 
                            const int32_t* k_per_row, const int32_t* kv_len_per_row, int32_t* kv_len_next,
                            const void* x, const int32_t* kept_idx, void* k_cache, void* v_cache, void* y_kept,
                            void* workspace, size_t workspace_bytes) {
-  if (!ctx || !weights) return NOVA_ERR_INVALID_ARG;
-  for (const void* p : {(const void*)k_per_row, (const void*)kv_len_per_row, (const void*)kv_len_next})
-    if (reinterpret_cast<uintptr_t>(p) & 3) return NOVA_ERR_INVALID_ARG;
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
   const RowCounts rows = {k_per_row, kv_len_per_row, kv_len_next};
-  nova_block_variant var = {};
-  if (variant) var = *variant;
-  if ((var.gelu_tanh != 0 && var.gelu_tanh != 1) || (var.qk_norm != 0 && var.qk_norm != 1))
-    return NOVA_ERR_INVALID_ARG;
-  if (var.qk_norm && (!var.qk_scale || (reinterpret_cast<uintptr_t>(var.qk_scale) & 3) != 0))
-    return NOVA_ERR_INVALID_ARG;
-  if (var.ada && !aligned16(var.ada)) return NOVA_ERR_INVALID_ARG;
-  if (int rc = shape_error(shape)) return rc;
-  if (var.w_cq) {
-    if (!var.w_co || !var.k_text || !var.v_text) return NOVA_ERR_INVALID_ARG;
-    if (var.text_len < 1 || var.text_len > var.text_capacity) return NOVA_ERR_INVALID_ARG;
-    const void* cptrs[] = {var.w_cq, var.b_cq, var.w_co, var.b_co, var.k_text, var.v_text};
-    for (const void* p : cptrs)
-      if (p && !aligned16(p)) return NOVA_ERR_INVALID_ARG;
-    const int dh = shape->C / shape->heads;
-    if (shape->dtype == NOVA_BF16 ? var.text_capacity % 64 != 0 : (int64_t)var.text_len + dh > 16384)
-      return NOVA_ERR_UNSUPPORTED;
-  }
-  if (shape->k == 0 || shape->B == 0) return NOVA_OK;
-  if (!x || !kept_idx || !k_cache || !v_cache || !y_kept) return NOVA_ERR_INVALID_ARG;
-  if (!weights->w_qkv || !weights->w_o || !weights->w_fc1 || !weights->w_fc2) return NOVA_ERR_INVALID_ARG;
-  const void* ptrs[] = {x, k_cache, v_cache, y_kept, weights->w_qkv, weights->w_o, weights->w_fc1, weights->w_fc2,
-                        weights->b_qkv, weights->b_o, weights->b_fc1, weights->b_fc2};
-  for (const void* p : ptrs)
-    if (p && !aligned16(p)) return NOVA_ERR_INVALID_ARG;
+  nova_block_variant var;
+  if (int rc = block_error(shape, weights, variant, rows, x, kept_idx, y_kept, &var)) return rc == 1 ? NOVA_OK : rc;
+  if (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)) return NOVA_ERR_INVALID_ARG;
   const size_t need = carve_workspace(*shape, nullptr).total;
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)
     return NOVA_ERR_WORKSPACE;
@@ -647,6 +695,51 @@ int nova_fourbit_evict(nova_ctx* ctx, void* stream, const nova_fourbit_cache* sr
   if (device.rc) return device.rc;
   return launch_fourbit_evict(static_cast<hipStream_t>(stream), *src, *dst, k, kept_idx, k_per_row, kv_len, kv_len_per_row,
                               kv_len_next, mass_src, mass_dst) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+size_t nova_fourbit_block_workspace_bytes(const nova_block_shape* shape) {
+  if (fourbit_shape_error(shape) != NOVA_OK || shape->k == 0 || shape->B == 0) return 0;
+  FourBitBlock fb = {};
+  return carve_fourbit(*shape, nullptr, &fb);
+}
+
+int nova_pruned_block_fourbit(nova_ctx* ctx, void* stream, const nova_block_shape* shape, const nova_block_weights* weights,
+                              const nova_block_variant* variant, const int32_t* k_per_row, const int32_t* kv_len_per_row,
+                              int32_t* kv_len_next, const void* x, const int32_t* kept_idx, const nova_fourbit_cache* cache,
+                              const float* mass_in, float* mass, void* y_kept, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  if (int rc = fourbit_shape_error(shape)) return rc;
+  if (int rc = fourbit_error(cache)) return rc;
+  if (cache->B != shape->B || cache->kv_heads != shape->heads || cache->dh != shape->C / shape->heads ||
+      cache->capacity != shape->kv_capacity)
+    return NOVA_ERR_INVALID_ARG;
+  if (int rc = counts_error({mass_in, mass})) return rc;
+  if (mass_in && !mass) return NOVA_ERR_INVALID_ARG;
+  const size_t mass_bytes = (size_t)cache->B * cache->capacity * 4;
+  if (mass_in != mass && overlap(mass_in, mass_bytes, mass, mass_bytes)) return NOVA_ERR_INVALID_ARG;
+  const RowCounts rows = {k_per_row, kv_len_per_row, kv_len_next};
+  nova_block_variant var;
+  const nova_block_shape plain = fourbit_plain_shape(*shape);
+  if (int rc = block_error(&plain, weights, variant, rows, x, kept_idx, y_kept, &var)) return rc == 1 ? NOVA_OK : rc;
+  FourBitBlock fb = {};
+  const size_t need = carve_fourbit(*shape, nullptr, &fb);
+  if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)
+    return NOVA_ERR_WORKSPACE;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  carve_fourbit(*shape, workspace, &fb);
+  fb.cache = *cache;
+  fb.mass_in = mass_in;
+  fb.mass = mass;
+  const BlockWorkspace ws = carve_workspace(plain, workspace);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (shape->dtype == NOVA_BF16)
+    e = launch_block_bf16(ctx, st, *shape, *weights, var, rows, x, kept_idx, nullptr, nullptr, y_kept, ws, &fb);
+  else
+    e = launch_block_f32(ctx, st, *shape, *weights, var, rows, static_cast<const float*>(x), kept_idx, nullptr, nullptr,
+                         static_cast<float*>(y_kept), ws, &fb);
+  return e == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
 }
 
 }  // extern "C"

@@ -17,11 +17,14 @@
 hipError_t launch_block_bf16(nova_ctx* ctx, hipStream_t st, const nova_block_shape& s,
                              const nova_block_weights& w, const nova_block_variant& var, const RowCounts& rc,
                              const void* xv, const int32_t* idx, void* kcv, void* vcv, void* yv,
-                             const BlockWorkspace& ws) {
+                             const BlockWorkspace& ws, const FourBitBlock* fb) {
   const int M = s.B * s.k, C = s.C, F = s.C * s.ffn_mult, dh = s.C / s.heads;
   const bf16_t* x = static_cast<const bf16_t*>(xv);
-  bf16_t* kc = static_cast<bf16_t*>(kcv);
-  bf16_t* vc = static_cast<bf16_t*>(vcv);
+  // with a cache in 4 bits the kept rows' keys and values go to a cache of theirs, without prior rows
+  bf16_t* kc = fb ? reinterpret_cast<bf16_t*>(fb->k_new) : static_cast<bf16_t*>(kcv);
+  bf16_t* vc = fb ? reinterpret_cast<bf16_t*>(fb->v_new) : static_cast<bf16_t*>(vcv);
+  const int cap = fb ? fb->pitch : s.kv_capacity, P = fb ? 0 : s.kv_len;
+  const int32_t* kv_rows = fb ? nullptr : rc.kv_rows;
   bf16_t* y = static_cast<bf16_t*>(yv);
   bf16_t* u = reinterpret_cast<bf16_t*>(ws.u);
   bf16_t* q = reinterpret_cast<bf16_t*>(ws.q);
@@ -35,9 +38,9 @@ hipError_t launch_block_bf16(nova_ctx* ctx, hipStream_t st, const nova_block_sha
   auto ada_row = [&](int j) { return ada ? ada + (int64_t)j * C : nullptr; };
 
   EpiParams<bf16_t> ep = {};
-  ep.C = C; ep.heads = s.heads; ep.dh = dh; ep.cap = s.kv_capacity; ep.P = s.kv_len; ep.k = s.k;
+  ep.C = C; ep.heads = s.heads; ep.dh = dh; ep.cap = cap; ep.P = P; ep.k = s.k;
   ep.idx = idx; ep.Ntok = s.N;
-  ep.k_rows = rc.k_rows; ep.kv_rows = rc.kv_rows;
+  ep.k_rows = rc.k_rows; ep.kv_rows = kv_rows;
   ep.gate_pitch = ada_pitch;
   ep.part = reinterpret_cast<float*>(ws.part_o);          // free once attention is done: K-slice sums of the projections back to C
   ep.part_floats = ws.part_floats;
@@ -66,12 +69,15 @@ hipError_t launch_block_bf16(nova_ctx* ctx, hipStream_t st, const nova_block_sha
     StageTimer t(ctx, st, NOVA_STAGE_QKV);
     e = launch_gemm_bf16(ctx, st, EPI_QKV, in, w.w_qkv, M, 3 * C, C, ep, in != u);
     if (e == hipSuccess && var.qk_norm)
-      e = launch_qk_norm(st, NOVA_BF16, q, kc, var.qk_scale, kAttnLog2e, s.B, s.k, C, s.heads, s.kv_capacity, s.kv_len,
-                         rc.k_rows, rc.kv_rows);
+      e = launch_qk_norm(st, NOVA_BF16, q, kc, var.qk_scale, kAttnLog2e, s.B, s.k, C, s.heads, cap, P, rc.k_rows, kv_rows);
   }
   if (e != hipSuccess) return e;
+  ep.P = s.kv_len; ep.kv_rows = rc.kv_rows;
 
-  {
+  if (fb) {
+    StageTimer t(ctx, st, NOVA_STAGE_ATTENTION);
+    e = launch_fourbit_block_attention(ctx, st, s, rc, *fb, q, 1.0f, attn);
+  } else {
     StageTimer t(ctx, st, NOVA_STAGE_ATTENTION);
     e = launch_attention_bf16(ctx, st, q, kc, vc, s.B, s.k, C, s.heads, s.kv_capacity, s.kv_len + s.k, attn,
                               reinterpret_cast<float*>(ws.part_o), reinterpret_cast<float*>(ws.part_ml), ws.part_floats,

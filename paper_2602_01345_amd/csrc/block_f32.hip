@@ -213,7 +213,14 @@ void gemm(hipStream_t st, const float* A, const float* W, int M, int Nout, int K
 
 hipError_t launch_block_f32(nova_ctx* ctx, hipStream_t st, const nova_block_shape& s, const nova_block_weights& w,
                             const nova_block_variant& var, const RowCounts& rc, const float* x, const int32_t* idx,
-                            float* kc, float* vc, float* y, const BlockWorkspace& ws) {
+                            float* kc, float* vc, float* y, const BlockWorkspace& ws, const FourBitBlock* fb) {
+  // with a cache in 4 bits the kept rows' keys and values go to a cache of theirs, without prior rows
+  if (fb) {
+    kc = reinterpret_cast<float*>(fb->k_new);
+    vc = reinterpret_cast<float*>(fb->v_new);
+  }
+  const int cap = fb ? fb->pitch : s.kv_capacity, P = fb ? 0 : s.kv_len;
+  const int32_t* kv_rows = fb ? nullptr : rc.kv_rows;
   const int M = s.B * s.k, C = s.C, F = s.C * s.ffn_mult, dh = s.C / s.heads;
   float* u = reinterpret_cast<float*>(ws.u);
   float* q = reinterpret_cast<float*>(ws.q);
@@ -227,8 +234,8 @@ hipError_t launch_block_f32(nova_ctx* ctx, hipStream_t st, const nova_block_shap
   auto ada_row = [&](int j) { return ada ? ada + (int64_t)j * C : nullptr; };
 
   EpiParams<float> ep = {};
-  ep.C = C; ep.heads = s.heads; ep.dh = dh; ep.cap = s.kv_capacity; ep.P = s.kv_len; ep.k = s.k;
-  ep.k_rows = rc.k_rows; ep.kv_rows = rc.kv_rows;
+  ep.C = C; ep.heads = s.heads; ep.dh = dh; ep.cap = cap; ep.P = P; ep.k = s.k;
+  ep.k_rows = rc.k_rows; ep.kv_rows = kv_rows;
   ep.idx = idx; ep.Ntok = s.N;
   ep.gate_pitch = ada_pitch;
 
@@ -252,15 +259,19 @@ hipError_t launch_block_f32(nova_ctx* ctx, hipStream_t st, const nova_block_shap
     if (in != u) gemm<EPI_QKV, true>(st, in, static_cast<const float*>(w.w_qkv), M, 3 * C, C, ep);
     else gemm<EPI_QKV>(st, u, static_cast<const float*>(w.w_qkv), M, 3 * C, C, ep);
     if (var.qk_norm) {
-      e = launch_qk_norm(st, NOVA_F32, q, kc, var.qk_scale, 1.0f, s.B, s.k, C, s.heads, s.kv_capacity, s.kv_len,
-                         rc.k_rows, rc.kv_rows);
+      e = launch_qk_norm(st, NOVA_F32, q, kc, var.qk_scale, 1.0f, s.B, s.k, C, s.heads, cap, P, rc.k_rows, kv_rows);
       if (e != hipSuccess) return e;
     }
   }
+  ep.P = s.kv_len; ep.kv_rows = rc.kv_rows;
 
-  const int kv_total = s.kv_len + s.k;
-  const size_t lds = attention_f32_lds(kv_total, dh);
-  {
+  if (fb) {
+    StageTimer t(ctx, st, NOVA_STAGE_ATTENTION);
+    e = launch_fourbit_block_attention(ctx, st, s, rc, *fb, q, var.qk_norm ? kAttnLog2e : kAttnLog2e / sqrtf((float)dh), attn);
+    if (e != hipSuccess) return e;
+  } else {
+    const int kv_total = s.kv_len + s.k;
+    const size_t lds = attention_f32_lds(kv_total, dh);
     StageTimer t(ctx, st, NOVA_STAGE_ATTENTION);
     attention_f32_kernel<<<dim3(M, s.heads), kAttnWaves * NOVA_WAVE, lds, st>>>(q, kc, vc, s.k, C, s.heads, dh, s.kv_capacity,
                                                                    kv_total, var.qk_norm ? 1.0f : 1.0f / sqrtf((float)dh), attn,

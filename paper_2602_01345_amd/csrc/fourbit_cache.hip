@@ -240,3 +240,19 @@ hipError_t launch_fourbit_evict(hipStream_t st, const nova_fourbit_cache& src, c
 #undef GO
   return hipGetLastError();
 }
+
+hipError_t launch_fourbit_block_attention(const nova_ctx* ctx, hipStream_t st, const nova_block_shape& s, const RowCounts& rc,
+                                          const FourBitBlock& fb, const void* q, float scale_log2, void* out) {
+  const int64_t dh = s.C / s.heads, rows = (int64_t)s.heads * fb.pitch * dh;
+  const nova_rows k = {fb.k_new, rows, dh, fb.pitch * dh, 1}, v = {fb.v_new, rows, 1, fb.pitch * dh, fb.pitch};
+  const nova_rows qv = {const_cast<void*>(q), (int64_t)s.k * s.C, s.C, dh, 1};
+  const int total = s.kv_len + s.k;
+  hipError_t e = launch_fourbit_append(st, s.dtype, fb.cache, s.k, &k, &v, rc.k_rows, s.kv_len, rc.kv_rows, fb.kv_after);
+  if (e != hipSuccess) return e;
+  const int32_t* after = rc.k_rows || rc.kv_rows ? fb.kv_after : nullptr;     // every image has `total` rows otherwise
+  e = launch_fourbit_attention(ctx, st, s.dtype, fb.cache, s.heads, s.k, qv, rc.k_rows, total, after, scale_log2, out,
+                               fb.mass ? fb.lse : nullptr, fb.work);
+  if (e != hipSuccess || !fb.mass) return e;
+  return launch_fourbit_mass(ctx, st, s.dtype, fb.cache, s.heads, s.k, qv, rc.k_rows, total, after, scale_log2, fb.lse, fb.mass_in,
+                             fb.mass, fb.work);
+}

@@ -111,10 +111,27 @@ struct RowCounts {
   int32_t* kv_next;
 };
 
-// block_f32.hip: plain fp32 kernels (correctness path for small fp32 models)
+// A block whose cache is held in 4 bits: the projection writes the kept rows' keys and values to k_new / v_new (the block's
+// cache layouts, `pitch` rows), from where they are appended to the cache; attention reads that.
+struct FourBitBlock {
+  nova_fourbit_cache cache;
+  const float* mass_in;
+  float* mass;           // or nullptr
+  int pitch;
+  char *k_new, *v_new;   // [B, heads, pitch, dh], [B, heads, dh, pitch]
+  int32_t* kv_after;     // [B] rows of the images after this block
+  float* lse;            // [B, k, heads]
+  char* work;            // of the attention, then of the masses
+};
+// Append, attention and masses of such a block; q [B, k, C] as the projection wrote it, scale_log2 what its scores are
+// still to be multiplied by.
+hipError_t launch_fourbit_block_attention(const nova_ctx* ctx, hipStream_t st, const nova_block_shape& s, const RowCounts& rc,
+                                          const FourBitBlock& fb, const void* q, float scale_log2, void* out);
+
+// block_f32.hip: plain fp32 kernels (correctness path for small fp32 models); fb: the cache is held in 4 bits (kc, vc unused)
 hipError_t launch_block_f32(nova_ctx* ctx, hipStream_t st, const nova_block_shape& s, const nova_block_weights& w,
                             const nova_block_variant& var, const RowCounts& rc, const float* x, const int32_t* idx,
-                            float* kc, float* vc, float* y, const BlockWorkspace& ws);
+                            float* kc, float* vc, float* y, const BlockWorkspace& ws, const FourBitBlock* fb = nullptr);
 // gemm_bf16.hip: out = epilogue(A W^T) on the matrix cores; mode is an EpiMode
 template <typename T> struct EpiParams;
 // norm: A's rows are normalised on the way (only where gemm_plan.h: gemm_takes_norm), in mode EPI_QKV gathered through ep.idx
@@ -164,7 +181,7 @@ hipError_t launch_attention_few_bf16(hipStream_t st, int waves, const void* q, c
 hipError_t launch_block_bf16(nova_ctx* ctx, hipStream_t st, const nova_block_shape& s,
                              const nova_block_weights& w, const nova_block_variant& var, const RowCounts& rc,
                              const void* x, const int32_t* idx, void* kc, void* vc, void* y,
-                             const BlockWorkspace& ws);
+                             const BlockWorkspace& ws, const FourBitBlock* fb = nullptr);
 
 // fourbit_cache.hip: rows into, out of and between caches in 4 bits (include/nova.h: nova_fourbit_append, _unpack, _evict)
 hipError_t launch_fourbit_append(hipStream_t st, int dtype, const nova_fourbit_cache& c, int n, const nova_rows* k,

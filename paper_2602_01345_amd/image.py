@@ -18,6 +18,10 @@ per block and the counts never leave the device: selection, block and merge take
 array (``nova_select`` / ``nova_pruned_block_rows`` / ``nova_merge_cache_rows``) with the row pitch
 N, and each block's per-image cache lengths are kept in a device array that the block call itself
 advances.  Nothing on that path synchronises with the host.
+
+With ``cache_bits=4`` the K/V caches are held in 4 bits (``nova_pruned_block_fourbit``), and ``evict_to`` bounds them: every
+block collects the attention weight of its cached rows, and after a scale that leaves a block with more rows than that, the
+rows that have collected least go (``nova_select`` on the weights, ``nova_fourbit_evict``).
 """
 from __future__ import annotations
 
@@ -26,7 +30,7 @@ from typing import Dict, List, Optional, Sequence
 
 import torch
 
-from .binding import NOVA_BF16, NOVA_F32, BlockShape, BlockVariant, Nova
+from .binding import NOVA_BF16, NOVA_F32, BlockShape, BlockVariant, FourBitCache, Nova
 
 
 @dataclass
@@ -61,14 +65,30 @@ class ScalePlan:
     cache_prev: List[Optional[torch.Tensor]]
     graph: Optional[torch.cuda.CUDAGraph] = None
     entropies: Optional[List[torch.Tensor]] = None     # per block [B, N] (a pruned scale); entropy is the last block's
+    stores: Optional[List["FourBitStore"]] = None      # cache_bits=4: where each block's rows are during this scale
+    evictions: Optional[List[tuple]] = None            # (store, store it moves to, rows it has) of what is evicted after it
+
+
+@dataclass
+class FourBitStore:
+    """One block's cache in 4 bits, the weights its rows have collected and the images' row counts."""
+    cache: FourBitCache
+    mass: Optional[torch.Tensor]          # [B, capacity] fp32, with evict_to
+    rows: torch.Tensor                    # [B] int32
 
 
 class ImageRunner:
     def __init__(self, nova: Nova, *, B: int, C: int, heads: int, grids: Sequence[int], dtype: torch.dtype,
                  weights: List[Dict[str, torch.Tensor]], ffn_mult: int = 4, device: str = "cuda",
-                 variants: Optional[List[Optional[BlockVariant]]] = None, interp: int = 0):
+                 variants: Optional[List[Optional[BlockVariant]]] = None, interp: int = 0, cache_bits: int = 16,
+                 evict_to: Optional[int] = None):
         """variants: per block, the block variations (nova_pruned_block_variant) or None; interp: the cache
-        interpolation kernel of nova_merge_cache_interp (0 bilinear, 1 nearest, 2 bicubic)."""
+        interpolation kernel of nova_merge_cache_interp (0 bilinear, 1 nearest, 2 bicubic); cache_bits: 16 (K/V in `dtype`)
+        or 4; evict_to (cache_bits=4): rows a block's cache keeps per image from one scale to the next, None: all."""
+        if cache_bits not in (4, 16):
+            raise ValueError(f"cache_bits is 4 or 16, not {cache_bits}")
+        if evict_to is not None and (cache_bits != 4 or evict_to < 1):
+            raise ValueError("evict_to is a positive number of rows and needs cache_bits=4")
         self.nova = nova
         self.variants = variants if variants is not None else [None] * len(weights)
         self.interp = interp
@@ -80,9 +100,22 @@ class ImageRunner:
         self.L = len(weights)
         self.device = device
         dh = C // heads
-        self.cap = (sum(g * g for g in self.grids) + 63) // 64 * 64
-        self.k_cache = [torch.zeros((B, heads, self.cap, dh), dtype=dtype, device=device) for _ in range(self.L)]
-        self.v_cache = [torch.zeros((B, heads, dh, self.cap), dtype=dtype, device=device) for _ in range(self.L)]
+        self.cache_bits, self.evict_to = cache_bits, evict_to
+        if cache_bits == 4:
+            # most rows a block can hold: what the scales before have left of theirs, and all of a scale
+            prior, self.cap = 0, 0
+            for g in self.grids:
+                self.cap = max(self.cap, prior + g * g)
+                prior = prior + g * g if evict_to is None else min(prior + g * g, evict_to)
+            if evict_to is not None and self.cap > 65536:
+                raise ValueError(f"{self.cap} rows per image: nova_select ranks 65536 at most")
+            self.stores = [self._store(dh) for _ in range(self.L)]
+            # where evicted rows move to; the block's former store is the next one's
+            self._spare = self._store(dh) if evict_to is not None else None
+        else:
+            self.cap = (sum(g * g for g in self.grids) + 63) // 64 * 64
+            self.k_cache = [torch.zeros((B, heads, self.cap, dh), dtype=dtype, device=device) for _ in range(self.L)]
+            self.v_cache = [torch.zeros((B, heads, dh, self.cap), dtype=dtype, device=device) for _ in range(self.L)]
         self.kv_len = [0] * self.L                      # rows appended so far, per block
         self.cache: List[Optional[torch.Tensor]] = [None] * self.L     # residual cache of the previous scale
         self.cache_grid: Optional[int] = None
@@ -92,7 +125,28 @@ class ImageRunner:
         self._k_row = torch.empty(B, dtype=torch.int32, device=device)
         # per-image cache lengths of every block (device): exact once images keep different numbers of tokens;
         # kv_len then holds the host's upper bound
-        self.kv_rows = [torch.zeros(B, dtype=torch.int32, device=device) for _ in range(self.L)]
+        self.kv_rows = ([st.rows for st in self.stores] if cache_bits == 4 else
+                        [torch.zeros(B, dtype=torch.int32, device=device) for _ in range(self.L)])
+
+    def _store(self, dh: int) -> FourBitStore:
+        B, dev = self.B, self.device
+        mass = None if self.evict_to is None else torch.empty((B, self.cap), dtype=torch.float32, device=dev)
+        return FourBitStore(FourBitCache.empty(B, self.heads, self.cap, dh, dev), mass, torch.zeros(B, dtype=torch.int32, device=dev))
+
+    def _workspace_bytes(self, shape: BlockShape) -> int:
+        return (self.nova.fourbit_block_workspace_bytes if self.cache_bits == 4 else self.nova.workspace_bytes)(shape)
+
+    def _evict(self, evictions: List[tuple], idx: List[torch.Tensor], mask: List[torch.Tensor], per_image: bool):
+        """Keeps evict_to rows of every (store, store it moves to, rows it has at most)."""
+        n = self.nova
+        n.select_blocks([src.mass for src, _, _ in evictions], [self.evict_to] * len(evictions), idx, mask)
+        for (src, dst, rows), kept in zip(evictions, idx):
+            n.fourbit_evict(src.cache, dst.cache, kept, rows, kv_len_per_row=src.rows if per_image else None,
+                            kv_len_next=dst.rows, mass_src=src.mass, mass_dst=dst.mass)
+
+    def _eviction_buffers(self, n: int):
+        return (list(torch.empty((n, self.B, self.evict_to), dtype=torch.int32, device=self.device)),
+                list(torch.empty((n, self.B, self.cap), dtype=torch.uint8, device=self.device)))
 
     def reset(self):
         """Forget the previous image: cache lengths back to zero, no residual cache (buffers are reused)."""
@@ -106,7 +160,7 @@ class ImageRunner:
         return BlockShape(self.code, self.B, N, self.C, self.heads, self.kv_len[j], self.cap, k, self.ffn_mult)
 
     def _ensure_workspace(self, shape: BlockShape):
-        need = self.nova.workspace_bytes(shape)
+        need = self._workspace_bytes(shape)
         if self._workspace is None or self._workspace.numel() < need:
             self._workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
 
@@ -121,6 +175,9 @@ class ImageRunner:
         prev_cache: List[Optional[torch.Tensor]] = [None] * self.L
         prev_grid = None
         need = 0
+        stores, spare = (list(self.stores), self._spare) if self.cache_bits == 4 else (None, None)
+        self._evict_idx: List[torch.Tensor] = []
+        self._evict_mask: List[torch.Tensor] = []
         for t, g in enumerate(self.grids):
             N = g * g
             dense = t not in k_tables
@@ -145,11 +202,19 @@ class ImageRunner:
                   [torch.empty((B, max(k, 1), C), dtype=self.dtype, device=dev) for k in ks],
                 out=out,
                 cache_new=[torch.empty((B, N, C), dtype=self.dtype, device=dev) if keep else None for _ in ks],
-                cache_prev=list(prev_cache))
+                cache_prev=list(prev_cache), stores=None if stores is None else list(stores))
             for j, k in enumerate(ks):
-                need = max(need, self.nova.workspace_bytes(
+                need = max(need, self._workspace_bytes(
                     BlockShape(self.code, B, N, C, self.heads, kv[j], self.cap, k, self.ffn_mult)))
                 kv[j] += k
+            if spare is not None and t + 1 < len(self.grids):
+                plan.evictions = []
+                for j in range(self.L):
+                    if kv[j] > self.evict_to:
+                        plan.evictions.append((stores[j], spare, kv[j]))
+                        stores[j], spare, kv[j] = spare, stores[j], self.evict_to
+                if len(plan.evictions) > len(self._evict_idx):
+                    self._evict_idx, self._evict_mask = self._eviction_buffers(len(plan.evictions))
             if keep:
                 prev_cache, prev_grid = plan.cache_new, g
             plans.append(plan)
@@ -168,12 +233,20 @@ class ImageRunner:
         for j in range(self.L):
             k = plan.k[j]
             shape = BlockShape(self.code, self.B, N, self.C, self.heads, plan.kv_len[j], self.cap, k, self.ffn_mult)
-            n.pruned_block_variant(shape, self.weights[j], self.variants[j], x, plan.idx[j], self.k_cache[j],
-                                   self.v_cache[j], plan.y[j], self._workspace)
+            if plan.stores is not None:
+                st = plan.stores[j]
+                n.pruned_block_fourbit(shape, self.weights[j], self.variants[j], None, None, None, x, plan.idx[j], st.cache,
+                                       plan.y[j], self._workspace, st.mass, st.mass if plan.kv_len[j] else None)
+            else:
+                n.pruned_block_variant(shape, self.weights[j], self.variants[j], x, plan.idx[j], self.k_cache[j],
+                                       self.v_cache[j], plan.y[j], self._workspace)
             if plan.y[j] is not plan.out[j]:
                 n.merge_cache_interp(self.interp, g, g, plan.prev_grid, plan.prev_grid, k, x, plan.y[j], plan.idx[j],
                                      plan.mask[j], plan.cache_prev[j], plan.out[j], plan.cache_new[j])
             x = plan.out[j]
+        if plan.evictions:
+            m = len(plan.evictions)
+            self._evict(plan.evictions, self._evict_idx[:m], self._evict_mask[:m], per_image=False)
         return x
 
     def capture(self, plan: ScalePlan):
@@ -254,8 +327,13 @@ class ImageRunner:
             cache_new = torch.empty((B, N, C), dtype=self.dtype, device=dev) if keep_cache else None
             # the block reads and advances the per-image cache lengths (equal to kv_len as long as every image
             # has kept the same number of tokens)
-            n.pruned_block_rows(shape, self.weights[j], self.variants[j], k_rows, self.kv_rows[j], self.kv_rows[j], x,
-                                idx, self.k_cache[j], self.v_cache[j], y, self._workspace)
+            if self.cache_bits == 4:
+                st = self.stores[j]
+                n.pruned_block_fourbit(shape, self.weights[j], self.variants[j], k_rows, st.rows, st.rows, x, idx, st.cache, y,
+                                       self._workspace, st.mass, st.mass if self.kv_len[j] else None)
+            else:
+                n.pruned_block_rows(shape, self.weights[j], self.variants[j], k_rows, self.kv_rows[j], self.kv_rows[j], x,
+                                    idx, self.k_cache[j], self.v_cache[j], y, self._workspace)
             pg = self.cache_grid if self.cache[j] is not None else g
             if k_rows is None and not whole:
                 n.merge_cache_interp(self.interp, g, g, pg, pg, k, x, y, idx, mask, self.cache[j], out, cache_new)
@@ -273,5 +351,15 @@ class ImageRunner:
             x = out
         if keep_cache:
             self.cache_grid = g
+        if self.evict_to is not None and t + 1 < len(self.grids):
+            evictions = []
+            for j in range(self.L):
+                if self.kv_len[j] > self.evict_to:
+                    src, dst = self.stores[j], self._spare
+                    evictions.append((src, dst, self.kv_len[j]))
+                    self.stores[j], self._spare, self.kv_len[j] = dst, src, self.evict_to
+                    self.kv_rows[j] = dst.rows
+            if evictions:
+                self._evict(evictions, *self._eviction_buffers(len(evictions)), per_image=True)
         return ScaleResult(out=x, k=ks, mean_entropy=mean if have_mean else None, block_out=outs, block_cache=caches,
                            block_entropy=ents, block_idx=idxs)

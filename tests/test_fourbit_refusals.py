@@ -179,3 +179,49 @@ def test_binding_looks_at_shapes_and_types():
         Bn._shaped("lse", torch.zeros(2, 3), (2, 3, 4), torch.float32)
     with pytest.raises(ValueError):
         Bn._shaped("n_per_row", torch.zeros(2, dtype=torch.int64), (2,), torch.int32)
+
+
+# ---- the block -------------------------------------------------------------------------------------------------------
+def _shape(**kw):
+    v = dict(dtype=1, B=2, N=20, C=128, heads=2, ffn_mult=4, kv_len=50, kv_capacity=100, k=10)
+    v.update(kw)
+    return Bn._Shape(*[v[n] for n, _ in Bn._Shape._fields_])
+
+
+def _block(lib, shape=None, cache=None, weights=True, variant=None, k_rows=None, kv_rows=None, kv_next=None, x=BASE, idx=BASE,
+           mass_in=None, mass=None, y=BASE, ws=BASE, ws_bytes=1 << 40, ctx=_CTX):
+    w = Bn._Weights(*[BASE * 4] * 8)
+    return lib.nova_pruned_block_fourbit(ctx, None, _ref(shape or _shape()), _ref(w) if weights else None, _ref(variant), k_rows,
+                                         kv_rows, kv_next, x, idx, _ref(cache or _cache()), mass_in, mass, y, ws, ws_bytes)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(ctx=None), INVALID), (dict(weights=False), INVALID), (dict(shape=_shape(dtype=5)), UNSUPPORTED),
+    (dict(shape=_shape(k=21)), INVALID), (dict(shape=_shape(kv_len=91)), INVALID), (dict(shape=_shape(kv_len=-1)), INVALID),
+    (dict(shape=_shape(C=64)), UNSUPPORTED), (dict(shape=_shape(C=192, dtype=0)), UNSUPPORTED),
+    (dict(cache=_cache(B=3)), INVALID), (dict(cache=_cache(kv_heads=1)), INVALID), (dict(cache=_cache(dh=128)), INVALID),
+    (dict(cache=_cache(capacity=101)), INVALID), (dict(k_rows=BASE + 1), INVALID), (dict(kv_rows=BASE + 2), INVALID),
+    (dict(kv_next=BASE + 3), INVALID), (dict(x=None), INVALID), (dict(idx=None), INVALID), (dict(y=None), INVALID),
+    (dict(y=BASE + 8), INVALID), (dict(mass_in=BASE), INVALID), (dict(mass=BASE + 2), INVALID),
+    (dict(mass=BASE, mass_in=BASE + 16), INVALID), (dict(variant=Bn._Variant(2, 0)), INVALID),
+    (dict(variant=Bn._Variant(0, 1)), INVALID), (dict(ws=None), WORKSPACE), (dict(ws=BASE + 128), WORKSPACE),
+])
+def test_block(lib, kw, rc):
+    assert _block(lib, **kw) == rc
+
+
+def test_block_workspace(lib):
+    size = lib.nova_fourbit_block_workspace_bytes
+    need = size(C.byref(_shape()))
+    assert need > lib.nova_workspace_bytes(C.byref(_shape(kv_len=0, kv_capacity=64)))
+    assert _block(lib, ws_bytes=need - 1) == WORKSPACE
+    assert size(None) == 0 and size(C.byref(_shape(k=0))) == 0 and size(C.byref(_shape(kv_len=91))) == 0
+    assert _block(lib, shape=_shape(k=0)) == 0 and _block(lib, shape=_shape(B=0), cache=_cache(B=0)) == 0
+
+
+def test_runner_refuses_what_it_cannot_keep():
+    from paper_2602_01345_amd.image import ImageRunner
+    for kw in (dict(cache_bits=8), dict(evict_to=10), dict(cache_bits=4, evict_to=0),
+               dict(cache_bits=4, evict_to=10 ** 6)):
+        with pytest.raises(ValueError):
+            ImageRunner(None, B=1, C=128, heads=2, grids=[1, 400], dtype=torch.bfloat16, weights=[{}], device="cpu", **kw)
