@@ -239,9 +239,9 @@ def _ptrs(ts: Sequence[torch.Tensor]) -> "C.Array":
 
 def _rows(t: torch.Tensor, heads: int, dh: int, name: str) -> "_Rows":
     """nova_rows of a [B, n, heads, dh] tensor of any strides."""
-    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != dh:
-        raise ValueError(f"{name}: {tuple(t.shape)}, expected [B, n, {heads}, {dh}]")
-    assert t.is_cuda, "device-resident tensors only"
+    shape = t.shape
+    if len(shape) != 4 or shape[2] != heads or shape[3] != dh:
+        raise ValueError(f"{name}: {tuple(shape)}, expected [B, n, {heads}, {dh}]")
     return _Rows(t.data_ptr(), *t.stride())
 
 
@@ -249,9 +249,9 @@ def _shaped(name: str, t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype:
     """Pointer of an optional dense tensor that has to have this shape and type."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
-    return _ptr(t)
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} {t.stride()}, expected dense {tuple(shape)} {dtype}")
+    return t.data_ptr()
 
 
 def _check_lengths(n: int, **lists):

@@ -5,6 +5,10 @@
 // wave has 64 keys, converted once into the operands it holds in registers (the order of the channels in the product is free:
 // a lane takes half a row of the cache as it lies); the rows come in tiles of 32 through LDS, shared by the four waves.
 // A launch leaves sums per key head (and run of rows, where there are few keys); a second one adds them up in a fixed order.
+//
+// Few rows (single tokens, a handful of queries): reading the keys once bounds it, and launches.  The waves of a workgroup take
+// 64 keys of several key heads and add up among themselves, one launch and no workspace.  16 x 16 MFMAs, the keys from the cache
+// into registers, as in fourbit_few.hip.
 #include <algorithm>
 
 #include "fourbit_attention.h"
@@ -178,12 +182,104 @@ __global__ __launch_bounds__(256) void add_kernel(const float* __restrict__ part
   mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
 }
 
+// kHeadWaves waves of a workgroup share 64 keys, each with every kHeadWaves-th key head; kFewWaves / kHeadWaves such groups.
+constexpr int kFewWaves = 8;
+constexpr int kFewRows = 32;         // rows per key head up to which this kernel is taken
+
+template <typename T, int DH, int HW>
+__global__ __launch_bounds__(kFewWaves * 64) void mass_few_kernel(MassArgs<T> a, const float* mass_in, float* mass) {
+  constexpr int NP = kParts<T>, GPR = DH / kGroup, KW = DH / 32, GROUPS = kFewWaves / HW;
+  __shared__ float part[kFewWaves][64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int b = blockIdx.y, key0 = (blockIdx.x * GROUPS + wave / HW) * 64;
+  const int live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};                       // key 16 i + col, rows 4 grp .. + 3 of every sixteen
+  if (key0 < len) {
+    for (int j = wave % HW; j < a.c.hk; j += HW) {
+      const int64_t base = ((int64_t)b * a.c.hk + j) * a.c.cap;
+      const auto kc = head_buffer(a.c.codes[0] + base * (DH / 2), len * (DH / 2)), ks = head_buffer(a.c.scales[0] + base * GPR, len * GPR);
+      const uint32_t o = (key0 + col) * (DH / 2) + grp * (DH / 8), os = (key0 + col) * GPR + grp * GPR / 4;
+      uint32_t kw[4][KW];
+      float kb[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (DH == 128) {
+          const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(kc, o + i * 16 * (DH / 2), 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kw[i][e] = w[e];
+        } else {
+          const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(kc, o + i * 16 * (DH / 2), 0, 0);
+          kw[i][0] = w[0];
+          kw[i][1] = w[1];
+        }
+        kb[i] = fourbit_scale(__builtin_amdgcn_raw_buffer_load_b8(ks, os + i * 16 * GPR, 0, 0));
+      }
+      for (int row0 = 0; row0 < live; row0 += 16) {
+        int g;
+        const int s = div_by(min(row0 + col, live - 1), a.G, a.G_inv, g);
+        const T* qp = a.q + b * a.q_sb + s * a.q_sr + (j * a.G + g) * a.q_sh + grp * (DH / 4);
+        bf16x8 qf[KW][NP];
+#pragma unroll
+        for (int e = 0; e < KW; ++e) load_eight(qp + e * 8, qf[e]);
+        float nl[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = row0 + 4 * grp + r;
+          const int sr = div_by(min(row, live - 1), a.G, a.G_inv, g);
+          nl[r] = row < live ? -kAttnLog2e * a.lse[((int64_t)b * a.n + sr) * a.heads + j * a.G + g] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < KW; ++e) {
+            const bf16x8 kf = fourbit_eight(kw[i][e], kb[i]);
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p) sc = mfma16(qf[e][p], kf, sc);
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale_log2, nl[r]));
+          acc[i] += sum;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    acc[i] += __shfl_xor(acc[i], 16, NOVA_WAVE);
+    acc[i] += __shfl_xor(acc[i], 32, NOVA_WAVE);
+  }
+  part[wave][lane] = grp == 0 ? acc[0] : grp == 1 ? acc[1] : grp == 2 ? acc[2] : acc[3];
+  __syncthreads();
+  if (tid >= GROUPS * 64) return;
+  const int k = blockIdx.x * GROUPS * 64 + tid;
+  if (k >= a.c.cap) return;
+  const int64_t at = (int64_t)b * a.c.cap + k;
+  if (k >= len) {
+    mass[at] = -1.0f;
+    return;
+  }
+  const float m0 = mass_in ? mass_in[at] : 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < HW; ++w) sum += part[wave * HW + w][lane];
+  mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+}
+
 struct Plan {
+  int few;               // waves that share keys, or 0: mass_kernel
   int chunks, nsplit, pitch;
 };
 constexpr int kCus = 256;
 Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
-  Plan p;
+  Plan p = {};
+  if ((int64_t)n * (heads / c.kv_heads) <= kFewRows) {
+    p.few = c.kv_heads >= 8 ? 8 : c.kv_heads >= 4 ? 4 : c.kv_heads >= 2 ? 2 : 1;
+    return p;
+  }
   p.chunks = (kv_len + kKeys - 1) / kKeys;
   p.pitch = (kv_len + 63) / 64 * 64;
   const int64_t items = std::max((int64_t)c.B * c.kv_heads * p.chunks, (int64_t)1);
@@ -207,8 +303,17 @@ hipError_t collect(hipStream_t st, const nova_fourbit_cache& c, int heads, int n
   a.lse = lse;
   a.chunks = p.chunks; a.nsplit = p.nsplit; a.pitch = p.pitch;
   a.part = static_cast<float*>(workspace);
+  if (p.few) {
+    const dim3 grid((c.capacity + kFewWaves / p.few * 64 - 1) / (kFewWaves / p.few * 64), c.B);
+#define GO(DH, HW) mass_few_kernel<T, DH, HW><<<grid, kFewWaves * 64, 0, st>>>(a, mass_in, mass)
+#define GO_DH(DH) if (p.few == 8) GO(DH, 8); else if (p.few == 4) GO(DH, 4); else if (p.few == 2) GO(DH, 2); else GO(DH, 1)
+    if (c.dh == 64) { GO_DH(64); } else { GO_DH(128); }
+#undef GO_DH
+#undef GO
+    return hipGetLastError();
+  }
   int parts = 0;
-  if (n > 0 && P > 0) {
+  if (P > 0) {
     parts = c.kv_heads * p.nsplit;
     const unsigned grid = (unsigned)((int64_t)c.B * c.kv_heads * p.chunks * p.nsplit);
     if (c.dh == 64) mass_kernel<T, 64><<<grid, kWaves * 64, 0, st>>>(a);
