@@ -182,41 +182,46 @@ __global__ __launch_bounds__(256) void add_kernel(const float* __restrict__ part
   mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
 }
 
-// kHeadWaves waves of a workgroup share 64 keys, each with every kHeadWaves-th key head; kFewWaves / kHeadWaves such groups.
+// HW waves of a workgroup share NT tiles of 64 keys, each with every HW-th key head; kFewWaves / HW such groups.
 constexpr int kFewWaves = 8;
 constexpr int kFewRows = 32;         // rows per key head up to which this kernel is taken
 
-template <typename T, int DH, int HW>
+template <typename T, int DH, int HW, int NT>
 __global__ __launch_bounds__(kFewWaves * 64) void mass_few_kernel(MassArgs<T> a, const float* mass_in, float* mass) {
-  constexpr int NP = kParts<T>, GPR = DH / kGroup, KW = DH / 32, GROUPS = kFewWaves / HW;
-  __shared__ float part[kFewWaves][64];
+  constexpr int NP = kParts<T>, GPR = DH / kGroup, KW = DH / 32, GROUPS = kFewWaves / HW, KEYS = NT * 64;
+  __shared__ float part[kFewWaves][KEYS];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  const int b = blockIdx.y, key0 = (blockIdx.x * GROUPS + wave / HW) * 64;
+  const int b = blockIdx.y, key0 = (blockIdx.x * GROUPS + wave / HW) * KEYS;
   const int live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};                       // key 16 i + col, rows 4 grp .. + 3 of every sixteen
+  float acc[NT][4];                                          // key 64 t + 16 i + col, rows 4 grp .. + 3 of every sixteen
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[t][i] = 0.f;
   if (key0 < len) {
     for (int j = wave % HW; j < a.c.hk; j += HW) {
       const int64_t base = ((int64_t)b * a.c.hk + j) * a.c.cap;
       const auto kc = head_buffer(a.c.codes[0] + base * (DH / 2), len * (DH / 2)), ks = head_buffer(a.c.scales[0] + base * GPR, len * GPR);
       const uint32_t o = (key0 + col) * (DH / 2) + grp * (DH / 8), os = (key0 + col) * GPR + grp * GPR / 4;
-      uint32_t kw[4][KW];
-      float kb[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (DH == 128) {
-          const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(kc, o + i * 16 * (DH / 2), 0, 0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) kw[i][e] = w[e];
-        } else {
-          const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(kc, o + i * 16 * (DH / 2), 0, 0);
-          kw[i][0] = w[0];
-          kw[i][1] = w[1];
-        }
-        kb[i] = fourbit_scale(__builtin_amdgcn_raw_buffer_load_b8(ks, os + i * 16 * GPR, 0, 0));
-      }
       for (int row0 = 0; row0 < live; row0 += 16) {
+        uint32_t kw[2][4][KW], kb[2][4];
+        auto request = [&](int t) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (DH == 128) {
+              const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(kc, o + (t * 64 + i * 16) * (DH / 2), 0, 0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) kw[t & 1][i][e] = w[e];
+            } else {
+              const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(kc, o + (t * 64 + i * 16) * (DH / 2), 0, 0);
+              kw[t & 1][i][0] = w[0];
+              kw[t & 1][i][1] = w[1];
+            }
+            kb[t & 1][i] = __builtin_amdgcn_raw_buffer_load_b8(ks, os + (t * 64 + i * 16) * GPR, 0, 0);
+          }
+        };
         int g;
         const int s = div_by(min(row0 + col, live - 1), a.G, a.G_inv, g);
         const T* qp = a.q + b * a.q_sb + s * a.q_sr + (j * a.G + g) * a.q_sh + grp * (DH / 4);
@@ -230,43 +235,53 @@ __global__ __launch_bounds__(kFewWaves * 64) void mass_few_kernel(MassArgs<T> a,
           const int sr = div_by(min(row, live - 1), a.G, a.G_inv, g);
           nl[r] = row < live ? -kAttnLog2e * a.lse[((int64_t)b * a.n + sr) * a.heads + j * a.G + g] : -INFINITY;
         }
+        request(0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NT; ++t) {
+          if (t + 1 < NT) request(t + 1);
 #pragma unroll
-          for (int e = 0; e < KW; ++e) {
-            const bf16x8 kf = fourbit_eight(kw[i][e], kb[i]);
+          for (int i = 0; i < 4; ++i) {
+            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int p = NP - 1; p >= 0; --p) sc = mfma16(qf[e][p], kf, sc);
+            for (int e = 0; e < KW; ++e) {
+              const bf16x8 kf = fourbit_eight(kw[t & 1][i][e], fourbit_scale(kb[t & 1][i]));
+#pragma unroll
+              for (int p = NP - 1; p >= 0; --p) sc = mfma16(qf[e][p], kf, sc);
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale_log2, nl[r]));
+            acc[t][i] += sum;
           }
-          float sum = 0.f;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(sc[r], a.scale_log2, nl[r]));
-          acc[i] += sum;
+          __builtin_amdgcn_sched_barrier(0);                   // one tile's operands at a time
         }
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    acc[i] += __shfl_xor(acc[i], 16, NOVA_WAVE);
-    acc[i] += __shfl_xor(acc[i], 32, NOVA_WAVE);
-  }
-  part[wave][lane] = grp == 0 ? acc[0] : grp == 1 ? acc[1] : grp == 2 ? acc[2] : acc[3];
-  __syncthreads();
-  if (tid >= GROUPS * 64) return;
-  const int k = blockIdx.x * GROUPS * 64 + tid;
-  if (k >= a.c.cap) return;
-  const int64_t at = (int64_t)b * a.c.cap + k;
-  if (k >= len) {
-    mass[at] = -1.0f;
-    return;
-  }
-  const float m0 = mass_in ? mass_in[at] : 0.f;
-  float sum = 0.f;
+  for (int t = 0; t < NT; ++t) {
 #pragma unroll
-  for (int w = 0; w < HW; ++w) sum += part[wave * HW + w][lane];
-  mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+    for (int i = 0; i < 4; ++i) {
+      acc[t][i] += __shfl_xor(acc[t][i], 16, NOVA_WAVE);
+      acc[t][i] += __shfl_xor(acc[t][i], 32, NOVA_WAVE);
+    }
+    part[wave][t * 64 + lane] = grp == 0 ? acc[t][0] : grp == 1 ? acc[t][1] : grp == 2 ? acc[t][2] : acc[t][3];
+  }
+  __syncthreads();
+  for (int x = tid; x < GROUPS * KEYS; x += kFewWaves * 64) {
+    const int k = blockIdx.x * GROUPS * KEYS + x;
+    if (k >= a.c.cap) return;
+    const int64_t at = (int64_t)b * a.c.cap + k;
+    if (k >= len) {
+      mass[at] = -1.0f;
+      continue;
+    }
+    const float m0 = mass_in ? mass_in[at] : 0.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < HW; ++w) sum += part[x / KEYS * HW + w][x % KEYS];
+    mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+  }
 }
 
 struct Plan {
@@ -304,10 +319,17 @@ hipError_t collect(hipStream_t st, const nova_fourbit_cache& c, int heads, int n
   a.chunks = p.chunks; a.nsplit = p.nsplit; a.pitch = p.pitch;
   a.part = static_cast<float*>(workspace);
   if (p.few) {
-    const dim3 grid((c.capacity + kFewWaves / p.few * 64 - 1) / (kFewWaves / p.few * 64), c.B);
-#define GO(DH, HW) mass_few_kernel<T, DH, HW><<<grid, kFewWaves * 64, 0, st>>>(a, mass_in, mass)
-#define GO_DH(DH) if (p.few == 8) GO(DH, 8); else if (p.few == 4) GO(DH, 4); else if (p.few == 2) GO(DH, 2); else GO(DH, 1)
-    if (c.dh == 64) { GO_DH(64); } else { GO_DH(128); }
+    // Two tiles per wave once that leaves two workgroups per CU: the rows are read once for them, and the next keys on the way
+    // meanwhile (us with one / two / four: 4 images, 32 heads of 128 on 8, 32768 rows 21.9 / 17.8 / 18.4; 16 images, 16 heads
+    // of 64, 4096 rows 12.5 / 10.9 / 11.0; 8 images, 600 rows 9.2 / 9.9 / 9.8).
+    const int tile_groups = kFewWaves / p.few * 64;
+    const bool two = (int64_t)c.B * c.capacity / tile_groups >= 4 * kCus;
+    const int keys = tile_groups * (two ? 2 : 1);
+    const dim3 grid((c.capacity + keys - 1) / keys, c.B);
+#define GO(DH, HW) if (two) mass_few_kernel<T, DH, HW, 2><<<grid, kFewWaves * 64, 0, st>>>(a, mass_in, mass); \
+                   else mass_few_kernel<T, DH, HW, 1><<<grid, kFewWaves * 64, 0, st>>>(a, mass_in, mass)
+#define GO_DH(DH) if (p.few == 8) { GO(DH, 8); } else if (p.few == 4) { GO(DH, 4); } else if (p.few == 2) { GO(DH, 2); } else { GO(DH, 1); }
+    if (c.dh == 64) { GO_DH(64) } else { GO_DH(128) }
 #undef GO_DH
 #undef GO
     return hipGetLastError();
