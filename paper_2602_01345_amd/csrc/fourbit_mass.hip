@@ -54,28 +54,66 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
   const int ntiles = (live + kTileRows - 1) / kTileRows, per = (ntiles + a.nsplit - 1) / a.nsplit;
   const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
 
-  // ---- rows of a tile: past the last one its copies, which weigh nothing (lse = inf)
+  // ---- rows of a tile: past the last one its copies, which weigh nothing (lse = inf).  A thread walks its rows in steps of a
+  // tile: row s G + g goes on by 32 / G queries and 32 % G heads, with one query more and G heads fewer where that passes G.
+  // (Dividing anew for every tile was 70 of the loop's 200 vector instructions.)
+  struct Walk {
+    int row, g;
+    const T* p;
+  };
+  int step_g;
+  const int64_t step_s = div_by(kTileRows, a.G, a.G_inv, step_g);
+  const int64_t step = step_s * a.q_sr + step_g * a.q_sh, wrap = a.q_sr - a.G * a.q_sh;
+  const T* q_head = a.q + b * a.q_sb + (int64_t)j * a.G * a.q_sh;
+  Walk walk[QL];
+  const T* last;
+  const float *lse_p, *lse_end;
+  int lse_g;
+  {
+    int g;
+    const int s = div_by(max(live - 1, 0), a.G, a.G_inv, g);
+    last = q_head + s * a.q_sr + g * a.q_sh;
+    const int sl = div_by(t0 * kTileRows + (tid & 31), a.G, a.G_inv, lse_g);
+    const float* l = a.lse + (int64_t)b * a.n * a.heads + j * a.G;
+    lse_p = l + (int64_t)sl * a.heads + lse_g;
+    lse_end = l + (int64_t)s * a.heads + g;                      // the last live row's, and nothing behind it is read
+  }
+#pragma unroll
+  for (int i = 0; i < QL; ++i) {
+    const int x = tid + i * kWaves * 64;
+    walk[i].row = t0 * kTileRows + x / CPR;
+    const int s = div_by(walk[i].row, a.G, a.G_inv, walk[i].g);
+    walk[i].p = q_head + s * a.q_sr + walk[i].g * a.q_sh;
+  }
   T qr[QL][8];
   float lse_r = 0.f;
-  auto request = [&](int t) {
+  auto request = [&]() {                                         // the next tile's
 #pragma unroll
     for (int i = 0; i < QL; ++i) {
-      const int x = tid + i * kWaves * 64;
-      int g;
-      const int s = div_by(min(t * kTileRows + x / CPR, live - 1), a.G, a.G_inv, g);
-      const T* p = a.q + b * a.q_sb + s * a.q_sr + (j * a.G + g) * a.q_sh + x % CPR * 8;
+      Walk& w = walk[i];
+      const T* p = (w.row < live ? w.p : last) + (tid + i * kWaves * 64) % CPR * 8;
       if constexpr (NP == 1) {
         *reinterpret_cast<u32x4*>(qr[i]) = *reinterpret_cast<const u32x4*>(p);
       } else {
         *reinterpret_cast<f32x4*>(qr[i]) = *reinterpret_cast<const f32x4*>(p);
         *reinterpret_cast<f32x4*>(qr[i] + 4) = *reinterpret_cast<const f32x4*>(p + 4);
       }
+      w.row += kTileRows;
+      w.g += step_g;
+      w.p += step;
+      if (w.g >= a.G) {
+        w.g -= a.G;
+        w.p += wrap;
+      }
     }
     if (tid < kTileRows) {
-      const int row = t * kTileRows + tid;
-      int g;
-      const int s = div_by(min(row, live - 1), a.G, a.G_inv, g);
-      lse_r = row < live ? -kAttnLog2e * a.lse[((int64_t)b * a.n + s) * a.heads + j * a.G + g] : -INFINITY;
+      lse_r = lse_p <= lse_end ? -kAttnLog2e * *lse_p : -INFINITY;
+      lse_g += step_g;
+      lse_p += step_s * a.heads + step_g;
+      if (lse_g >= a.G) {
+        lse_g -= a.G;
+        lse_p += a.heads - a.G;
+      }
     }
   };
   auto place = [&](int stage) {
@@ -95,7 +133,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  if (t0 < t1) request(t0);
+  if (t0 < t1) request();
 
   // ---- this lane's keys: channels half dh / 2 + 8 t of key col of block kb
   bf16x8 kf[2][KS];
@@ -119,7 +157,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
   float acc[2] = {0.f, 0.f};
   if (t0 < t1) {
     place(0);
-    if (t0 + 1 < t1) request(t0 + 1);
+    if (t0 + 1 < t1) request();
     barrier();
   }
   for (int t = t0; t < t1; ++t) {
@@ -130,6 +168,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -138,9 +177,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) s[kb] = mfma32(qf, kf[kb][ks], s[kb]);
       }
+    __builtin_amdgcn_s_setprio(0);
     if (t + 1 < t1) {
       place(stage ^ 1);
-      if (t + 2 < t1) request(t + 2);
+      if (t + 2 < t1) request();
     }
     // register r is row 8 (r / 4) + 4 half + r % 4 of the tile
     float sum[2] = {0.f, 0.f};
