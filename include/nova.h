@@ -383,8 +383,8 @@ typedef struct nova_fourbit_cache {
   int32_t dh;
 } nova_fourbit_cache;
 
-/* Rows [B, n, heads, dh] in a buffer of the caller's, with strides in elements (any sign is refused but >= 0; the stride of
- * an extent of 1 is not looked at). */
+/* Rows [B, n, heads, dh] in a buffer of the caller's, with strides in elements: 0 <= stride <= 2^40, the stride of an extent of
+ * 1 is not looked at. */
 typedef struct nova_rows {
   void* data;
   int64_t stride_b;
@@ -468,7 +468,8 @@ int nova_fourbit_evict(nova_ctx* ctx, void* stream, const nova_fourbit_cache* sr
 /*
  * nova_pruned_block_rows with the block's cache in 4 bits: the kept rows' keys and values are quantised and appended to `cache`,
  * and attention reads prior and kept rows from there.  Everything else, variants and per-image counts included, as there, with
- *   shape    kv_capacity is cache->capacity (no multiple needed); heads of 64 or 128 channels in either dtype
+ *   shape    kv_capacity is cache->capacity (no multiple needed); heads of 64 or 128 channels in either dtype; NOVA_F32:
+ *            k + dh <= 16384, whatever kv_len
  *   cache    B, kv_heads = heads, dh of the shape
  *   mass     fp32 [B, capacity] or NULL: the weight that the rows have collected after this block, from mass_in [B, capacity]
  *            (NULL: none before; may be the mass array itself) and the kept queries of this call, as nova_fourbit_mass

@@ -67,6 +67,8 @@ class ScalePlan:
     entropies: Optional[List[torch.Tensor]] = None     # per block [B, N] (a pruned scale); entropy is the last block's
     stores: Optional[List["FourBitStore"]] = None      # cache_bits=4: where each block's rows are during this scale
     evictions: Optional[List[tuple]] = None            # (store, store it moves to, rows it has) of what is evicted after it
+    evict_idx: Optional[List[torch.Tensor]] = None     # per eviction [B, evict_to] rows that stay, and their masks
+    evict_mask: Optional[List[torch.Tensor]] = None
 
 
 @dataclass
@@ -176,8 +178,6 @@ class ImageRunner:
         prev_grid = None
         need = 0
         stores, spare = (list(self.stores), self._spare) if self.cache_bits == 4 else (None, None)
-        self._evict_idx: List[torch.Tensor] = []
-        self._evict_mask: List[torch.Tensor] = []
         for t, g in enumerate(self.grids):
             N = g * g
             dense = t not in k_tables
@@ -213,8 +213,7 @@ class ImageRunner:
                     if kv[j] > self.evict_to:
                         plan.evictions.append((stores[j], spare, kv[j]))
                         stores[j], spare, kv[j] = spare, stores[j], self.evict_to
-                if len(plan.evictions) > len(self._evict_idx):
-                    self._evict_idx, self._evict_mask = self._eviction_buffers(len(plan.evictions))
+                plan.evict_idx, plan.evict_mask = self._eviction_buffers(len(plan.evictions))
             if keep:
                 prev_cache, prev_grid = plan.cache_new, g
             plans.append(plan)
@@ -245,8 +244,7 @@ class ImageRunner:
                                      plan.mask[j], plan.cache_prev[j], plan.out[j], plan.cache_new[j])
             x = plan.out[j]
         if plan.evictions:
-            m = len(plan.evictions)
-            self._evict(plan.evictions, self._evict_idx[:m], self._evict_mask[:m], per_image=False)
+            self._evict(plan.evictions, plan.evict_idx, plan.evict_mask, per_image=False)
         return x
 
     def capture(self, plan: ScalePlan):

@@ -250,6 +250,41 @@ def test_images_with_their_own_lengths(nova, dtype, dh, n, kv_len):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [None, [700, 699, 0, 64, 1, 333, 650, 128, 700]])
+def test_whole_items_and_runs_in_one_launch(nova, dtype, lens):
+    """More blocks of queries than there is room for at a time: a full round of whole ones, the rest cut into runs of keys."""
+    _check_attention(nova, dtype, 9, 32, 32, 64, 140, 700, 700, lens)
+
+
+def test_no_queries_leave_the_weights_as_they_were(nova):
+    cache, _ = _fill(2, 2, 30, 64, [30, 30], 1)
+    q = torch.empty((2, 0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    m = torch.rand((2, 30), device="cuda")
+    m[0, 3], m[1, 4] = -1.0, float("inf")
+    out = torch.empty_like(m)
+    nova.fourbit_mass(cache, q, torch.empty((2, 0, 4), device="cuda"), out, None, 20, mass_in=m, kv_len_per_row=_ints([20, 7]))
+    want = torch.where(m > 0, m, 0.0)
+    want[0, 20:], want[1, 7:] = -1.0, -1.0
+    assert torch.equal(out, want)
+    nova.fourbit_attention(cache, q, torch.empty_like(q), None, 20)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_weights_of_protected_rows_stay_infinite(nova, n):
+    cache, _ = _fill(1, 2, 90, 64, [90], 1)
+    q = torch.randn((1, n, 2, 64), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    ws = torch.empty(max(nova.fourbit_mass_workspace_bytes(cache, 2, n, 90), 16), dtype=torch.uint8, device="cuda")
+    out, lse = _run_attention(nova, cache, q, 90)
+    m = torch.zeros((1, 90), device="cuda")
+    m[0, 70:] = float("inf")
+    nova.fourbit_mass(cache, q, lse, m, ws, 90, mass_in=m)                        # in place
+    assert torch.isinf(m[0, 70:]).all() and torch.isfinite(m[0, :70]).all() and (m[0, :70] > 0).all()
+    plain = torch.empty((1, 90), device="cuda")
+    nova.fourbit_mass(cache, q, lse, plain, ws, 90)
+    assert torch.equal(plain[0, :70], m[0, :70])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [1, 20, 140])
 def test_queries_in_place(nova, dtype, n):
     """Queries as they lie in a joint projection's output, and with the heads in front of the rows."""
