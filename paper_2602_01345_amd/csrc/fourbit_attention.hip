@@ -48,8 +48,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
   const uint8_t* codes[2] = {a.c.codes[0] + bh * a.c.cap * (DH / 2), a.c.codes[1] + bh * a.c.cap * (DH / 2)};
   const uint8_t* scales[2] = {a.c.scales[0] + bh * a.c.cap * GPR, a.c.scales[1] + bh * a.c.cap * GPR};
 
-  // this thread's quarter (the wave's) of row lane of a tile, so that neighbouring lanes write one chunk of neighbouring rows: rows past the last take the last one's place (their scores are set to
-  // -inf below, their values are those of a row that counts)
+  // this thread's quarter (the wave's) of row lane of a tile, so that neighbouring lanes write one chunk of neighbouring rows; rows
+  // past the last take the last one's place (their scores are set to -inf below, their values are those of a row that counts)
   const int frow = lane, fq = wave;
   uint32_t cw[2][CW], cb[2];
   auto request = [&](int t) {
@@ -89,7 +89,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
   const int row = row0 + wave * 32 + col;
   bf16x8 qf[KS][NP];                                       // channels 16 t + 8 half .. + 7 of this lane's row
   {
-    const T* qp = a.query(b, j, min(row, rows - 1)) + half * 8;
+    // past the last live row its copies: what lies in padding (NaN, say) is nobody's
+    const T* qp = a.query(b, j, max(min(row, live - 1), 0)) + half * 8;
 #pragma unroll
     for (int t = 0; t < KS; ++t) load_eight(qp + t * 16, qf[t]);
   }
@@ -186,6 +187,13 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
           }
       }
       l_run += psum;
+      if constexpr (NP > 1) {
+        // in the scores' place: with three operands per row registers are short (fp32, 128 channels: 124 -> 111 us; bf16 2 % slower)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = e[kb][r];
+      }
       __builtin_amdgcn_s_setprio(1);
       // ---- O^T += V^T P^T, 16 keys per MFMA: the lane's keys 16 u + 4 half .. + 3 and 8 behind them
 #pragma unroll
@@ -194,7 +202,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           bf16_t p[NP];
-          split(e[u >> 1][(u & 1) * 8 + i], p);
+          split(NP > 1 ? s[u >> 1][(u & 1) * 8 + i] : e[u >> 1][(u & 1) * 8 + i], p);
 #pragma unroll
           for (int x = 0; x < NP; ++x) pf[x][i] = p[x];
         }
@@ -311,6 +319,13 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
   const int rows = n * (heads / c.kv_heads), ntiles = (kv_len + kTile - 1) / kTile;
   Plan p = {};
   p.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+  // More rows, but no more than two workgroups per CU in blocks of 32, and no wave with more than eight tiles: no tile waits for
+  // the others, and nothing is joined afterwards (us in blocks of 128 / of 32; 16 heads of 64, one image: 205 queries, 629 keys
+  // 9.1 + 3.9 / 7.9; 64, 155 6.4 / 5.9; two images, 30 heads, 128 queries, 2000 keys 13.3 + 6.5 / 13.9; of 128 channels: 256
+  // queries, 521 keys 13.0 + 4.0 / 12.2; but 100 queries, 3100 keys 14.3 + 4.5 / 25.1).
+  const int64_t blocks32 = (int64_t)c.B * c.kv_heads * ((rows + 31) / 32);
+  const bool spread = p.mt == 0 && blocks32 <= 2 * kCus && ntiles <= 32;
+  if (spread) p.mt = 2;
   p.waves = 4;
   p.block_rows = p.mt ? 16 * p.mt : kRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;
@@ -323,7 +338,7 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
     p.run_tiles = ntiles;
     if (want > 4 && p.mt == 1 && ntiles <= kFewWhole) {
       p.waves = 8;
-    } else if (want > 4) {
+    } else if (want > 4 && !spread) {
       p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
       p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
       if (p.nsplit > 1) p.n_whole = 0;

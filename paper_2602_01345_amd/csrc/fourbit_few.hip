@@ -79,11 +79,11 @@ __global__ __launch_bounds__(NW * 64, NW == 8 || MT == 2 || sizeof(T) * DH == 51
     load_k(first);
     load_v(first);
   }
-  // operand of step e: channels grp dh / 4 + 8 e .. + 7 of row col
+  // operand of step e: channels grp dh / 4 + 8 e .. + 7 of row col; past the last live row its copies (padding is nobody's)
   bf16x8 qf[MT][KW][NP];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const T* qp = a.query(b, j, min(row0 + mt * 16 + col, rows - 1)) + grp * (DH / 4);
+    const T* qp = a.query(b, j, max(min(row0 + mt * 16 + col, live - 1), 0)) + grp * (DH / 4);
 #pragma unroll
     for (int e = 0; e < KW; ++e) load_eight(qp + e * 8, qf[mt][e]);
   }

@@ -250,6 +250,23 @@ def test_images_with_their_own_lengths(nova, dtype, dh, n, kv_len):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n,L", [(33, 2049), (128, 2112), (129, 2111), (300, 2113), (257, 4100)])
+def test_blocks_of_128_rows_over_many_tiles(nova, dtype, dh, n, L):
+    """Too many tiles for blocks of 32 rows: ends of tiles and blocks of the kernel for many rows, in runs of keys."""
+    _check_attention(nova, dtype, 1, 2, 1, dh, n, L + 1, L)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n,L", [(70, 1), (65, 63), (33, 64), (96, 65), (70, 129), (130, 200)])
+def test_blocks_of_128_rows_of_many_heads(nova, dtype, dh, n, L):
+    """Too many key heads for blocks of 32 rows: the same kernel with a tile or a few, whole items only."""
+    _check_attention(nova, dtype, 9, 30, 30, dh, n, L, L)
+    _check_attention(nova, dtype, 9, 30, 30, dh, n, L, L, lens=[L - b * L // 9 for b in range(8)] + [0], counts=[n - 3 * b for b in range(9)])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("lens", [None, [700, 699, 0, 64, 1, 333, 650, 128, 700]])
 def test_whole_items_and_runs_in_one_launch(nova, dtype, lens):
     """More blocks of queries than there is room for at a time: a full round of whole ones, the rest cut into runs of keys."""
@@ -573,3 +590,25 @@ def test_two_streams_at_once(nova):
                 nova.fourbit_attention(c, q, out, ws, L)
     torch.cuda.synchronize()
     assert all(torch.equal(a[3], w) for a, w in zip(args, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,L", [(8, 40), (40, 300), (300, 2300)])
+def test_padding_behind_the_live_queries_is_nobodys(nova, dtype, n, L):
+    """NaN and infinities in the padded slots of a batch: the live queries get the bits they get with zeros there, and the weights
+    collected are the same."""
+    B, H, hk, dh = 3, 4, 2, 64
+    cache, _ = _fill(B, hk, L, dh, [L] * B, 6)
+    counts = _ints([n, n // 2, 1])
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(7)).to(DTYPES[dtype]).cuda()
+    got = []
+    for pad in (0.0, float("nan"), float("inf")):
+        for b, c in enumerate(counts.tolist()):
+            q[b, c:] = pad
+        out, lse = _run_attention(nova, cache, q, L, counts=counts)
+        mass = torch.empty((B, L), device="cuda")
+        ws = torch.empty(max(nova.fourbit_mass_workspace_bytes(cache, H, n, L), 16), dtype=torch.uint8, device="cuda")
+        nova.fourbit_mass(cache, q, lse, mass, ws, L, n_per_row=counts)
+        got.append((out, lse, mass))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
