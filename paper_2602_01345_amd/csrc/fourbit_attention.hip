@@ -9,7 +9,9 @@
 // all of its threads on the way from registers into LDS, once for the 128 rows; the codes of the tile after next are
 // on the way meanwhile.  Two stages of LDS, two workgroups per CU, so that one wave's softmax runs next to another's MFMAs; a
 // wave asks for priority while it issues MFMAs, or two waves of a SIMD fall into step and take turns at everything (385 us
-// without, 340 with: 2458 queries of 2 images, 16 heads of 128, 8883 keys).
+// without, 340 with: 2458 queries of 2 images, 16 heads of 128, 8883 keys).  Bound by MFMA and power there (1.1 PFLOP/s, a
+// library product of 8192^3 1.17); with heads of 64 by the softmax's vector instructions (1024 queries of 4 images, 32 heads,
+// 4096 keys 165 us, 0.83 PFLOP/s).
 #include <algorithm>
 
 #include "fourbit_attention.h"

@@ -5,6 +5,10 @@
 // everything is a multiple of 16 bytes) a thread takes eight channels, four neighbours a group: loads and stores of whole
 // lines on both sides.  Otherwise (values key-minor, say) a thread takes a group of one row and neighbouring lanes neighbouring
 // rows, so that the caller's side is read or written along the rows.
+//
+// Measured: 6425 rows of 2 images, 16 heads of 128 in bf16 in 34.6 us (133 MB, 3.8 TB/s; the values key-minor with an odd pitch) and
+// out again in 21.4 (6.2 TB/s); a row of 8 images in 3; 8192 of 32768 rows of 4 images, 8 heads of 128, moved in 25 us (71 MB: lines of
+// 128 bytes are fetched for rows of 64).
 #include <algorithm>
 
 #include "fourbit.h"

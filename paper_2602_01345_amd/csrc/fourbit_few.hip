@@ -10,6 +10,8 @@
 //   O^T += V^T P^T the order of the keys is free as well: the scores a lane holds after two S^T tiles, keys 4 grp .. + 3 of
 //                  either, are its operand as they are.  Values are converted as they come (a lane: 32 channels of a key),
 //                  laid into the wave's own LDS by rows and read back transposed.
+// Measured: one query of 32 heads of 128 on 8 key heads, 4 images of 32768 rows (143 MB) 29.5 us, of which 6.6 are start, first
+// latency and the joining of waves and the rest runs at 6.1 TB/s; of 16 heads of 64, 8 images of 424 rows 5.6 us, a tile per wave.
 #include "fourbit_attention.h"
 
 namespace {
