@@ -245,12 +245,14 @@ def _rows(t: torch.Tensor, heads: int, dh: int, name: str) -> "_Rows":
     return _Rows(t.data_ptr(), *t.stride())
 
 
-def _shaped(name: str, t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype: torch.dtype) -> Optional[int]:
-    """Pointer of an optional dense tensor that has to have this shape and type."""
+def _shaped(name: str, t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype: torch.dtype,
+            device: Optional[int] = None) -> Optional[int]:
+    """Pointer of an optional dense tensor that has to have this shape and type, and lie on this device where one is given."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} {t.stride()}, expected dense {tuple(shape)} {dtype}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or (device is not None and t.get_device() != device):
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} {t.stride()} on {t.device}, expected dense {tuple(shape)} {dtype}"
+                         + ("" if device is None else f" on device {device}"))
     return t.data_ptr()
 
 
@@ -529,10 +531,7 @@ class Nova:
         return c
 
     def _counts(self, B: int, name: str, t: Optional[torch.Tensor]) -> Optional[int]:
-        if t is None:
-            return None
-        self._here(t)
-        return _shaped(name, t, (B,), torch.int32)
+        return None if t is None else _shaped(name, t, (B,), torch.int32, self.device)
 
     def fourbit_append(self, cache: FourBitCache, k: torch.Tensor, v: torch.Tensor, kv_len: int,
                        n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None,
@@ -581,12 +580,14 @@ class Nova:
         B, n, heads, dh = shape
         if B != c.B:
             raise ValueError(f"{B} images of queries, {c.B} in the cache")
-        self._here(q, out, lse, workspace)
+        dev = self.device
+        self._here(q, workspace)
         rc = self.lib.nova_fourbit_attention(
-            self.ctx, _stream(self.device), _dtype_code(q), c, heads, n, _rows(q, heads, c.dh, "q"),
+            self.ctx, _stream(dev), _dtype_code(q), c, heads, n, _rows(q, heads, c.dh, "q"),
             self._counts(B, "n_per_row", n_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
-            dh ** -0.5 if scale is None else scale, _shaped("out", out, shape, q.dtype),
-            _shaped("lse", lse, (B, n, heads), torch.float32), _ptr(workspace), 0 if workspace is None else workspace.nbytes)
+            dh ** -0.5 if scale is None else scale, _shaped("out", out, shape, q.dtype, dev),
+            _shaped("lse", lse, (B, n, heads), torch.float32, dev), _ptr(workspace),
+            0 if workspace is None else workspace.nbytes)
         if rc:
             self._check(rc, "nova_fourbit_attention")
 
@@ -603,12 +604,13 @@ class Nova:
         B, n, heads, dh = q.shape
         if B != c.B:
             raise ValueError(f"{B} images of queries, {c.B} in the cache")
-        self._here(q, lse, mass, mass_in, workspace)
+        dev, per_row = self.device, (B, c.capacity)
+        self._here(q, workspace)
         rc = self.lib.nova_fourbit_mass(
-            self.ctx, _stream(self.device), _dtype_code(q), c, heads, n, _rows(q, heads, c.dh, "q"),
+            self.ctx, _stream(dev), _dtype_code(q), c, heads, n, _rows(q, heads, c.dh, "q"),
             self._counts(B, "n_per_row", n_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
-            dh ** -0.5 if scale is None else scale, _shaped("lse", lse, (B, n, heads), torch.float32),
-            _shaped("mass_in", mass_in, (B, c.capacity), torch.float32), _shaped("mass", mass, (B, c.capacity), torch.float32),
+            dh ** -0.5 if scale is None else scale, _shaped("lse", lse, (B, n, heads), torch.float32, dev),
+            _shaped("mass_in", mass_in, per_row, torch.float32, dev), _shaped("mass", mass, per_row, torch.float32, dev),
             _ptr(workspace), 0 if workspace is None else workspace.nbytes)
         if rc:
             self._check(rc, "nova_fourbit_mass")
@@ -619,13 +621,12 @@ class Nova:
                       mass_dst: Optional[torch.Tensor] = None):
         """Rows kept_idx [B, k] of src to the front of dst, with their masses."""
         s, d = self._cache(src), self._cache(dst)
-        B, k = s.B, kept_idx.shape[1]
-        self._here(kept_idx, mass_src, mass_dst)
+        B, k, dev = s.B, kept_idx.shape[1], self.device
         rc = self.lib.nova_fourbit_evict(
-            self.ctx, _stream(self.device), s, d, k, _shaped("kept_idx", kept_idx, (B, k), torch.int32),
+            self.ctx, _stream(dev), s, d, k, _shaped("kept_idx", kept_idx, (B, k), torch.int32, dev),
             self._counts(B, "k_per_row", k_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
-            self._counts(B, "kv_len_next", kv_len_next), _shaped("mass_src", mass_src, (B, s.capacity), torch.float32),
-            _shaped("mass_dst", mass_dst, (B, d.capacity), torch.float32))
+            self._counts(B, "kv_len_next", kv_len_next), _shaped("mass_src", mass_src, (B, s.capacity), torch.float32, dev),
+            _shaped("mass_dst", mass_dst, (B, d.capacity), torch.float32, dev))
         if rc:
             self._check(rc, "nova_fourbit_evict")
 
@@ -642,15 +643,15 @@ class Nova:
         what the rows had before) where the weight they collect is wanted."""
         c = self._cache(cache)
         B = shape.B
-        self._here(x, kept_idx, y_kept, workspace, mass, mass_in)
+        self._here(x, kept_idx, y_kept, workspace)
         s = shape.c_struct()
         w = _Weights(*[_ptr(weights.get(n)) for n, _ in _Weights._fields_])
         rc = self.lib.nova_pruned_block_fourbit(
             self.ctx, _stream(self.device), C.byref(s), C.byref(w), None if variant is None else C.byref(variant.c_struct()),
             self._counts(B, "k_per_row", k_per_row), self._counts(B, "kv_len_per_row", kv_len_per_row),
             self._counts(B, "kv_len_next", kv_len_next), _ptr(x), _ptr(kept_idx), c,
-            _shaped("mass_in", mass_in, (B, c.capacity), torch.float32), _shaped("mass", mass, (B, c.capacity), torch.float32),
-            _ptr(y_kept), _ptr(workspace), workspace.nbytes)
+            _shaped("mass_in", mass_in, (B, c.capacity), torch.float32, self.device),
+            _shaped("mass", mass, (B, c.capacity), torch.float32, self.device), _ptr(y_kept), _ptr(workspace), workspace.nbytes)
         if rc:
             self._check(rc, "nova_pruned_block_fourbit")
 
