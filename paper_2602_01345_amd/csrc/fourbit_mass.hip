@@ -3,11 +3,11 @@
 //
 // S = Q K^T, 32 rows x 32 keys per MFMA, a lane owning one key of either of two blocks: the sum over rows stays in the lane.  A
 // wave has 64 keys, converted once into the operands it holds in registers (the order of the channels in the product is free:
-// a lane takes half a row of the cache as it lies); the rows come in tiles of 32 through LDS, shared by the four waves.
+// a lane takes half a row of the cache as it lies); the rows come in tiles of 32 or 64 through LDS, shared by the four waves.
 // A launch leaves sums per key head (and run of rows, where there are few keys); a second one adds them up in a fixed order.
 //
-// Bound by vector instructions, an fma, an exp2 and an add per score: 1640 queries of 2 images, 16 heads of 128, 8065 keys 137 us,
-// 0.79 PFLOP/s.
+// Bound by vector instructions, an fma, an exp2 and an add per score: 1640 queries of 2 images, 16 heads of 128, 8065 keys 133 us,
+// 0.82 PFLOP/s.
 //
 // Few rows (single tokens, a handful of queries): reading the keys once bounds it, and launches.  The waves of a workgroup take
 // 64 keys of several key heads and add up among themselves, one launch and no workspace.  16 x 16 MFMAs, the keys from the cache
@@ -18,7 +18,8 @@
 
 namespace {
 
-constexpr int kWaves = 4, kKeys = kWaves * 64, kTileRows = 32;
+constexpr int kWaves = 4, kKeys = kWaves * 64, kSubRows = 32;
+constexpr int kTallRows = 512;       // rows per key head from which a bf16 tile has 64 of them (both measured at the launch)
 
 template <typename T>
 struct MassArgs {
@@ -35,9 +36,9 @@ struct MassArgs {
   int pitch;
 };
 
-template <typename T, int DH>
+template <typename T, int DH, int SUBS>
 __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
-  constexpr int NP = kParts<T>;
+  constexpr int NP = kParts<T>, kTileRows = SUBS * kSubRows;
   constexpr int GPR = DH / kGroup, ROWB = DH * 2, KS = DH / 16;
   constexpr int PLANE = kTileRows * ROWB, STAGE = NP * PLANE;
   constexpr int QL = kTileRows * DH / 8 / (kWaves * 64);       // runs of eight channels per thread and tile
@@ -76,7 +77,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
     int g;
     const int s = div_by(max(live - 1, 0), a.G, a.G_inv, g);
     last = q_head + s * a.q_sr + g * a.q_sh;
-    const int sl = div_by(t0 * kTileRows + (tid & 31), a.G, a.G_inv, lse_g);
+    const int sl = div_by(t0 * kTileRows + tid % kTileRows, a.G, a.G_inv, lse_g);
     const float* l = a.lse + (int64_t)b * a.n * a.heads + j * a.G;
     lse_p = l + (int64_t)sl * a.heads + lse_g;
     lse_end = l + (int64_t)s * a.heads + g;                      // the last live row's, and nothing behind it is read
@@ -166,34 +167,41 @@ __global__ __launch_bounds__(kWaves * 64, 2) void mass_kernel(MassArgs<T> a) {
   for (int t = t0; t < t1; ++t) {
     const int stage = (t - t0) & 1;
     const char* sq = lds + stage * STAGE;
-    f32x16 s[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-    __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int p = NP - 1; p >= 0; --p) {
-        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(sq + p * PLANE + qa[ks]);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) s[kb] = mfma32(qf, kf[kb][ks], s[kb]);
+    auto next = [&] {
+      if (t + 1 < t1) {
+        place(stage ^ 1);
+        if (t + 2 < t1) request();
       }
-    __builtin_amdgcn_s_setprio(0);
-    if (t + 1 < t1) {
-      place(stage ^ 1);
-      if (t + 2 < t1) request();
-    }
-    // register r is row 8 (r / 4) + 4 half + r % 4 of the tile
+    };
     float sum[2] = {0.f, 0.f};
+    if constexpr (SUBS > 1) next();
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const f32x4 nl = *reinterpret_cast<const f32x4*>(&neg_lse[stage][8 * r4 + 4 * half]);
+    for (int sub = 0; sub < SUBS; ++sub) {
+      f32x16 s[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) sum[kb] += __builtin_amdgcn_exp2f(fmaf(s[kb][r4 * 4 + e], a.scale_log2, nl[e]));
+        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) {
+          const bf16x8 qf = *reinterpret_cast<const bf16x8*>(sq + p * PLANE + sub * kSubRows * ROWB + qa[ks]);
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) s[kb] = mfma32(qf, kf[kb][ks], s[kb]);
+        }
+      __builtin_amdgcn_s_setprio(0);
+      if constexpr (SUBS == 1) next();
+      // register r is row 8 (r / 4) + 4 half + r % 4 of the 32
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 nl = *reinterpret_cast<const f32x4*>(&neg_lse[stage][sub * kSubRows + 8 * r4 + 4 * half]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) sum[kb] += __builtin_amdgcn_exp2f(fmaf(s[kb][r4 * 4 + e], a.scale_log2, nl[e]));
+      }
     }
     acc[0] += sum[0];
     acc[1] += sum[1];
@@ -353,7 +361,7 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
   p.chunks = (kv_len + kKeys - 1) / kKeys;
   p.pitch = (kv_len + 63) / 64 * 64;
   const int64_t items = std::max((int64_t)c.B * c.kv_heads * p.chunks, (int64_t)1);
-  const int tiles = (int)(((int64_t)n * (heads / c.kv_heads) + kTileRows - 1) / kTileRows);
+  const int tiles = (int)(((int64_t)n * (heads / c.kv_heads) + kSubRows - 1) / kSubRows);
   p.nsplit = (int)std::max((int64_t)1, std::min((int64_t)tiles, 2 * kCus / items));
   return p;
 }
@@ -393,8 +401,18 @@ hipError_t collect(hipStream_t st, const nova_fourbit_cache& c, int heads, int n
   if (P > 0) {
     parts = c.kv_heads * p.nsplit;
     const unsigned grid = (unsigned)((int64_t)c.B * c.kv_heads * p.chunks * p.nsplit);
-    if (c.dh == 64) mass_kernel<T, 64><<<grid, kWaves * 64, 0, st>>>(a);
-    else mass_kernel<T, 128><<<grid, kWaves * 64, 0, st>>>(a);
+    // Tiles of 64 rows halve the barriers and give the softmax of one half the products of the other to run beside (us with 32 /
+    // 64, bf16: 2 images of 1640 queries, 16 heads of 128 140.9 / 136.8; 8 of 512, 36 heads of 64 50.4 / 46.9).  Few rows would
+    // be padding (40 of them 20.5 / 22.7), and in fp32 the LDS then holds one workgroup per CU (500 rows 53 / 70).
+    constexpr int kTall = sizeof(T) == 2 ? 2 : 1;
+    const bool tall = (int64_t)n * a.G >= kTallRows;
+    if (c.dh == 64) {
+      if (tall) mass_kernel<T, 64, kTall><<<grid, kWaves * 64, 0, st>>>(a);
+      else mass_kernel<T, 64, 1><<<grid, kWaves * 64, 0, st>>>(a);
+    } else {
+      if (tall) mass_kernel<T, 128, kTall><<<grid, kWaves * 64, 0, st>>>(a);
+      else mass_kernel<T, 128, 1><<<grid, kWaves * 64, 0, st>>>(a);
+    }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   add_kernel<<<dim3((c.capacity + kAddKeys - 1) / kAddKeys, c.B), kAddKeys * kAddGroups, 0, st>>>(a.part, p.pitch, parts, c.capacity, P, kv_rows, mass_in, mass);

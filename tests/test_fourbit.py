@@ -273,6 +273,16 @@ def test_whole_items_and_runs_in_one_launch(nova, dtype, lens):
     _check_attention(nova, dtype, 9, 32, 32, 64, 140, 700, 700, lens)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n,H,hk,L", [(511, 1, 1, 130), (512, 2, 2, 257), (513, 1, 1, 64), (545, 2, 2, 1), (86, 12, 2, 300), (1100, 2, 1, 255)])
+def test_weights_from_hundreds_of_rows(nova, dtype, dh, n, H, hk, L):
+    """Around the size from which a tile has 64 rows: ends inside either half of one, heads that change inside it, runs that get
+    none, images with fewer rows than that."""
+    _check_attention(nova, dtype, 1, H, hk, dh, n, L + 2, L)
+    _check_attention(nova, dtype, 4, H, hk, dh, n, L + 2, L, lens=[L, L // 2, 0, L], counts=[n, n - 33, n, 3])
+
+
 def test_no_queries_leave_the_weights_as_they_were(nova):
     cache, _ = _fill(2, 2, 30, 64, [30, 30], 1)
     q = torch.empty((2, 0, 4, 64), dtype=torch.bfloat16, device="cuda")
