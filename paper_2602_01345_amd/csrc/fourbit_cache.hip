@@ -216,7 +216,9 @@ hipError_t launch_fourbit_append(hipStream_t st, int dtype, const nova_fourbit_c
   if (n == 0 && !kv_next) return hipSuccess;
   const RowsView in = rows_view(dtype, k, v);
   const FourBitView to = fourbit_view(c);
-#define GO(T, DH)                                                                                                          append_kernel<T, DH><<<dim3((std::max(n, 1) + kBlockRows<DH> - 1) / kBlockRows<DH>, 2 * c.kv_heads, c.B), kThreads, 0, st>>>(       in, to, n, P, n_rows, kv_rows, kv_next)
+#define GO(T, DH)                                                                                                                  \
+  append_kernel<T, DH><<<dim3((std::max(n, 1) + kBlockRows<DH> - 1) / kBlockRows<DH>, 2 * c.kv_heads, c.B), kThreads, 0, st>>>(    \
+      in, to, n, P, n_rows, kv_rows, kv_next)
   if (dtype == NOVA_BF16) { if (c.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
   else { if (c.dh == 64) GO(float, 64); else GO(float, 128); }
 #undef GO
@@ -227,7 +229,9 @@ hipError_t launch_fourbit_unpack(hipStream_t st, int dtype, const nova_fourbit_c
                                  const int32_t* first_rows, const int32_t* n_rows, const nova_rows* k, const nova_rows* v) {
   const RowsView out = rows_view(dtype, k, v);
   const FourBitView from = fourbit_view(c);
-#define GO(T, DH)                                                                                               unpack_kernel<T, DH><<<dim3((n + kBlockRows<DH> - 1) / kBlockRows<DH>, 2 * c.kv_heads, c.B), kThreads, 0, st>>>(       out, from, n, first, first_rows, n_rows)
+#define GO(T, DH)                                                                                                                  \
+  unpack_kernel<T, DH><<<dim3((n + kBlockRows<DH> - 1) / kBlockRows<DH>, 2 * c.kv_heads, c.B), kThreads, 0, st>>>(                 \
+      out, from, n, first, first_rows, n_rows)
   if (dtype == NOVA_BF16) { if (c.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
   else { if (c.dh == 64) GO(float, 64); else GO(float, 128); }
 #undef GO
@@ -239,7 +243,9 @@ hipError_t launch_fourbit_evict(hipStream_t st, const nova_fourbit_cache& src, c
                                 const float* mass_src, float* mass_dst) {
   const int slots = mass_src ? dst.capacity : k;               // k <= capacity
   if (slots == 0 && !kv_next) return hipSuccess;
-#define GO(DH)                                                                                                                evict_kernel<DH><<<dim3((std::max(slots, 1) + kBlockRows<DH> - 1) / kBlockRows<DH>, 2 * src.kv_heads, src.B), kThreads, 0, st>>>(       fourbit_view(src), fourbit_view(dst), k, slots, P, idx, k_rows, kv_rows, kv_next, mass_src, mass_dst)
+#define GO(DH)                                                                                                                     \
+  evict_kernel<DH><<<dim3((std::max(slots, 1) + kBlockRows<DH> - 1) / kBlockRows<DH>, 2 * src.kv_heads, src.B), kThreads, 0, st>>>(\
+      fourbit_view(src), fourbit_view(dst), k, slots, P, idx, k_rows, kv_rows, kv_next, mass_src, mass_dst)
   if (src.dh == 64) GO(64); else GO(128);
 #undef GO
   return hipGetLastError();

@@ -415,7 +415,8 @@ hipError_t collect(hipStream_t st, const nova_fourbit_cache& c, int heads, int n
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  add_kernel<<<dim3((c.capacity + kAddKeys - 1) / kAddKeys, c.B), kAddKeys * kAddGroups, 0, st>>>(a.part, p.pitch, parts, c.capacity, P, kv_rows, mass_in, mass);
+  add_kernel<<<dim3((c.capacity + kAddKeys - 1) / kAddKeys, c.B), kAddKeys * kAddGroups, 0, st>>>(
+      a.part, p.pitch, parts, c.capacity, P, kv_rows, mass_in, mass);
   return hipGetLastError();
 }
 
