@@ -86,6 +86,7 @@ struct AttentionArgs {
   uint32_t blocks_inv, hk_inv, G_inv, nsplit_inv;
   int n_whole, nsplit;
   int run_tiles;         // tiles per run; 0: an item's tiles divided by nsplit
+  int ranked;            // > 0: items come by falling length of their images, this many (64 at most)
   float* part_o;
   float* part_ml;
 
@@ -100,6 +101,16 @@ struct AttentionArgs {
       bh = div_by(item, blocks, blocks_inv, block);
     }
     b = div_by(bh, c.hk, hk_inv, j);
+  }
+  // The image of rank b by length (of two alike the earlier one first), for all lanes of a wave at once.
+  __device__ __forceinline__ int by_length(int b) const {
+    const int lane = threadIdx.x & 63, mine = lane < ranked ? image_prior(kv_rows, lane, P) : 0;
+    int rank = lane < ranked ? 0 : lane;
+    for (int i = 0; i < ranked; ++i) {
+      const int other = __builtin_amdgcn_readlane(mine, i);
+      if (lane < ranked) rank += other > mine || (other == mine && i < lane);
+    }
+    return __shfl(__builtin_amdgcn_ds_permute(rank * 4, lane), b, NOVA_WAVE);
   }
   __device__ __forceinline__ const T* query(int b, int j, int row) const {
     int g;

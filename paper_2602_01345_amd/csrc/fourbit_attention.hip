@@ -40,6 +40,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
   const int nparts = whole ? 1 : a.nsplit;
   int b, j, block;
   a.place(whole ? blockIdx.x : a.n_whole + run / a.nsplit, b, j, block);
+  if (a.ranked) b = __builtin_amdgcn_readfirstlane(a.by_length(b));
   const int64_t bh = (int64_t)b * a.c.hk + j;
   const int row0 = block * kRows;
   const int rows = a.n * a.G, live = image_count(a.n_rows, b, a.n) * a.G, len = image_prior(a.kv_rows, b, a.P);
@@ -264,6 +265,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block
   const int ci = (int)(r / used_rows), rr = (int)(r - (int64_t)ci * used_rows);
   int b, j, block;
   a.place(min(a.n_whole + ci, a.items - 1), b, j, block);
+  if (a.ranked) b = a.by_length(b);
   const int row = block * block_rows + rr;
   const int len = image_prior(a.kv_rows, b, a.P);
   const bool there = a.n_whole + ci < a.items && row < a.n * a.G;
@@ -312,12 +314,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttentionArgs<T> a, int block
 // How a call is divided: mt > 0: blocks of 16 mt rows (fourbit_few.hip), else blocks of kRows; items below n_whole are one
 // workgroup each, the others nsplit.
 struct Plan {
-  int mt, waves, block_rows, blocks, items, n_whole, nsplit, run_tiles;
+  int mt, waves, block_rows, blocks, items, n_whole, nsplit, run_tiles, ranked;
   int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
 };
 constexpr int kCus = 256;
 constexpr int kFewWhole = 24;
-Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
+constexpr int kRanked = 32;          // most images that are ranked: every workgroup does it for itself, a step per image
+Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len, bool ragged) {
   const int rows = n * (heads / c.kv_heads), ntiles = (kv_len + kTile - 1) / kTile;
   Plan p = {};
   p.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
@@ -348,7 +351,12 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
     return p;
   }
   const int slots = 2 * kCus, rest = p.items % slots;
-  if (rest == 0) return p;
+  // Images with lengths of their own: the longest first, so that short ones fill up the end; from two rounds of items on that is
+  // enough and none is cut (us without / with, lengths falling, rising, mixed, equal: 8 images of 512 queries, 36 heads of 64, up
+  // to 1728 keys 71, 69, 69, 82 / 65, 64, 62, 84; 24 of 300, 16 heads, 1200 keys 45, 45, 49, 57 / 42, 42, 41, 58; 6 of 1000, 16 heads
+  // of 128, 3000 keys, cut as ever, 121, 122, 123, 150 / 123, 117, 116, 152).
+  p.ranked = ragged && p.items > slots && c.B > 1 && c.B <= kRanked ? c.B : 0;
+  if (rest == 0 || (p.ranked && p.items >= 2 * slots)) return p;
   const int s = std::min(slots / rest, ntiles / 4);
   if (s >= 2) {
     p.n_whole = p.items - rest;
@@ -362,7 +370,7 @@ size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 template <typename T>
 hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n, const nova_rows& q, const int32_t* n_rows, int P,
                   const int32_t* kv_rows, float scale_log2, void* out, float* lse, void* workspace) {
-  const Plan p = plan(c, heads, n, P);
+  const Plan p = plan(c, heads, n, P, kv_rows != nullptr);
   AttentionArgs<T> a = {};
   a.q = static_cast<const T*>(q.data);
   a.q_sb = q.stride_b; a.q_sr = q.stride_row; a.q_sh = q.stride_head;
@@ -375,7 +383,7 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
   a.lse = lse;
   a.blocks = p.blocks; a.items = p.items; a.dealt = p.items / (8 * p.blocks) * 8 * p.blocks;
   a.blocks_inv = div_inv(p.blocks); a.hk_inv = div_inv(c.kv_heads); a.G_inv = div_inv(a.G); a.nsplit_inv = div_inv(p.nsplit);
-  a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles;
+  a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles; a.ranked = p.ranked;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
   const unsigned grid = (unsigned)(p.n_whole + p.runs());
@@ -400,7 +408,7 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
 }  // namespace
 
 size_t fourbit_attention_workspace_bytes(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
-  const Plan p = plan(c, heads, n, kv_len);
+  const Plan p = plan(c, heads, n, kv_len, false);           // of the two the one that asks for more
   if (p.nsplit == 1) return 0;
   const size_t rows = (size_t)p.runs() * p.block_rows;
   return up256(rows * c.dh * 4) + up256(rows * 8);

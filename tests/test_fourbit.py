@@ -275,6 +275,18 @@ def test_whole_items_and_runs_in_one_launch(nova, dtype, lens):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("B,hk,n", [(2, 150, 130), (2, 520, 40), (31, 18, 40), (32, 33, 40), (33, 33, 40)])
+def test_many_items_of_images_in_any_order(nova, dtype, dh, B, hk, n):
+    """More blocks of queries than there is room for, of few and of many images: those come by length, or as they are; lengths of
+    zero, past the bound and alike, images with fewer queries."""
+    L = 140
+    lens = [(b * 97 + 40) % (L + 20) if b % 5 else (0, L, 64, L + 9)[b // 5 % 4] for b in range(B)]
+    counts = [n if b % 3 else n - 2 * b for b in range(B)]
+    _check_attention(nova, dtype, B, hk, hk, dh, n, L + 1, L, lens=lens[::-1], counts=counts)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("n,H,hk,L", [(511, 1, 1, 130), (512, 2, 2, 257), (513, 1, 1, 64), (545, 2, 2, 1), (86, 12, 2, 300), (1100, 2, 1, 255)])
 def test_weights_from_hundreds_of_rows(nova, dtype, dh, n, H, hk, L):
     """Around the size from which a tile has 64 rows: ends inside either half of one, heads that change inside it, runs that get
