@@ -357,7 +357,11 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len, bool ragged
   // of 128, 3000 keys, cut as ever, 121, 122, 123, 150 / 123, 117, 116, 152).
   p.ranked = ragged && p.items > slots && c.B > 1 && c.B <= kRanked ? c.B : 0;
   if (rest == 0 || (p.ranked && p.items >= 2 * slots)) return p;
-  const int s = std::min(slots / rest, ntiles / 4);
+  // A few more items than CUs, and long ones: most CUs would have one, which is little to hide anything behind, and the others two
+  // (us whole / in three: 264 items, 8000 keys 135 / 110 of 64 channels, 204 / 176 of 128; 320 136 / 117, 214 / 195; images of
+  // different lengths 115 / 94, 181 / 149; but 400 140 / 143, 235 / 246, and 320 of 3000 keys 57 / 55, 87 / 93).
+  const bool in_three = p.items > kCus && p.items <= kCus + kCus / 4 && ntiles >= 64;
+  const int s = in_three ? 3 : std::min(slots / rest, ntiles / 4);
   if (s >= 2) {
     p.n_whole = p.items - rest;
     p.nsplit = s;

@@ -51,6 +51,19 @@ def _fill(B, hk, cap, dh, lens, seed, scale=1.0, dead=255):
     return FourBitCache(*[torch.from_numpy(t).cuda() for h in halves for t in h]), halves
 
 
+def _fill_codes(B, hk, cap, dh, lens, seed, scale=1.0, dead=255):
+    """The same of any codes, for large caches: quantising on the host takes its time."""
+    g = np.random.default_rng(seed)
+    halves = []
+    for _ in range(2):
+        codes = g.integers(0, 256, (B, hk, cap, dh // 2), dtype=np.uint8)
+        scales = g.integers(124, 127, (B, hk, cap, dh // 32), dtype=np.uint8)
+        for b, n in enumerate(lens):
+            codes[b, :, n:], scales[b, :, n:] = dead, dead
+        halves.append((codes, scales))
+    return FourBitCache(*[torch.from_numpy(t).cuda() for h in halves for t in h]), halves
+
+
 def _values(half, lens):
     v = F.values(*half)
     for b, n in enumerate(lens):
@@ -79,11 +92,11 @@ def _run_attention(nova, cache, q, kv_len, lens=None, counts=None, scale=None):
     return out, lse
 
 
-def _check_attention(nova, dtype, B, H, hk, dh, n, cap, kv_len, lens=None, counts=None, scale=None, seed=1, kscale=1.0, q=None):
+def _check_attention(nova, dtype, B, H, hk, dh, n, cap, kv_len, lens=None, counts=None, scale=None, seed=1, kscale=1.0, q=None, fill=_fill):
     print(f"fourbit attention {dtype} B={B} H={H}/{hk} dh={dh} n={n} kv_len={kv_len} lens={lens} counts={counts}", flush=True)
     real = [kv_len] * B if lens is None else [min(max(x, 0), kv_len) for x in lens]
     live = [n] * B if counts is None else [min(max(x, 0), n) for x in counts]
-    cache, halves = _fill(B, hk, cap, dh, real, seed, kscale)
+    cache, halves = fill(B, hk, cap, dh, real, seed, kscale)
     if q is None:
         q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(seed)).to(DTYPES[dtype]).cuda()
     out, lse = _run_attention(nova, cache, q, kv_len, None if lens is None else _ints(lens), None if counts is None else _ints(counts),
@@ -282,7 +295,14 @@ def test_many_items_of_images_in_any_order(nova, dtype, dh, B, hk, n):
     L = 140
     lens = [(b * 97 + 40) % (L + 20) if b % 5 else (0, L, 64, L + 9)[b // 5 % 4] for b in range(B)]
     counts = [n if b % 3 else n - 2 * b for b in range(B)]
-    _check_attention(nova, dtype, B, hk, hk, dh, n, L + 1, L, lens=lens[::-1], counts=counts)
+    _check_attention(nova, dtype, B, hk, hk, dh, n, L + 1, L, lens=lens[::-1], counts=counts, fill=_fill_codes)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_a_few_more_blocks_than_fit_at_once(nova, dtype, dh):
+    """Cut into three runs, of which some have no keys."""
+    _check_attention(nova, dtype, 4, 65, 65, dh, 33, 4033, 4033, lens=[4033, 65, 0, 129], fill=_fill_codes)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
