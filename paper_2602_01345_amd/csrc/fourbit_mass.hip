@@ -362,7 +362,11 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
   p.pitch = (kv_len + 63) / 64 * 64;
   const int64_t items = std::max((int64_t)c.B * c.kv_heads * p.chunks, (int64_t)1);
   const int tiles = (int)(((int64_t)n * (heads / c.kv_heads) + kSubRows - 1) / kSubRows);
-  p.nsplit = (int)std::max((int64_t)1, std::min((int64_t)tiles, 2 * kCus / items));
+  // Two workgroups per CU at least; eight, so that they end together, where a run still has 512 rows: its start, the conversion of
+  // its keys, is then little (us with two / eight: 280 items of 30360 rows 765 / 368; 423 of 1887 77 / 72; 1024 of 1640 the same; but
+  // 1024 of 512 in runs of 256 46 / 49, 192 of 600 in runs of 128 19 / 21).
+  const int64_t two = std::min((int64_t)tiles, 2 * kCus / items), eight = std::min((int64_t)tiles / 16, (8 * kCus + items - 1) / items);
+  p.nsplit = (int)std::max({(int64_t)1, two, eight});
   return p;
 }
 
