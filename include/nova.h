@@ -422,7 +422,8 @@ int nova_fourbit_unpack(nova_ctx* ctx, void* stream, int dtype, const nova_fourb
  *   out        out [B, n, heads, dh] dense, 16-byte aligned; must not alias q
  *   lse        out fp32 [B, n, heads] or NULL: ln of the sum of e^(scale * score)
  *   workspace  of at least nova_fourbit_attention_workspace_bytes, 16-byte aligned (may be NULL where that is 0); calls that
- *              overlap, captured graphs among them, need one each
+ *              overlap, captured graphs among them, need one each.  0 bytes for sizes that the call refuses
+ * B * heads * n <= 2^30.
  * Queries past n_per_row[b], and all queries of an image without rows, get zeros and lse = -inf.  NOVA_F32: queries and
  * probabilities take part with all their 24 bits; NOVA_BF16: probabilities are rounded to bf16 in front of the second product.
  */

@@ -67,11 +67,15 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 // A cache in 4 bits.  At most 2^24 rows: a head's codes are 1 GiB, offsets within a head have 32 bits (between heads 64).
-int fourbit_error(const nova_fourbit_cache* c) {
+int fourbit_sizes_error(const nova_fourbit_cache* c) {
   if (!c) return NOVA_ERR_INVALID_ARG;
   if (c->B < 0 || c->kv_heads < 1 || c->capacity < 0) return NOVA_ERR_INVALID_ARG;
   if (c->dh != 64 && c->dh != 128) return NOVA_ERR_UNSUPPORTED;
   if (c->B > 65535 || c->kv_heads > 32767 || c->capacity > 1 << 24) return NOVA_ERR_UNSUPPORTED;
+  return NOVA_OK;
+}
+int fourbit_error(const nova_fourbit_cache* c) {
+  if (int rc = fourbit_sizes_error(c)) return rc;
   if (c->B == 0 || c->capacity == 0) return NOVA_OK;
   for (const void* p : {c->k_codes, c->k_scales, c->v_codes, c->v_scales})
     if (!p || !aligned16(p)) return NOVA_ERR_INVALID_ARG;
@@ -106,12 +110,24 @@ nova_rows settled(const nova_rows& r, int B, int n, int heads) {
   return s;
 }
 
-// What nova_fourbit_attention and nova_fourbit_mass have in common; 1: nothing to do.
+// n queries per image of `heads` heads over kv_len rows of a cache: at most 2^30 queries of one head in all, looked at factor by
+// factor, since the product of three ints may pass 64 bits.
+int query_sizes_error(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
+  if (heads < 1 || n < 0 || kv_len < 0 || kv_len > c.capacity || heads % c.kv_heads != 0) return NOVA_ERR_INVALID_ARG;
+  constexpr int kMost = 1 << 30;
+  if (c.B > 0 && (heads > kMost / c.B || n > kMost / (c.B * heads))) return NOVA_ERR_UNSUPPORTED;
+  return NOVA_OK;
+}
+// Such a call has work to do, so that it may need a workspace.
+bool query_has_work(const nova_fourbit_cache* c, int heads, int n, int kv_len) {
+  return fourbit_sizes_error(c) == NOVA_OK && c->B > 0 && n > 0 && query_sizes_error(*c, heads, n, kv_len) == NOVA_OK;
+}
+
+// What nova_fourbit_attention and nova_fourbit_mass check alike.
 int fourbit_query_error(int dtype, const nova_fourbit_cache* cache, int heads, int n, const nova_rows* q, int kv_len) {
   if (!valid_dtype(dtype)) return NOVA_ERR_UNSUPPORTED;
   if (int rc = fourbit_error(cache)) return rc;
-  if (heads < 1 || n < 0 || kv_len < 0 || kv_len > cache->capacity || heads % cache->kv_heads != 0) return NOVA_ERR_INVALID_ARG;
-  if ((int64_t)cache->B * heads * std::max(n, 1) > (int64_t)1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (int rc = query_sizes_error(*cache, heads, n, kv_len)) return rc;
   if (cache->B == 0 || n == 0) return NOVA_OK;
   if (!q) return NOVA_ERR_INVALID_ARG;
   return rows_error(q, dtype, cache->B, n, heads, true);
@@ -617,10 +633,7 @@ int nova_fourbit_unpack(nova_ctx* ctx, void* stream, int dtype, const nova_fourb
 }
 
 size_t nova_fourbit_attention_workspace_bytes(const nova_fourbit_cache* cache, int heads, int n, int kv_len) {
-  if (!cache || heads < 1 || n < 1 || kv_len < 0 || cache->B < 1 || cache->kv_heads < 1 || heads % cache->kv_heads != 0 ||
-      (cache->dh != 64 && cache->dh != 128) || (int64_t)cache->B * heads * n > (int64_t)1 << 30)
-    return 0;
-  return fourbit_attention_workspace_bytes(*cache, heads, n, kv_len);
+  return query_has_work(cache, heads, n, kv_len) ? fourbit_attention_workspace_bytes(*cache, heads, n, kv_len) : 0;
 }
 
 int nova_fourbit_attention(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int heads, int n,
@@ -641,10 +654,7 @@ int nova_fourbit_attention(nova_ctx* ctx, void* stream, int dtype, const nova_fo
 }
 
 size_t nova_fourbit_mass_workspace_bytes(const nova_fourbit_cache* cache, int heads, int n, int kv_len) {
-  if (!cache || heads < 1 || n < 1 || kv_len < 0 || cache->B < 1 || cache->kv_heads < 1 || heads % cache->kv_heads != 0 ||
-      (cache->dh != 64 && cache->dh != 128) || (int64_t)cache->B * heads * n > (int64_t)1 << 30)
-    return 0;
-  return fourbit_mass_workspace_bytes(*cache, heads, n, kv_len);
+  return query_has_work(cache, heads, n, kv_len) ? fourbit_mass_workspace_bytes(*cache, heads, n, kv_len) : 0;
 }
 
 int nova_fourbit_mass(nova_ctx* ctx, void* stream, int dtype, const nova_fourbit_cache* cache, int heads, int n,

@@ -142,6 +142,30 @@ def test_workspace_of_shapes_that_are_none(lib):
         assert size(C.byref(_cache()), 4, 0, 10) == 0 and size(C.byref(_cache(dh=80)), 4, 1, 10) == 0
 
 
+# (B, heads, n): products past 2^30, past 2^31, and 2^64 exactly, which is 0 in 64 bits
+_TOO_MANY = [(2, 4, 1 << 28), (1, 2, 1 << 30), (2, 1 << 30, 1), (3, 2147483646, 1), (16, 1 << 30, 1 << 30), (4, 1 << 30, 1 << 30),
+             (16, 1 << 29, 1 << 30), (65535, 2147483646, 2147483647)]
+
+
+@pytest.mark.parametrize("call", [_attend, _mass])
+@pytest.mark.parametrize("B,heads,n", _TOO_MANY)
+def test_sizes_whose_product_wraps(lib, call, B, heads, n):
+    for kv_heads in (1, 2):
+        assert call(lib, cache=_cache(B=B, kv_heads=kv_heads), heads=heads, n=n, q=_rows(heads=4)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("size", ["nova_fourbit_attention_workspace_bytes", "nova_fourbit_mass_workspace_bytes"])
+def test_no_workspace_for_sizes_that_the_calls_refuse(lib, size):
+    f = getattr(lib, size)
+    for B, heads, n in _TOO_MANY:
+        for kv_heads in (1, 2):
+            assert f(C.byref(_cache(B=B, kv_heads=kv_heads)), heads, n, 10) == 0
+    for cache, kv_len in ((_cache(), 101), (_cache(), 2147483647), (_cache(), -1), (_cache(B=65536), 10), (_cache(B=-1), 10),
+                          (_cache(kv_heads=32768), 10), (_cache(kv_heads=0), 10), (_cache(capacity=(1 << 24) + 1), 10)):
+        for n in (1, 700):
+            assert f(C.byref(cache), 2 * max(cache.kv_heads, 1), n, kv_len) == 0
+
+
 def _evict(lib, src=None, dst=None, k=4, idx=BASE, k_rows=None, kv_len=50, kv_rows=None, kv_next=None, ms=None, md=None):
     return lib.nova_fourbit_evict(_CTX, None, _ref(src or _cache()), _ref(dst or _cache(2, capacity=20)), k, idx, k_rows, kv_len,
                                   kv_rows, kv_next, ms, md)
