@@ -436,6 +436,8 @@ int nova_fourbit_attention(nova_ctx* ctx, void* stream, int dtype, const nova_fo
  * Attention weight that the cached rows collect, summed over queries and heads:
  *   mass[b, j] = m0 + sum_{s, h} exp(scale * <q[b, s, h], K[b, g, j]> - lse[b, s, h])     for j < kv_len_per_row[b]
  *   mass[b, j] = -1                                                                      for the other j < capacity
+ * A sum that is NaN (one query or cached key of NaN makes all of its image's so) adds nothing: mass[b, j] = m0, and nova_select,
+ * which ranks NaN behind -1, goes on preferring the rows that an image has.
  *   mass_in    fp32 [B, capacity] or NULL: m0 = mass_in[b, j] if that is > 0, else 0 (so a row that was marked -1 when it did
  *              not exist yet starts from 0); may be the mass array itself
  *   mass       out fp32 [B, capacity], the scores nova_select ranks for nova_fourbit_evict.  A row that a caller sets to

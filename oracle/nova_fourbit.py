@@ -78,7 +78,7 @@ def attention(q: np.ndarray, K: np.ndarray, V: np.ndarray, scale: float, lens: S
 
 def mass(q: np.ndarray, K: np.ndarray, scale: float, lse: np.ndarray, mass_in: Optional[np.ndarray], lens: Sequence[int],
          counts: Sequence[int]) -> Tuple[np.ndarray, np.ndarray]:
-    """Masses [B, capacity] and what was collected by this call alone."""
+    """Masses [B, capacity] and what was collected by this call alone.  A sum that is NaN adds nothing to a row's mass."""
     B, n, H, dh = q.shape
     G = H // K.shape[1]
     cap = K.shape[2]
@@ -91,7 +91,7 @@ def mass(q: np.ndarray, K: np.ndarray, scale: float, lse: np.ndarray, mass_in: O
                 s = scale * (q[b, :c, h] @ K[b, h // G, :L].T)
                 got[b, :L] += np.exp(s - lse[b, :c, h][:, None]).sum(0)
         m0 = np.zeros(L) if mass_in is None else mass_in[b, :L]
-        out[b, :L] = np.where(m0 > 0, m0, 0.0) + got[b, :L]
+        out[b, :L] = np.where(m0 > 0, m0, 0.0) + np.where(np.isnan(got[b, :L]), 0.0, got[b, :L])
     return out, got
 
 

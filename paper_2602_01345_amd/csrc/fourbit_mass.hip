@@ -21,6 +21,12 @@ namespace {
 constexpr int kWaves = 4, kKeys = kWaves * 64, kSubRows = 32;
 constexpr int kTallRows = 512;       // rows per key head from which a bf16 tile has 64 of them (both measured at the launch)
 
+// What a row has collected after a call.  A sum that is no number (one query or key of NaN is enough) adds nothing: a NaN would be
+// ranked behind the rows that do not exist (-1), which would then be kept in place of the image's own.
+__device__ __forceinline__ float collected(float before, float sum) {
+  return (before > 0.f ? before : 0.f) + (sum == sum ? sum : 0.f);
+}
+
 template <typename T>
 struct MassArgs {
   const T* q;
@@ -242,7 +248,7 @@ __global__ __launch_bounds__(kAddKeys* kAddGroups) void add_kernel(const float* 
   const float m0 = mass_in ? mass_in[at] : 0.f;
 #pragma unroll
   for (int i = 1; i < kAddGroups; ++i) sum += sums[i][x];
-  mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+  mass[at] = collected(m0, sum);
 }
 
 // HW waves of a workgroup share NT tiles of 64 keys, each with every HW-th key head; kFewWaves / HW such groups.
@@ -343,7 +349,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void mass_few_kernel(MassArgs<T> a,
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < HW; ++w) sum += part[x / KEYS * HW + w][x % KEYS];
-    mass[at] = (m0 > 0.f ? m0 : 0.f) + sum;
+    mass[at] = collected(m0, sum);
   }
 }
 

@@ -654,3 +654,47 @@ def test_padding_behind_the_live_queries_is_nobodys(nova, dtype, n, L):
         got.append((out, lse, mass))
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("spoil", ["query", "key"])
+@pytest.mark.parametrize("n", [1, 12, 40, 600])
+def test_weights_that_are_no_numbers_leave_an_image_its_rows(nova, dtype, spoil, n):
+    """A query or a key of NaN makes every weight of its image NaN: its rows keep what they had collected, in front of the rows
+    that it does not have, and eviction finds them.  The other image gets the bits it gets without."""
+    B, H, hk, dh, cap, keep = 2, 4, 2, 64, 90, 60
+    lens = [50, 90]
+    cache, halves = _fill(B, hk, cap, dh, lens, 17)
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(18)).to(DTYPES[dtype]).cuda()
+    m_in = torch.rand((B, cap), generator=torch.Generator().manual_seed(19)).cuda()
+    m_in[:, ::5] = -1.0
+    m_in[:, 7], m_in[:, 11] = float("inf"), float("nan")
+
+    def weights():
+        out, lse = _run_attention(nova, cache, q, cap, _ints(lens))
+        mass = torch.full((B, cap), float("nan"), device="cuda")
+        ws = torch.full((max(nova.fourbit_mass_workspace_bytes(cache, H, n, cap), 16),), 255, dtype=torch.uint8, device="cuda")
+        nova.fourbit_mass(cache, q, lse, mass, ws, cap, mass_in=m_in, kv_len_per_row=_ints(lens))
+        return mass
+
+    clean = weights()
+    if spoil == "query":
+        q[0, n // 2, 3, 5] = float("nan")
+    else:
+        cache.k_scales[0, :, 20, 1] = 255
+        halves[0][1][0, :, 20, 1] = 255
+    mass = weights()
+    before = torch.where(m_in > 0, m_in, 0.0)
+    assert torch.equal(mass[0, :50], before[0, :50])          # a row's sum is over all key heads: NaN in one is NaN in all
+    assert (mass[0, 50:] == -1).all() and torch.equal(mass[1], clean[1])
+    idx = torch.empty((B, keep), dtype=torch.int32, device="cuda")
+    mask = torch.empty((B, cap), dtype=torch.uint8, device="cuda")
+    nova.select(mass, keep, idx, mask)
+    dst = FourBitCache.empty(B, hk, keep, dh)
+    m_dst = torch.empty((B, keep), device="cuda")
+    after = torch.empty(B, dtype=torch.int32, device="cuda")
+    nova.fourbit_evict(cache, dst, idx, cap, kv_len_per_row=_ints(lens), kv_len_next=after, mass_src=mass, mass_dst=m_dst)
+    assert after.tolist() == [50, 60] and idx[0, :50].tolist() == list(range(50))
+    assert torch.equal(m_dst[0, :50], mass[0, :50]) and (m_dst[0, 50:] == -1).all()
+    for half, got in ((halves[0], (dst.k_codes, dst.k_scales)), (halves[1], (dst.v_codes, dst.v_scales))):
+        assert all(np.array_equal(g[0, :, :50].cpu().numpy(), w[0, :, :50]) for g, w in zip(got, half))

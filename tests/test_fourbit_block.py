@@ -221,3 +221,29 @@ def test_counts_of_the_controller_with_eviction(hx):
         if t >= 3:
             assert all(len(set(k.tolist())) == 2 for k in res.k)
     assert all(0 < n <= r.cap for rows in r.kv_rows for n in rows.tolist())
+
+
+def test_an_image_of_nan_keeps_its_rows_and_leaves_the_other_alone(hx):
+    """One image's tokens are NaN at a scale: eviction still takes rows that the image has, never one made of zeros, and the other
+    image gets the bits that it gets without."""
+    got = []
+    for spoil in (False, True):
+        r, xs, logits, tables = _runner(hx, "bf16", 12)
+        for st in r.stores + [r._spare]:
+            for nme in ("k_codes", "k_scales", "v_codes", "v_scales"):
+                getattr(st.cache, nme).fill_(0)               # scale byte 0: not the 127 of a row made of zeros
+        ratio = torch.tensor([0.9, 0.2], device="cuda")
+        outs = []
+        for t in range(len(GRIDS)):
+            x = xs[t].clone()
+            if spoil and t == 3:
+                x[0] = float("nan")
+            outs.append(r.run_scale(t, x, logits=logits[t], ratio_t=ratio if t >= 3 else None, keep_cache=t >= 2).out[1])
+            if t == 3:
+                for st in r.stores:
+                    for b, rows in enumerate(st.rows.tolist()):
+                        made = (st.cache.k_codes[b, 0, :rows] == 0).all(-1) & (st.cache.k_scales[b, 0, :rows] == 127).all(-1)
+                        assert rows == 12 and not made.any()
+                        assert (st.mass[b, :rows] >= 0).all() and (st.mass[b, rows:] == -1).all()
+        got.append(outs)
+    assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -61,3 +61,15 @@ def test_attention_mass_is_one_per_query_and_head():
     assert (out[1] == 0).all() and np.isneginf(lse[1]).all()
     m, got = F.mass(q, K, 0.125, lse, None, [9, 0], [3, 3])
     assert np.isclose(got[0].sum(), 3 * 4) and (m[1] == -1).all()
+
+
+def test_sums_that_are_no_numbers_add_nothing():
+    rng = np.random.default_rng(6)
+    K = F.values(*F.quantise(rng.standard_normal((2, 1, 5, 64))))
+    q = rng.standard_normal((2, 3, 2, 64))
+    _, lse, _, _ = F.attention(q, K, K, 0.125, [4, 5], [3, 3])
+    q[0, 1, 0, 2] = lse[0, 1, 0] = np.nan
+    m_in = np.array([[0.5, -1.0, np.inf, np.nan, 3.0], [0.0] * 5])
+    m, got = F.mass(q, K, 0.125, lse, m_in, [4, 5], [3, 3])
+    assert np.isnan(got[0, :4]).all() and m[0].tolist() == [0.5, 0.0, np.inf, 0.0, -1.0]
+    assert np.isclose(m[1].sum(), 3 * 2)
