@@ -13,6 +13,7 @@
 // library product of 8192^3 1.17); with heads of 64 by the softmax's vector instructions (1024 queries of 4 images, 32 heads,
 // 4096 keys 165 us, 0.83 PFLOP/s).
 #include <algorithm>
+#include <cfloat>
 
 #include "fourbit_attention.h"
 
@@ -381,8 +382,9 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
   a.c = fourbit_view(c);
   a.heads = heads; a.G = heads / c.kv_heads; a.n = n; a.P = P;
   a.n_rows = n_rows; a.kv_rows = kv_rows;
-  // a score of -inf stays one when it is multiplied (the rows past the last): scores times 1e-30 weigh alike to the last bit, too
-  a.scale_log2 = scale_log2 == 0.f ? 1e-30f : scale_log2;
+  // Rows past the last have scores of -inf, which a scale of 0 would make NaN.  The smallest positive fp32 number (2^-149) in its
+  // place leaves less than 2^-21 of any finite score: no two weights differ by more than that.
+  a.scale_log2 = scale_log2 == 0.f ? FLT_TRUE_MIN : scale_log2;
   a.out = static_cast<T*>(out);
   a.lse = lse;
   a.blocks = p.blocks; a.items = p.items; a.dealt = p.items / (8 * p.blocks) * 8 * p.blocks;

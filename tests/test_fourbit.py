@@ -698,3 +698,12 @@ def test_weights_that_are_no_numbers_leave_an_image_its_rows(nova, dtype, spoil,
     assert torch.equal(m_dst[0, :50], mass[0, :50]) and (m_dst[0, 50:] == -1).all()
     for half, got in ((halves[0], (dst.k_codes, dst.k_scales)), (halves[1], (dst.v_codes, dst.v_scales))):
         assert all(np.array_equal(g[0, :, :50].cpu().numpy(), w[0, :, :50]) for g, w in zip(got, half))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n", [1, 20, 140])
+def test_a_scale_of_zero_and_scores_without_bound(nova, dtype, dh, n):
+    """Every row weighs the same, however large the finite scores are (around 2^115 here)."""
+    q = 2.0 ** 112 * torch.randn((1, n, 2, dh), generator=torch.Generator().manual_seed(23))
+    _check_attention(nova, dtype, 1, 2, 2, dh, n, 301, 300, scale=0.0, q=q.to(DTYPES[dtype]).cuda())
