@@ -13,15 +13,17 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 }
 
 // An operand of the caller's type as bf16 numbers whose sum it is.  Cached values are bf16 as they are, so a bf16 operand
-// takes one MFMA and an fp32 one three: 3 x 8 bits of significand are all 24 of it.
+// takes one MFMA and an fp32 one three: 3 x 8 bits of significand are all 24 of it.  Each part is the leading bits of what is
+// left, cut off and not rounded: the largest fp32 numbers round to an infinity.
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
 
+__device__ __forceinline__ bf16_t leading(float x) { return __builtin_bit_cast(bf16_t, (uint16_t)(__float_as_uint(x) >> 16)); }
 __device__ __forceinline__ void split(float x, bf16_t (&p)[1]) { p[0] = (bf16_t)x; }
 __device__ __forceinline__ void split(float x, bf16_t (&p)[3]) {
-  p[0] = (bf16_t)x;
+  p[0] = leading(x);
   const float r = x - (float)p[0];
-  p[1] = (bf16_t)r;
-  p[2] = (bf16_t)(r - (float)p[1]);
+  p[1] = leading(r);
+  p[2] = leading(r - (float)p[1]);
 }
 template <typename T>
 __device__ __forceinline__ void load_eight(const T* src, bf16x8 (&f)[kParts<T>]) {

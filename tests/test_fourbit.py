@@ -707,3 +707,28 @@ def test_a_scale_of_zero_and_scores_without_bound(nova, dtype, dh, n):
     """Every row weighs the same, however large the finite scores are (around 2^115 here)."""
     q = 2.0 ** 112 * torch.randn((1, n, 2, dh), generator=torch.Generator().manual_seed(23))
     _check_attention(nova, dtype, 1, 2, 2, dh, n, 301, 300, scale=0.0, q=q.to(DTYPES[dtype]).cuda())
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n", [1, 20, 140])
+def test_queries_at_the_end_of_fp32(nova, dh, n):
+    """fp32 queries between the largest bf16 number and the largest fp32 one, scores of order one."""
+    L = 130
+    q = torch.zeros((1, n, 2, dh), device="cuda")
+    q[..., 3], q[..., dh - 1] = torch.finfo(torch.float32).max, -3.397e38
+    cache = FourBitCache.empty(1, 2, L, dh)
+    g = torch.Generator().manual_seed(29)
+    k, v = (torch.randn((1, L, 2, dh), generator=g).cuda() for _ in range(2))
+    k = k.clamp(-1, 1) * 0.25
+    nova.fourbit_append(cache, k, v, 0)
+    scale = 2.0 ** -126
+    out, lse = _run_attention(nova, cache, q, L, scale=scale)
+    K, V = (F.values(a.cpu().numpy(), s.cpu().numpy()) for a, s in ((cache.k_codes, cache.k_scales), (cache.v_codes, cache.v_scales)))
+    ref = F.attention(_np(q), K, V, scale, [L], [n])
+    t_out, t_lse, d = _bounds(ref, "f32", dh, L)
+    assert (np.abs(_np(out) - ref[0]) <= t_out).all() and (np.abs(_np(lse) - ref[1]) <= t_lse).all()
+    mass = torch.empty((1, L), device="cuda")
+    ws = torch.empty(max(nova.fourbit_mass_workspace_bytes(cache, 2, n, L), 16), dtype=torch.uint8, device="cuda")
+    nova.fourbit_mass(cache, q, lse, mass, ws, L, scale=scale)
+    want, got = F.mass(_np(q), K, scale, _np(lse), None, [L], [n])
+    assert (np.abs(_np(mass) - want) <= got * (2 * d.max() + (2 * n + 128) * U) + 2 * U * want).all()
