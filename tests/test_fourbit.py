@@ -732,3 +732,44 @@ def test_queries_at_the_end_of_fp32(nova, dh, n):
     nova.fourbit_mass(cache, q, lse, mass, ws, L, scale=scale)
     want, got = F.mass(_np(q), K, scale, _np(lse), None, [L], [n])
     assert (np.abs(_np(mass) - want) <= got * (2 * d.max() + (2 * n + 128) * U) + 2 * U * want).all()
+
+
+def _check_weights(nova, dtype, B, H, hk, dh, n, L, lens=None, counts=None, seed=31):
+    """The weights alone, of any logarithms, at a closer bound: a sum is a chain of 32 numbers of a tile, one addition per tile of a
+    run (33 here) and one of the lane's halves, of an eighth of the parts (66), of eight groups and of what was there: fewer than
+    256 roundings of numbers that are none of them negative."""
+    print(f"fourbit weights {dtype} B={B} H={H}/{hk} dh={dh} n={n} L={L} lens={lens} counts={counts}", flush=True)
+    real, live = lens or [L] * B, counts or [n] * B
+    cache, halves = _fill_codes(B, hk, L + 1, dh, real, seed)
+    g = torch.Generator().manual_seed(seed)
+    q = (0.05 * torch.randn((B, n, H, dh), generator=g)).to(DTYPES[dtype]).cuda()
+    lse = (np.log(L) + torch.randn((B, n, H), generator=g)).cuda()
+    m_in = torch.rand((B, L + 1), generator=g).cuda()
+    ws = torch.full((max(nova.fourbit_mass_workspace_bytes(cache, H, n, L), 16),), 255, dtype=torch.uint8, device="cuda")
+    mass = torch.full((B, L + 1), float("nan"), device="cuda")
+    nova.fourbit_mass(cache, q, lse, mass, ws, L, mass_in=m_in, n_per_row=None if counts is None else _ints(counts),
+                      kv_len_per_row=None if lens is None else _ints(lens))
+    q64, K, sc = _np(q), _values(halves[0], real), dh ** -0.5
+    want, got = F.mass(q64, K, sc, _np(lse), _np(m_in), real, live)
+    reach = max(sc * (np.abs(q64[b, :live[b], h]) @ np.abs(K[b, h // (H // hk), :real[b]]).T).max(initial=0)
+                for b in range(B) for h in range(H))
+    d = (2 * dh + 32) * U * (reach + float(lse.abs().max()) + 1)
+    diff = np.abs(_np(mass) - want)
+    assert (diff <= got * (2 * d + 256 * U) + 2 * U * np.abs(want)).all(), (diff / np.maximum(got, 1e-30)).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("B,H,hk,n,L", [(3, 90, 90, 521, 3), (2, 390, 130, 187, 5), (1, 2080, 260, 70, 257), (2, 300, 150, 531, 40)])
+def test_weights_of_runs_with_many_tiles(nova, dtype, dh, B, H, hk, n, L):
+    """More chunks of keys than CUs: all tiles of rows in one run, or in two with a shorter second; one, two, three and eight heads
+    to a key head, so that the walk over rows wraps inside tiles and between them; images with fewer rows and keys."""
+    _check_weights(nova, dtype, B, H, hk, dh, n, L)
+    if B > 1:
+        _check_weights(nova, dtype, B, H, hk, dh, n, L, lens=[L, L // 2, 1][:B], counts=[n - 1, n, n // 3][:B])
+
+
+@pytest.mark.parametrize("dtype,dh,H,hk,L", [("bf16", 64, 60, 30, 2500), ("bf16", 128, 30, 15, 5000), ("f32", 64, 60, 30, 2500)])
+def test_weights_of_several_runs_with_many_tiles(nova, dtype, dh, H, hk, L):
+    """Four runs of nine tiles of 64 rows (of 17 of 32 in fp32), the last one shorter."""
+    _check_weights(nova, dtype, 1, H, hk, dh, 1050, L)
