@@ -110,9 +110,10 @@ def evict(half: Tuple[np.ndarray, np.ndarray], dst: Tuple[np.ndarray, np.ndarray
 
 
 def block(x: np.ndarray, idx: np.ndarray, weights, K: np.ndarray, V: np.ndarray, heads: int, lens: Sequence[int],
-          counts: Sequence[int], gelu_form: str = "erf", qk_scale=None, ada=None):
+          counts: Sequence[int], gelu_form: str = "erf", qk_scale=None, ada=None, cross=None):
     """The pruned block on cached rows as they read: K, V values [B, heads, capacity, dh], image b's kept tokens
-    idx[b, :counts[b]] among its lens[b] rows (prior ones first, its own behind them).  Returns y_kept [B, k, C], the keys and
+    idx[b, :counts[b]] among its lens[b] rows (prior ones first, its own behind them); the variants are those of
+    nova_oracle.pruned_block.  Returns y_kept [B, k, C], the keys and
     values [B, k, C] of the kept tokens before they are quantised, and the weight the rows collect [B, capacity]."""
     from . import nova_oracle as O
     x = np.asarray(x, dtype=np.float64)
@@ -145,6 +146,12 @@ def block(x: np.ndarray, idx: np.ndarray, weights, K: np.ndarray, V: np.ndarray,
             got[b, :L] += p.sum(0)
             a[:, sl] = p @ V[b, h, :L]
         x1 = xs + g1 * (a @ W["w_o"].T + W.get("b_o", 0.0))
+        if cross is not None:
+            t = {n: np.asarray(cross[n], dtype=np.float64) for n in ("w_cq", "b_cq", "w_co", "b_co", "k_text", "v_text")}
+            qc = O.layer_norm(x1) @ t["w_cq"].T + t["b_cq"]
+            ac = np.concatenate([O.softmax(qc[:, s] @ t["k_text"][b][:, s].T / np.sqrt(dh)) @ t["v_text"][b][:, s]
+                                 for s in (slice(h * dh, (h + 1) * dh) for h in range(heads))], 1)
+            x1 = x1 + ac @ t["w_co"].T + t["b_co"]
         hid = act((O.layer_norm(x1) * (1 + s2) + b2) @ W["w_fc1"].T + W.get("b_fc1", 0.0))
         y[b, :c] = x1 + g2 * (hid @ W["w_fc2"].T + W.get("b_fc2", 0.0))
     return y, kn, vn, got

@@ -27,6 +27,16 @@ def _ints(xs):
     return torch.tensor(list(xs), dtype=torch.int32, device="cuda")
 
 
+def _cross(hx, hb, heads):
+    """Device side of a cross-attention sub-layer; what lies behind the condition tokens is NaN."""
+    c = hb.variant["cross"]
+    n = c["k_text"].shape[1]
+    cap = (n + 63) // 64 * 64
+    return {"text_len": n, "k_text": hx.pack_k_cache(c["k_text"].cuda(), heads, cap, float("nan")),
+            "v_text": hx.pack_v_cache(c["v_text"].cuda(), heads, cap, float("nan")),
+            **{w: c[w].cuda() for w in ("w_cq", "b_cq", "w_co", "b_co")}}
+
+
 def _check(hx, dtype, C, heads, B, grid, P, k, counts=None, lens=None, variant=None, cap_extra=3, seed=31):
     print(f"fourbit block {dtype} C={C} heads={heads} B={B} P={P} k={k} counts={counts} lens={lens} {variant}", flush=True)
     wl = WL.Workload("fourbit", dtype, B=B, C=C, heads=heads, L=1, V=64, keep_hi=.5, keep_lo=.5,
@@ -51,6 +61,8 @@ def _check(hx, dtype, C, heads, B, grid, P, k, counts=None, lens=None, variant=N
         qs, ada = hb.variant.get("qk_scale"), hb.variant.get("ada")
         var = BlockVariant(gelu_tanh=bool(hb.variant.get("gelu_tanh", False)), qk_scale=None if qs is None else qs.cuda(),
                            ada=None if ada is None else ada.cuda())
+        if hb.variant.get("cross") is not None:
+            var.cross = _cross(hx, hb, heads)
     shape = BlockShape(NOVA_BF16 if dtype == "bf16" else NOVA_F32, B, grid * grid, C, heads, P, cap, k)
     ws = torch.full((nova.fourbit_block_workspace_bytes(shape),), 255, dtype=torch.uint8, device="cuda")
     y = torch.full((B, k, C), float("nan"), dtype=tdt, device="cuda")
@@ -69,6 +81,8 @@ def _check(hx, dtype, C, heads, B, grid, P, k, counts=None, lens=None, variant=N
         kw = dict(gelu_form="tanh" if hb.variant.get("gelu_tanh") else "erf",
                   qk_scale=None if hb.variant.get("qk_scale") is None else hx.f64(hb.variant["qk_scale"]),
                   ada=None if hb.variant.get("ada") is None else hx.f64(hb.variant["ada"]))
+        if hb.variant.get("cross") is not None:
+            kw["cross"] = {n: hx.f64(t) for n, t in hb.variant["cross"].items()}
     ry, rk, rv, got = F.block(hx.f64(hb.x), idx, {n: hx.f64(t) for n, t in hb.weights.items()}, K, V, heads, total, live, **kw)
     tol = hx.BF16_TOL if dtype == "bf16" else hx.F32_TOL
     err = max(float(np.abs(hx.f64(y[b, :live[b]]) - ry[b, :live[b]]).max()) for b in range(B) if live[b])
@@ -247,3 +261,13 @@ def test_an_image_of_nan_keeps_its_rows_and_leaves_the_other_alone(hx):
                         assert (st.mass[b, :rows] >= 0).all() and (st.mass[b, rows:] == -1).all()
         got.append(outs)
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("variant", [{"qk_norm"}, {"cross"}, {"cross", "gelu_tanh", "ada"}, {"qk_norm", "gelu_tanh", "ada", "cross"}])
+@pytest.mark.parametrize("C,heads,P,k", [(128, 2, 70, 50), (256, 2, 600, 130)])
+def test_variants_over_prior_rows(hx, dtype, variant, C, heads, P, k):
+    """Unit-length keys in front of the block's own, cross-attention behind the attention over the 4-bit cache, all of it at once;
+    then with images that have lengths and counts of their own."""
+    _check(hx, dtype, C, heads, 2, 13, P, k, variant=variant)
+    _check(hx, dtype, C, heads, 4, 13, P, k, counts=[k, 1, 0, k // 3], lens=[P, 0, 7, P // 2], variant=variant)

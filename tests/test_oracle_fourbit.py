@@ -73,3 +73,25 @@ def test_sums_that_are_no_numbers_add_nothing():
     m, got = F.mass(q, K, 0.125, lse, m_in, [4, 5], [3, 3])
     assert np.isnan(got[0, :4]).all() and m[0].tolist() == [0.5, 0.0, np.inf, 0.0, -1.0]
     assert np.isclose(m[1].sum(), 3 * 2)
+
+
+def test_block_is_the_16_bit_block_on_the_same_rows():
+    """On cached rows that are the block's own keys and values, not rounded, all variants give nova_oracle.pruned_block's result."""
+    from oracle import nova_oracle as O
+    rng = np.random.default_rng(7)
+    B, N, C, heads, k, P, T = 2, 9, 64, 2, 4, 5, 3
+    W = {n: 0.1 * rng.standard_normal(s) for n, s in dict(w_qkv=(3 * C, C), b_qkv=(3 * C,), w_o=(C, C), b_o=(C,), w_fc1=(4 * C, C),
+                                                         b_fc1=(4 * C,), w_fc2=(C, 4 * C), b_fc2=(C,)).items()}
+    x, kp, vp = (rng.standard_normal((B, m, C)) for m in (N, P, P))
+    idx = np.stack([np.sort(rng.permutation(N)[:k]) for _ in range(B)])
+    cross = {"w_cq": 0.1 * rng.standard_normal((C, C)), "b_cq": rng.standard_normal(C), "w_co": 0.1 * rng.standard_normal((C, C)),
+             "b_co": rng.standard_normal(C), "k_text": rng.standard_normal((B, T, C)), "v_text": rng.standard_normal((B, T, C))}
+    for kw in ({}, dict(gelu_form="tanh", ada=rng.standard_normal((B, 6, C))), dict(cross=cross),
+               dict(qk_scale=np.array([3.0, 5.0]), gelu_form="tanh", ada=rng.standard_normal((B, 6, C)), cross=cross)):
+        unit = (lambda t: O.unit_rows(t.reshape(B, -1, heads, C // heads)).reshape(t.shape)) if "qk_scale" in kw else (lambda t: t)
+        prior = unit(kp)
+        y, kn, vn = O.pruned_block(x, idx, W, prior, vp, heads, **kw)
+        K, V = (np.concatenate(p, 1).reshape(B, P + k, heads, C // heads).transpose(0, 2, 1, 3) for p in ((prior, kn), (vp, vn)))
+        y4, k4, v4, got = F.block(x, idx, W, K, V, heads, [P + k] * B, [k] * B, **kw)
+        assert np.allclose(y4, y, atol=1e-12) and np.allclose(k4, kn, atol=1e-12) and np.allclose(v4, vn, atol=1e-12)
+        assert np.isclose(got.sum(), B * heads * k)
