@@ -191,8 +191,9 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
           }
       }
       l_run += psum;
-      if constexpr (NP > 1) {
-        // in the scores' place: with three operands per row registers are short (fp32, 128 channels: 124 -> 111 us; bf16 2 % slower)
+      if constexpr (NP > 1 && DH == 128) {
+        // in the scores' place: with three operands per row registers are short (2458 queries of 2 images, 16 heads of 128, 8883
+        // keys 892 -> 811 us; with 64 channels 2-6 % slower, in bf16 2 %)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 && sizeof(T) == 2 ? 3 : 2) vo
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           bf16_t p[NP];
-          split(NP > 1 ? s[u >> 1][(u & 1) * 8 + i] : e[u >> 1][(u & 1) * 8 + i], p);
+          split(NP > 1 && DH == 128 ? s[u >> 1][(u & 1) * 8 + i] : e[u >> 1][(u & 1) * 8 + i], p);
 #pragma unroll
           for (int x = 0; x < NP; ++x) pf[x][i] = p[x];
         }
