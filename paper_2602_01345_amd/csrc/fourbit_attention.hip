@@ -7,11 +7,14 @@
 //                  softmax: the order of the keys in that product is free, so the values follow the scores' lane layout
 // A workgroup is four waves of 32 rows.  Tiles of 64 keys are converted to bf16 (exactly: a level times a power of two) by
 // all of its threads on the way from registers into LDS, once for the 128 rows; the codes of the tile after next are
-// on the way meanwhile.  Two stages of LDS, two workgroups per CU, so that one wave's softmax runs next to another's MFMAs; a
-// wave asks for priority while it issues MFMAs, or two waves of a SIMD fall into step and take turns at everything (385 us
-// without, 340 with: 2458 queries of 2 images, 16 heads of 128, 8883 keys).  Bound by MFMA and power there (1.1 PFLOP/s, a
-// library product of 8192^3 1.17); with heads of 64 by the softmax's vector instructions (1024 queries of 4 images, 32 heads,
-// 4096 keys 165 us, 0.83 PFLOP/s).
+// on the way meanwhile.  Two stages of LDS, two workgroups per CU (three with bf16 heads of 64), so that one wave's softmax runs
+// next to another's MFMAs; a wave asks for priority while it issues MFMAs, or two waves of a SIMD fall into step and take turns
+// at everything (385 us without, 340 with: 2458 queries of 2 images, 16 heads of 128, 8883 keys).  1.06 PFLOP/s there (a library
+// product x W^T of 8192^3 1.60, with both operands by rows 1.36); with heads of 64 the softmax's vector instructions add to the
+// MFMAs' time (1024 queries of 4 images, 32 heads, 4096 keys 160 us, 0.86 PFLOP/s).
+// Probabilities of bf16 calls go into the second product as bf16: one rounding each (half a step, 2^-8 at most) instead of three
+// MFMAs per operand.  The sum they are divided by is that of the fp32 ones.  One token, 424 keys: rms error 1.93e-3 of the
+// result against 1.67e-3 for its own rounding to bf16 alone.
 #include <algorithm>
 #include <cfloat>
 
@@ -320,6 +323,12 @@ struct Plan {
   int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
 };
 constexpr int kCus = 256;
+// Tiles up to which a block of 16 rows stays whole, eight waves of one workgroup with up to three each, and nothing is joined by a
+// second launch.  One line for both types and head sizes, between the places where it would lie for each (us in one launch / in
+// runs and joined, 32 key heads: bf16, 64 channels 8 tiles 4.9 / 6.2, 16 5.9 / 6.5, 24 6.9 / 6.8, 40 8.7 / 8.0; 128 channels 8
+// 6.0 / 6.8, 16 7.6 / 7.3, 24 9.1 / 7.3; fp32, 128 channels 8 7.8 / 7.9, 24 12.5 / 8.4; 128 key heads: bf16 24 7.7 / 9.7 and 10.3 /
+// 12.2, 40 9.8 / 11.5 and 13.7 / 15.3, fp32, 128 channels 24 13.8 / 16.3).  With 512 key heads the other side is one launch of
+// four waves per block, and faster (128 channels 8 tiles 12.9 / 9.9, 24 24.3 / 22.2).
 constexpr int kFewWhole = 24;
 constexpr int kRanked = 32;          // most images that are ranked: every workgroup does it for itself, a step per image
 Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len, bool ragged) {

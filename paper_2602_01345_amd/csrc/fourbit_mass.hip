@@ -368,7 +368,8 @@ Plan plan(const nova_fourbit_cache& c, int heads, int n, int kv_len) {
   p.pitch = (kv_len + 63) / 64 * 64;
   const int64_t items = std::max((int64_t)c.B * c.kv_heads * p.chunks, (int64_t)1);
   const int tiles = (int)(((int64_t)n * (heads / c.kv_heads) + kSubRows - 1) / kSubRows);
-  // Two workgroups per CU at least; eight, so that they end together, where a run still has 512 rows: its start, the conversion of
+  // Up to two workgroups per CU, as many as fit (one run per item from 257 items on; tiles are counted in 32 rows, so that of
+  // taller ones some runs may get none); eight, so that they end together, where a run still has 512 rows: its start, the conversion of
   // its keys, is then little (us with two / eight: 280 items of 30360 rows 765 / 368; 423 of 1887 77 / 72; 1024 of 1640 the same; but
   // 1024 of 512 in runs of 256 46 / 49, 192 of 600 in runs of 128 19 / 21).
   const int64_t two = std::min((int64_t)tiles, 2 * kCus / items), eight = std::min((int64_t)tiles / 16, (8 * kCus + items - 1) / items);
@@ -394,7 +395,9 @@ hipError_t collect(hipStream_t st, const nova_fourbit_cache& c, int heads, int n
   if (p.few) {
     // Two tiles per wave once that leaves two workgroups per CU: the rows are read once for them, and the next keys on the way
     // meanwhile (us with one / two / four: 4 images, 32 heads of 128 on 8, 32768 rows 21.9 / 17.8 / 18.4; 16 images, 16 heads
-    // of 64, 4096 rows 12.5 / 10.9 / 11.0; 8 images, 600 rows 9.2 / 9.9 / 9.8).
+    // of 64, 4096 rows 12.5 / 10.9 / 11.0; 8 images, 600 rows 9.2 / 9.9 / 9.8).  The capacity decides, which the grid has to cover:
+    // rows behind an image's are marked.  A long cache with few rows in it pays for that (the first of these shapes with one /
+    // two: 300 rows of 32768 6.6 / 7.7, 2000 7.5 / 8.0, 8000 10.2 / 9.5).
     const int tile_groups = kFewWaves / p.few * 64;
     const bool two = (int64_t)c.B * c.capacity / tile_groups >= 4 * kCus;
     const int keys = tile_groups * (two ? 2 : 1);
