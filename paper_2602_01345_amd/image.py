@@ -21,7 +21,8 @@ advances.  Nothing on that path synchronises with the host.
 
 With ``cache_bits=4`` the K/V caches are held in 4 bits (``nova_pruned_block_fourbit``), and ``evict_to`` bounds them: every
 block collects the attention weight of its cached rows, and after a scale that leaves a block with more rows than that, the
-rows that have collected least go (``nova_select`` on the weights, ``nova_fourbit_evict``).
+rows that have collected least go (``nova_select`` on the weights, ``nova_fourbit_evict``).  A planned scale then changes what
+it reads: it is launched once per image, in order.
 """
 from __future__ import annotations
 
@@ -247,9 +248,23 @@ class ImageRunner:
             self._evict(plan.evictions, plan.evict_idx, plan.evict_mask, per_image=False)
         return x
 
+    def _moved_by(self, plan: ScalePlan) -> List[torch.Tensor]:
+        """What a second run of the scale would not find as the first one did: nothing unless rows are evicted (a block's own rows
+        are appended where they were); else the weights, which grow, and after the scale the caches, which change places."""
+        if plan.stores is None or self.evict_to is None:
+            return []
+        moved = {id(st): st for e in plan.evictions or [] for st in e[:2]}
+        return ([st.mass for st in {**moved, **{id(st): st for st in plan.stores}}.values()] +
+                [t for st in moved.values()
+                 for t in (st.cache.k_codes, st.cache.k_scales, st.cache.v_codes, st.cache.v_scales, st.rows)])
+
     def capture(self, plan: ScalePlan):
-        """Records the scale's launches into a HIP graph (after one eager run that warms every code path)."""
+        """Records the scale's launches into a HIP graph (after one eager run that warms every code path).  The caches, their
+        weights and row counts are afterwards what they were before, so that an image may be at any of its scales."""
+        saved = [(t, t.clone()) for t in self._moved_by(plan)]
         self.enqueue(plan)
+        for t, was in saved:
+            t.copy_(was)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):

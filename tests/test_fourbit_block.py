@@ -271,3 +271,19 @@ def test_variants_over_prior_rows(hx, dtype, variant, C, heads, P, k):
     then with images that have lengths and counts of their own."""
     _check(hx, dtype, C, heads, 2, 13, P, k, variant=variant)
     _check(hx, dtype, C, heads, 4, 13, P, k, counts=[k, 1, 0, k // 3], lens=[P, 0, 7, P // 2], variant=variant)
+
+
+@pytest.mark.parametrize("evict_to", [None, 12, 4])
+def test_scales_captured_in_the_middle_of_an_image(hx, evict_to):
+    """Every scale is recorded when the image has come to it, then launched: recording leaves the caches, the weights and the row
+    counts as they were.  The graphs then serve further images."""
+    r, xs, logits, tables = _runner(hx, "bf16", evict_to)
+    want = [s.out.clone() for s in _run(r, xs, logits, tables)]
+    r.reset()
+    plans = r.plan_image(tables, {t: logits[t] for t in tables}, 2)
+    for image in range(3):
+        for p, w in zip(plans, want):
+            p.x.copy_(xs[p.t])
+            if image == 0:
+                r.capture(p)
+            assert torch.equal(r.launch(p), w), (image, p.t)
