@@ -476,6 +476,7 @@ int nova_fourbit_evict(nova_ctx* ctx, void* stream, const nova_fourbit_cache* sr
  *   cache    B, kv_heads = heads, dh of the shape
  *   mass     fp32 [B, capacity] or NULL: the weight that the rows have collected after this block, from mass_in [B, capacity]
  *            (NULL: none before; may be the mass array itself) and the kept queries of this call, as nova_fourbit_mass
+ *            (k == 0 is a no-op here as there: a mass array of its own is not written either)
  *   workspace  of at least nova_fourbit_block_workspace_bytes(shape), 256-byte aligned
  */
 size_t nova_fourbit_block_workspace_bytes(const nova_block_shape* shape);
