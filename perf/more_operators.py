@@ -424,7 +424,6 @@ def _prepare_own(case, s):
     H, hk = case["heads"], case["kv_heads"]
     if case["kind"] == "choose":
         s["idx"] = torch.empty((B, n, hk, case["k"]), dtype=torch.int32, device="cuda")
-        s["before"] = s["lens"] - n                              # rows that were there before the chunk
         return
     if case["kind"] == "attend":
         need = _NOVA.paged_attention_workspace_bytes(s["own"], B, H, n, case["kv_len"])
@@ -456,8 +455,7 @@ def run(s):
         return s["cache"]
     lens = s["lens"] if case["ragged"] else None
     if kind == "choose":
-        _NOVA.paged_summarise(s["own"], s["table"], s["means"], L - case["n"], L, first_per_row=s["before"] if case["ragged"] else None,
-                              kv_len_per_row=lens)
+        _NOVA.paged_summarise(s["own"], s["table"], s["means"], case["n"], L, kv_len_per_row=lens)
         _NOVA.paged_select(s["means"], s["table"], case["page_rows"], s["q"], s["idx"], L, first=1, recent=1,
                            causal=case["causal"], kv_len_per_row=lens)
         return s["means"], s["idx"]
