@@ -486,6 +486,110 @@ int nova_pruned_block_fourbit(nova_ctx* ctx, void* stream, const nova_block_shap
                               const float* mass_in, float* mass, void* y_kept, void* workspace, size_t workspace_bytes);
 
 /*
+ * A key/value cache in pages: one pool for images (and blocks) whose lengths differ and change, in place of a buffer of full
+ * capacity for each.  Keys and values have one layout, a row per key:
+ *   k_pages, v_pages   [pages, kv_heads, page_rows, dh] in dtype NOVA_F32 | NOVA_BF16, dense, 16-byte aligned
+ *   table              DEVICE int32 [B, pitch]: row r of image b is row r % page_rows of page table[b][r / page_rows].  Entries from
+ *                      an image's last page on are not looked at; an entry that is no page of the pool reads as rows of zeros
+ * page_rows is 16, 32, 64, 128 or 256, dh 64 or 128; pages * page_rows <= 2^30; heads that attend share a key head in runs of
+ * heads / kv_heads.  Nothing reads what lies behind an image's rows.  Per-image arrays (..._per_row) are DEVICE int32 [B] or NULL,
+ * clamped on the device like those of nova_pruned_block_rows; kv_len <= pitch * page_rows.
+ */
+typedef struct nova_paged_cache {
+  void* k_pages;
+  void* v_pages;
+  int32_t dtype;
+  int32_t pages;
+  int32_t kv_heads;
+  int32_t page_rows;
+  int32_t dh;
+} nova_paged_cache;
+
+/*
+ * Page lists and slots from the images' lengths, on the device.  Image b has now = kv_len_per_row[b] rows (NULL: kv_len) in
+ * ceil(now / page_rows) pages; the first keep_per_row[b] of them stay (clamped to [0, now]; NULL: all), and n_per_row[b] come behind
+ * those (clamped to [0, n]; NULL: n).  So 0 kept and 0 to come give an image's pages back, 0 kept and some to come put another
+ * in its place, some kept and 0 to come cut it back.
+ *   table        in/out [B, pitch].  Pages an image no longer needs go onto the stack of free pages, in the order of images and
+ *                pages; then images that need more take theirs from its top, in the same order, behind what they have.  The
+ *                first image that asks for more pages than are left, and every later one that asks for any, gets none: it keeps
+ *                what it has, and of its new rows come those that fit there
+ *   free_pages   in/out DEVICE int32 [pages]: the stack, its bottom first; free_count DEVICE int32 [1]: its height (clamped to
+ *                [0, pages]).  Entries from the new height on are left as they were
+ *   free_next    out DEVICE int32 [1]: its height afterwards; may be free_count itself
+ *   kv_len_next  out DEVICE int32 [B]: rows of the images afterwards; may be kv_len_per_row (or another input) itself
+ *   slots        out DEVICE int32 [B, n] or NULL: where image b's new row s goes, page * page_rows + row of the page; -1 where none
+ *                comes.  One map serves all blocks whose pools share the table
+ * kv_len + n <= pitch * page_rows, B <= 4096, B * max(n, pitch) <= 2^30, pages * page_rows <= 2^30.  The table's other entries are
+ * untouched.  free_pages, table, slots and the rest must not overlap but as said.
+ */
+int nova_paged_reserve(nova_ctx* ctx, void* stream, int B, int32_t* table, int pitch, int page_rows, int pages, int n,
+                       const int32_t* n_per_row, const int32_t* keep_per_row, int kv_len, const int32_t* kv_len_per_row,
+                       int32_t* free_pages, const int32_t* free_count, int32_t* free_next, int32_t* kv_len_next, int32_t* slots);
+
+/* Rows k, v [B, n, kv_heads, dh] of the cache's dtype and any strides (rows of a projection's output, or the dense caches of
+ * nova_pruned_block) to the slots [B, n]: one launch.  A slot outside [0, pages * page_rows) takes no row; two rows with one slot
+ * leave either. */
+int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, int n, const nova_rows* k,
+                      const nova_rows* v, const int32_t* slots);
+
+/*
+ * Attention of a chunk of n queries per image over the image's rows.  The live queries, n_per_row[b] of them (clamped to [0, n];
+ * NULL: n), are those of the image's last rows, kv_len_per_row[b] (clamped to [0, kv_len]; NULL: kv_len) of which there are:
+ *   out[b, s, h] = sum_j softmax_j(scale * <q[b, s, h], K[b, g, j]>) V[b, g, j],  g = h / (heads / kv_heads),
+ * over all rows j of the image (causal 0), or (causal 1) over j <= kv_len_per_row[b] - n_per_row[b] + s.
+ *   q          [B, n, heads, dh] of the cache's dtype, stride_channel 1, every other stride a multiple of 16 bytes, 16-byte aligned
+ *   out        out [B, n, heads, dh] dense, 16-byte aligned; must not alias q
+ *   lse        out fp32 [B, n, heads] or NULL: ln of the sum of e^(scale * score)
+ *   workspace  of at least nova_paged_attention_workspace_bytes, 16-byte aligned (may be NULL where that is 0); calls that overlap,
+ *              captured graphs among them, need one each.  0 bytes for sizes that the call refuses
+ * B * heads * n <= 2^30, B <= 65535.  Queries past n_per_row[b], and queries that see no row, get zeros and lse = -inf.  A row that a
+ * query does not see has no part in its result, whatever its key and value are (NaN among them).  NOVA_F32: products of fp32
+ * numbers, summed in fp32; NOVA_BF16: probabilities are rounded to bf16 in front of the second product.
+ */
+size_t nova_paged_attention_workspace_bytes(const nova_paged_cache* cache, int B, int heads, int n, int kv_len);
+int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch,
+                         int heads, int n, const nova_rows* q, const int32_t* n_per_row, int kv_len,
+                         const int32_t* kv_len_per_row, int causal, float scale, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes);
+
+/*
+ * Sparse attention: every query reads the pages it has chosen.
+ *
+ * nova_paged_summarise writes the means of the pages that the last n_per_row[b] rows (NULL: n) of every image lie in, after they
+ * have been appended:
+ *   means   in/out DEVICE bf16 [pages, kv_heads, dh], 16-byte aligned: the mean of a page's rows that exist, taken in 64 bits, as the
+ *           nearest w * 2^e, w a whole number (of two the even one), with one e per page and key head: the smallest, -100 <= e <= 100,
+ *           for which no |w| passes 127 (from e = 100 on they stop there).  A page with a NaN or an infinity has means of NaN.
+ *           Other pages' means are untouched.
+ *
+ * nova_paged_select chooses for every (query, key head) k of the pages it sees, by
+ *   score[i] = max over the heads h that share the key head of <w[h], means[i]>,
+ * w[h] being the query rounded as the means are, one e for all these heads (a query with a NaN or an infinity: zeros).  The `first`
+ * pages from the front and the `recent` ones that end the rows the query sees are chosen in any case, and so are pages with means
+ * of NaN; of two scores alike the lower page's counts as higher.  Scores are exact: what a query chooses does not depend on what else
+ * is in the call.
+ *   chosen  out DEVICE int32 [B, n, kv_heads, k]: ordinals in the image's page list, ascending, then -1
+ *   q       as in nova_paged_attention, of type dtype
+ * 1 <= k <= 256, first + recent <= k, kv_len <= 16384 * page_rows; with causal 1 recent >= 1 (the page a query lies in may hold rows
+ * behind it, in its mean too).
+ *
+ * nova_paged_sparse_attention is nova_paged_attention over the rows of the chosen pages alone (those of them that the query sees).
+ * Order and repeats in a list do not matter, entries that are no page of the image's rows count for nothing.  A query without any
+ * gets zeros and lse = -inf.
+ */
+int nova_paged_summarise(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch, int n,
+                         const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row, void* means);
+int nova_paged_select(nova_ctx* ctx, void* stream, int dtype, const void* means, int pages, int kv_heads, int page_rows, int dh,
+                      int B, const int32_t* table, int pitch, int heads, int n, const nova_rows* q, const int32_t* n_per_row,
+                      int kv_len, const int32_t* kv_len_per_row, int causal, int first, int recent, int k, int32_t* chosen);
+size_t nova_paged_sparse_attention_workspace_bytes(const nova_paged_cache* cache, int B, int heads, int n, int kv_len, int k);
+int nova_paged_sparse_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch,
+                                const int32_t* chosen, int k, int heads, int n, const nova_rows* q, const int32_t* n_per_row,
+                                int kv_len, const int32_t* kv_len_per_row, int causal, float scale, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes);
+
+/*
  * Instrumentation (not part of the hot path): per-kernel device timing with HIP events on
  * the caller's stream.  While a stage's bit is set in `stage_mask`, every launch of that
  * stage by the four entry points is bracketed by a pair of events (created on the host as

@@ -50,6 +50,11 @@ class _Rows(C.Structure):
     _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("stride_b", "stride_row", "stride_head", "stride_channel")]
 
 
+class _PagedCache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p)] + [(n, C.c_int32) for n in
+                                                                     ("dtype", "pages", "kv_heads", "page_rows", "dh")]
+
+
 @dataclass(frozen=True, eq=False)
 class FourBitCache:
     """nova_fourbit_cache: keys and values of B images in 4 bits, uint8 device tensors: codes [B, kv_heads, capacity, dh / 2]
@@ -92,6 +97,38 @@ class FourBitCache:
         c.made_of, c.device = ptrs, ts[0].get_device()
         if any(t.get_device() != c.device for t in ts):
             raise ValueError("the arrays of a cache lie on one device")
+        object.__setattr__(self, "_c", c)
+        return c
+
+
+@dataclass(frozen=True, eq=False)
+class PagedCache:
+    """nova_paged_cache: a pool of pages of keys and of values, device tensors [pages, kv_heads, page_rows, dh] (f32 | bf16)."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    _c: Optional["_PagedCache"] = field(default=None, init=False, repr=False)
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, page_rows: int, dh: int, dtype: torch.dtype = torch.bfloat16,
+              device: Union[str, int, torch.device] = "cuda") -> "PagedCache":
+        """A pool of pages that hold whatever the memory held."""
+        return cls(*[torch.empty((pages, kv_heads, page_rows, dh), dtype=dtype, device=device) for _ in range(2)])
+
+    @property
+    def page_rows(self) -> int:
+        return self.k_pages.shape[2]
+
+    def c_struct(self) -> "_PagedCache":
+        """The C structure: made and checked on the first call, and again only if a tensor has got other memory since."""
+        k, v = self.k_pages, self.v_pages
+        ptrs = (k.data_ptr(), v.data_ptr())
+        c = self._c
+        if c is not None and c.made_of == ptrs:
+            return c
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.get_device() != v.get_device():
+            raise ValueError(f"no cache in pages: {tuple(k.shape)} {k.dtype} on {k.device}, {tuple(v.shape)} {v.dtype} on {v.device}")
+        c = _PagedCache(_ptr(k), _ptr(v), _dtype_code(k), *k.shape)
+        c.made_of, c.device = ptrs, k.get_device()
         object.__setattr__(self, "_c", c)
         return c
 
@@ -207,6 +244,21 @@ def load_library() -> C.CDLL:
         f.restype = i32
     for f in (lib.nova_fourbit_attention_workspace_bytes, lib.nova_fourbit_mass_workspace_bytes):
         f.argtypes, f.restype = [cache, i32, i32, i32], sz
+    pool = C.POINTER(_PagedCache)
+    lib.nova_paged_reserve.argtypes = [vp, vp, i32, vp, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.nova_paged_append.argtypes = [vp, vp, pool, i32, i32, rows, rows, vp]
+    lib.nova_paged_attention.argtypes = [vp, vp, pool, i32, vp, i32, i32, i32, rows, vp, i32, vp, i32, C.c_float, vp, vp, vp, sz]
+    lib.nova_paged_summarise.argtypes = [vp, vp, pool, i32, vp, i32, i32, vp, i32, vp, vp]
+    lib.nova_paged_select.argtypes = ([vp, vp, i32, vp, i32, i32, i32, i32, i32, vp, i32, i32, i32, rows, vp, i32, vp] + [i32] * 4 +
+                                      [vp])
+    lib.nova_paged_sparse_attention.argtypes = [vp, vp, pool, i32, vp, i32, vp, i32, i32, i32, rows, vp, i32, vp, i32, C.c_float, vp,
+                                                vp, vp, sz]
+    for f in (lib.nova_paged_reserve, lib.nova_paged_append, lib.nova_paged_attention, lib.nova_paged_summarise,
+              lib.nova_paged_select, lib.nova_paged_sparse_attention):
+        f.restype = i32
+    lib.nova_paged_attention_workspace_bytes.argtypes = [pool, i32, i32, i32, i32]
+    lib.nova_paged_sparse_attention_workspace_bytes.argtypes = [pool, i32, i32, i32, i32, i32]
+    lib.nova_paged_attention_workspace_bytes.restype = lib.nova_paged_sparse_attention_workspace_bytes.restype = sz
     lib.nova_probe.argtypes = [vp, vp, i32, vp, vp, i64, i32, vp, C.POINTER(C.c_double)]
     lib.nova_probe.restype = i32
     lib.nova_profile_stages.restype = i32
@@ -654,6 +706,128 @@ class Nova:
             _shaped("mass", mass, (B, c.capacity), torch.float32, self.device), _ptr(y_kept), _ptr(workspace), workspace.nbytes)
         if rc:
             self._check(rc, "nova_pruned_block_fourbit")
+
+    # -- a cache in pages -----------------------------------------------------------
+    # Like those of the 4-bit cache: on the context's device, on that device's current stream.
+    def _pool(self, cache: PagedCache) -> "_PagedCache":
+        c = cache.c_struct()
+        if c.device != self.device:
+            raise ValueError(f"cache on device {c.device}, context on device {self.device}")
+        return c
+
+    def _table(self, table: torch.Tensor) -> int:
+        if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_contiguous() or table.get_device() != self.device:
+            raise ValueError(f"table: {tuple(table.shape)} {table.dtype} {table.stride()} on {table.device}, expected dense [B, pitch] "
+                             f"int32 on device {self.device}")
+        return table.data_ptr()
+
+    def paged_reserve(self, table: torch.Tensor, page_rows: int, n: int, kv_len: int, free_pages: torch.Tensor,
+                      free_count: torch.Tensor, kv_len_next: torch.Tensor, free_next: Optional[torch.Tensor] = None,
+                      slots: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None,
+                      n_per_row: Optional[torch.Tensor] = None, keep_per_row: Optional[torch.Tensor] = None):
+        """Page lists table [B, pitch] int32 and slots [B, n] int32 of n rows to come per image.  free_pages [pages] int32: the
+        stack of free pages, free_count [1] int32 its height; free_next [1]: its height afterwards (None: free_count itself);
+        kv_len_next [B] int32: rows of the images afterwards (may be kv_len_per_row)."""
+        dev, at = self.device, self._table(table)
+        B, pitch = table.shape
+        pages = free_pages.shape[0]
+        rc = self.lib.nova_paged_reserve(
+            self.ctx, _stream(dev), B, at, pitch, page_rows, pages, n, self._counts(B, "n_per_row", n_per_row),
+            self._counts(B, "keep_per_row", keep_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row),
+            _shaped("free_pages", free_pages, (pages,), torch.int32, dev), self._counts(1, "free_count", free_count),
+            self._counts(1, "free_next", free_count if free_next is None else free_next),
+            self._counts(B, "kv_len_next", kv_len_next), _shaped("slots", slots, (B, n), torch.int32, dev))
+        if rc:
+            self._check(rc, "nova_paged_reserve")
+
+    def paged_append(self, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor):
+        """Rows k, v [B, n, kv_heads, dh] (the cache's dtype, any strides) to slots [B, n] int32 (-1: nowhere)."""
+        c = self._pool(cache)
+        if k.shape != v.shape or k.dtype != cache.k_pages.dtype or v.dtype != k.dtype:
+            raise ValueError(f"k {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}, a cache of {cache.k_pages.dtype}")
+        self._here(k, v)
+        ks = _rows(k, c.kv_heads, c.dh, "k")
+        rc = self.lib.nova_paged_append(self.ctx, _stream(self.device), c, k.shape[0], k.shape[1], ks,
+                                        _rows(v, c.kv_heads, c.dh, "v"),
+                                        _shaped("slots", slots, k.shape[:2], torch.int32, self.device))
+        if rc:
+            self._check(rc, "nova_paged_append")
+
+    def paged_attention_workspace_bytes(self, cache: PagedCache, B: int, heads: int, n: int, kv_len: int) -> int:
+        return self.lib.nova_paged_attention_workspace_bytes(cache.c_struct(), B, heads, n, kv_len)
+
+    def paged_attention(self, cache: PagedCache, table: torch.Tensor, q: torch.Tensor, out: torch.Tensor,
+                        workspace: Optional[torch.Tensor], kv_len: int, causal: bool = False, scale: Optional[float] = None,
+                        lse: Optional[torch.Tensor] = None, n_per_row: Optional[torch.Tensor] = None,
+                        kv_len_per_row: Optional[torch.Tensor] = None):
+        """out [B, n, heads, dh] = attention of q [B, n, heads, dh] (the cache's dtype, channels dense), the images' last rows, over
+        all of their rows or (causal) those up to their own; lse [B, n, heads] f32 or None.  scale: 1 / sqrt(dh) where None."""
+        self._paged_attention("nova_paged_attention", cache, table, None, q, out, workspace, kv_len, causal, scale, lse, n_per_row,
+                              kv_len_per_row)
+
+    def _paged_attention(self, name, cache, table, chosen, q, out, workspace, kv_len, causal, scale, lse, n_per_row, kv_len_per_row):
+        c = self._pool(cache)
+        shape = q.shape
+        if len(shape) != 4 or q.dtype != cache.k_pages.dtype:
+            raise ValueError(f"q {tuple(shape)} {q.dtype}, a cache of {cache.k_pages.dtype}")
+        B, n, heads, dh = shape
+        if table.shape[0] != B:
+            raise ValueError(f"{B} images of queries, {table.shape[0]} in the table")
+        dev, at = self.device, self._table(table)
+        self._here(q, workspace)
+        lists = ()
+        if chosen is not None:
+            k = chosen.shape[-1]
+            lists = (_shaped("chosen", chosen, (B, n, c.kv_heads, k), torch.int32, dev), k)
+        rc = getattr(self.lib, name)(
+            self.ctx, _stream(dev), c, B, at, table.shape[1], *lists, heads, n, _rows(q, heads, c.dh, "q"),
+            self._counts(B, "n_per_row", n_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row), int(causal),
+            dh ** -0.5 if scale is None else scale, _shaped("out", out, shape, q.dtype, dev),
+            _shaped("lse", lse, (B, n, heads), torch.float32, dev), _ptr(workspace), 0 if workspace is None else workspace.nbytes)
+        if rc:
+            self._check(rc, name)
+
+    def paged_summarise(self, cache: PagedCache, table: torch.Tensor, means: torch.Tensor, n: int, kv_len: int,
+                        n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None):
+        """means [pages, kv_heads, dh] bf16: those of the pages that the images' last n rows lie in."""
+        c = self._pool(cache)
+        B, dev, at = table.shape[0], self.device, self._table(table)
+        rc = self.lib.nova_paged_summarise(
+            self.ctx, _stream(dev), c, B, at, table.shape[1], n, self._counts(B, "n_per_row", n_per_row), kv_len,
+            self._counts(B, "kv_len_per_row", kv_len_per_row),
+            _shaped("means", means, (c.pages, c.kv_heads, c.dh), torch.bfloat16, dev))
+        if rc:
+            self._check(rc, "nova_paged_summarise")
+
+    def paged_select(self, means: torch.Tensor, table: torch.Tensor, page_rows: int, q: torch.Tensor, chosen: torch.Tensor,
+                     kv_len: int, first: int = 1, recent: int = 1, causal: bool = False, n_per_row: Optional[torch.Tensor] = None,
+                     kv_len_per_row: Optional[torch.Tensor] = None):
+        """chosen [B, n, kv_heads, k] int32: the pages that queries q [B, n, heads, dh] (f32 | bf16, channels dense) read, by the means
+        [pages, kv_heads, dh] bf16 of the pages."""
+        B, n, heads, dh = q.shape
+        pages, kv_heads, _ = means.shape
+        k, dev, at = chosen.shape[-1], self.device, self._table(table)
+        if table.shape[0] != B:
+            raise ValueError(f"{B} images of queries, {table.shape[0]} in the table")
+        self._here(q)
+        rc = self.lib.nova_paged_select(
+            self.ctx, _stream(dev), _dtype_code(q), _shaped("means", means, (pages, kv_heads, dh), torch.bfloat16, dev), pages,
+            kv_heads, page_rows, dh, B, at, table.shape[1], heads, n, _rows(q, heads, dh, "q"),
+            self._counts(B, "n_per_row", n_per_row), kv_len, self._counts(B, "kv_len_per_row", kv_len_per_row), int(causal), first,
+            recent, k, _shaped("chosen", chosen, (B, n, kv_heads, k), torch.int32, dev))
+        if rc:
+            self._check(rc, "nova_paged_select")
+
+    def paged_sparse_attention_workspace_bytes(self, cache: PagedCache, B: int, heads: int, n: int, kv_len: int, k: int) -> int:
+        return self.lib.nova_paged_sparse_attention_workspace_bytes(cache.c_struct(), B, heads, n, kv_len, k)
+
+    def paged_sparse_attention(self, cache: PagedCache, table: torch.Tensor, chosen: torch.Tensor, q: torch.Tensor,
+                               out: torch.Tensor, workspace: Optional[torch.Tensor], kv_len: int, causal: bool = False,
+                               scale: Optional[float] = None, lse: Optional[torch.Tensor] = None,
+                               n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None):
+        """paged_attention over the rows of the pages chosen [B, n, kv_heads, k] alone (as paged_select writes them)."""
+        self._paged_attention("nova_paged_sparse_attention", cache, table, chosen, q, out, workspace, kv_len, causal, scale, lse,
+                              n_per_row, kv_len_per_row)
 
 
 # ------------------------------------------------------------------------------------

@@ -133,6 +133,73 @@ int fourbit_query_error(int dtype, const nova_fourbit_cache* cache, int heads, i
   return rows_error(q, dtype, cache->B, n, heads, true);
 }
 
+// A cache in pages.  At most 2^30 rows in a pool: slots have 32 bits, offsets between pages 64.
+int paged_sizes_error(const nova_paged_cache* c) {
+  if (!c) return NOVA_ERR_INVALID_ARG;
+  if (!valid_dtype(c->dtype)) return NOVA_ERR_UNSUPPORTED;
+  if (c->pages < 0 || c->kv_heads < 1) return NOVA_ERR_INVALID_ARG;
+  if (c->dh != 64 && c->dh != 128) return NOVA_ERR_UNSUPPORTED;
+  if (c->page_rows < 16 || c->page_rows > 256 || (c->page_rows & (c->page_rows - 1)) != 0) return NOVA_ERR_UNSUPPORTED;
+  if (c->kv_heads > 32767 || c->pages > (1 << 30) / c->page_rows) return NOVA_ERR_UNSUPPORTED;
+  return NOVA_OK;
+}
+int paged_error(const nova_paged_cache* c) {
+  if (int rc = paged_sizes_error(c)) return rc;
+  if (c->pages == 0) return NOVA_OK;
+  for (const void* p : {c->k_pages, c->v_pages})
+    if (!p || !aligned16(p)) return NOVA_ERR_INVALID_ARG;
+  return NOVA_OK;
+}
+// Page lists of B images that have kv_len rows at most.
+int table_error(const int32_t* table, int B, int pitch, int page_rows, int64_t kv_len) {
+  if (B < 0 || pitch < 0 || kv_len < 0 || kv_len > (int64_t)pitch * page_rows) return NOVA_ERR_INVALID_ARG;
+  if (B > 65535 || kv_len > 1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (!aligned(table, 4) || (B > 0 && pitch > 0 && !table)) return NOVA_ERR_INVALID_ARG;
+  return NOVA_OK;
+}
+constexpr int kMostChosen = 256;         // pages per query and key head
+constexpr int kMostPages = 16384;        // pages of an image that queries choose from
+int chosen_error(int64_t kv_len, int page_rows, int k) {
+  if (k < 1) return NOVA_ERR_INVALID_ARG;
+  if (k > kMostChosen || kv_len > (int64_t)kMostPages * page_rows) return NOVA_ERR_UNSUPPORTED;
+  return NOVA_OK;
+}
+int paged_query_sizes_error(int B, int kv_heads, int heads, int n) {
+  if (heads < 1 || n < 0 || heads % kv_heads != 0) return NOVA_ERR_INVALID_ARG;
+  constexpr int kMost = 1 << 30;
+  if (B > 0 && (heads > kMost / B || n > kMost / (B * heads))) return NOVA_ERR_UNSUPPORTED;
+  return NOVA_OK;
+}
+size_t paged_workspace(const nova_paged_cache* c, int B, int heads, int n, int kv_len, int k) {
+  if (paged_sizes_error(c) != NOVA_OK || B < 1 || B > 65535 || n < 1 || kv_len < 0 || kv_len > 1 << 30) return 0;
+  if (paged_query_sizes_error(B, c->kv_heads, heads, n) != NOVA_OK) return 0;
+  if (k != 0 && chosen_error(kv_len, c->page_rows, k) != NOVA_OK) return 0;
+  return paged_attention_workspace_bytes(*c, B, heads, n, kv_len, k);
+}
+// nova_paged_attention (chosen == nullptr, k == 0) and nova_paged_sparse_attention.
+int paged_attend(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch,
+                 const int32_t* chosen, int k, int heads, int n, const nova_rows* q, const int32_t* n_per_row, int kv_len,
+                 const int32_t* kv_len_per_row, int causal, float scale, void* out, float* lse, void* workspace,
+                 size_t workspace_bytes) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  if (int rc = paged_error(cache)) return rc;
+  if (int rc = table_error(table, B, pitch, cache->page_rows, kv_len)) return rc;
+  if (int rc = paged_query_sizes_error(B, cache->kv_heads, heads, n)) return rc;
+  if (int rc = counts_error({n_per_row, kv_len_per_row, lse, chosen})) return rc;
+  if (causal != 0 && causal != 1) return NOVA_ERR_INVALID_ARG;
+  if (B == 0 || n == 0) return NOVA_OK;
+  if (!q) return NOVA_ERR_INVALID_ARG;
+  if (int rc = rows_error(q, cache->dtype, B, n, heads, true)) return rc;
+  if (!out || !aligned16(out) || out == q->data) return NOVA_ERR_INVALID_ARG;
+  const size_t need = paged_workspace(cache, B, heads, n, kv_len, k);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace))) return NOVA_ERR_WORKSPACE;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  const PagedCall call = {cache, B, table, pitch, heads, n, settled(*q, B, n, heads), n_per_row, kv_len, kv_len_per_row, causal,
+                          scale * kAttnLog2e, chosen, k, out, lse, workspace};
+  return launch_paged_attention(static_cast<hipStream_t>(stream), call) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
 // What the block calls check of everything but the cache and the workspace; `plain`: the shape to hold against the kernels'
 // limits.  Sets `var`.  Returns 1 where there is nothing to do.
 int block_error(const nova_block_shape* plain, const nova_block_weights* weights, const nova_block_variant* variant,
@@ -750,6 +817,116 @@ int nova_pruned_block_fourbit(nova_ctx* ctx, void* stream, const nova_block_shap
     e = launch_block_f32(ctx, st, *shape, *weights, var, rows, static_cast<const float*>(x), kept_idx, nullptr, nullptr,
                          static_cast<float*>(y_kept), ws, &fb);
   return e == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+int nova_paged_reserve(nova_ctx* ctx, void* stream, int B, int32_t* table, int pitch, int page_rows, int pages, int n,
+                       const int32_t* n_per_row, const int32_t* keep_per_row, int kv_len, const int32_t* kv_len_per_row,
+                       int32_t* free_pages, const int32_t* free_count, int32_t* free_next, int32_t* kv_len_next, int32_t* slots) {
+  if (!ctx || n < 0) return NOVA_ERR_INVALID_ARG;
+  const nova_paged_cache sizes = {nullptr, nullptr, NOVA_BF16, pages, 1, page_rows, 64};
+  if (int rc = paged_sizes_error(&sizes)) return rc;
+  if (kv_len < 0) return NOVA_ERR_INVALID_ARG;
+  if (int rc = table_error(table, B, pitch, page_rows, (int64_t)kv_len + n)) return rc;
+  if (B > 4096 || (int64_t)B * std::max(n, pitch) > 1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (int rc = counts_error({n_per_row, keep_per_row, kv_len_per_row, free_pages, free_count, free_next, kv_len_next, slots})) return rc;
+  if (B == 0) return NOVA_OK;
+  if (!free_count || !free_next || !kv_len_next || (pages > 0 && !free_pages)) return NOVA_ERR_INVALID_ARG;
+  // what a launch writes while others of its threads read
+  const size_t per = (size_t)B * 4, lists = per * pitch, map = slots ? per * n : 0, stack = (size_t)pages * 4;
+  if (overlap(table, lists, free_pages, stack) || overlap(table, lists, slots, map) || overlap(free_pages, stack, slots, map))
+    return NOVA_ERR_INVALID_ARG;
+  for (const void* p : {n_per_row, keep_per_row, kv_len_per_row, (const int32_t*)kv_len_next})
+    if (overlap(table, lists, p, per) || overlap(free_pages, stack, p, per) || overlap(slots, map, p, per)) return NOVA_ERR_INVALID_ARG;
+  for (const void* p : {free_count, (const int32_t*)free_next})
+    if (overlap(table, lists, p, 4) || overlap(free_pages, stack, p, 4) || overlap(slots, map, p, 4)) return NOVA_ERR_INVALID_ARG;
+  if (overlap(kv_len_next, per, free_next, 4)) return NOVA_ERR_INVALID_ARG;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  PagedReserve r = {};
+  r.B = B; r.shift = __builtin_ctz(page_rows); r.pages = pages; r.pitch = pitch; r.n = n; r.kv_len = kv_len;
+  r.table = table; r.free_pages = free_pages; r.free_count = free_count;
+  r.kv_rows = kv_len_per_row; r.n_rows = n_per_row; r.keep_rows = keep_per_row;
+  r.kv_next = kv_len_next; r.free_next = free_next; r.slots = slots;
+  return launch_paged_reserve(static_cast<hipStream_t>(stream), r) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, int n, const nova_rows* k,
+                      const nova_rows* v, const int32_t* slots) {
+  if (!ctx || B < 0 || n < 0) return NOVA_ERR_INVALID_ARG;
+  if (int rc = paged_error(cache)) return rc;
+  if (int rc = counts_error({slots})) return rc;
+  if (B > 65535 || (int64_t)B * n > 1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (B == 0 || n == 0 || cache->pages == 0) return NOVA_OK;
+  if (!k || !v || !slots) return NOVA_ERR_INVALID_ARG;
+  for (const nova_rows* r : {k, v})
+    if (int rc = rows_error(r, cache->dtype, B, n, cache->kv_heads, false)) return rc;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  return launch_paged_append(static_cast<hipStream_t>(stream), *cache, B, n, settled(*k, B, n, cache->kv_heads),
+                             settled(*v, B, n, cache->kv_heads), slots) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+size_t nova_paged_attention_workspace_bytes(const nova_paged_cache* cache, int B, int heads, int n, int kv_len) {
+  return paged_workspace(cache, B, heads, n, kv_len, 0);
+}
+
+int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch,
+                         int heads, int n, const nova_rows* q, const int32_t* n_per_row, int kv_len,
+                         const int32_t* kv_len_per_row, int causal, float scale, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes) {
+  return paged_attend(ctx, stream, cache, B, table, pitch, nullptr, 0, heads, n, q, n_per_row, kv_len, kv_len_per_row, causal, scale,
+                      out, lse, workspace, workspace_bytes);
+}
+
+int nova_paged_summarise(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch, int n,
+                         const int32_t* n_per_row, int kv_len, const int32_t* kv_len_per_row, void* means) {
+  if (!ctx || n < 0) return NOVA_ERR_INVALID_ARG;
+  if (int rc = paged_error(cache)) return rc;
+  if (int rc = table_error(table, B, pitch, cache->page_rows, kv_len)) return rc;
+  if (int rc = counts_error({n_per_row, kv_len_per_row})) return rc;
+  if (B == 0 || n == 0 || kv_len == 0 || cache->pages == 0) return NOVA_OK;
+  if (!means || !aligned16(means)) return NOVA_ERR_INVALID_ARG;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  return launch_paged_summarise(static_cast<hipStream_t>(stream), *cache, B, table, pitch, n, n_per_row, kv_len, kv_len_per_row,
+                                means) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+int nova_paged_select(nova_ctx* ctx, void* stream, int dtype, const void* means, int pages, int kv_heads, int page_rows, int dh,
+                      int B, const int32_t* table, int pitch, int heads, int n, const nova_rows* q, const int32_t* n_per_row,
+                      int kv_len, const int32_t* kv_len_per_row, int causal, int first, int recent, int k, int32_t* chosen) {
+  if (!ctx) return NOVA_ERR_INVALID_ARG;
+  const nova_paged_cache sizes = {nullptr, nullptr, dtype, pages, kv_heads, page_rows, dh};
+  if (int rc = paged_sizes_error(&sizes)) return rc;
+  if (int rc = table_error(table, B, pitch, page_rows, kv_len)) return rc;
+  if (int rc = paged_query_sizes_error(B, kv_heads, heads, n)) return rc;
+  if (int rc = chosen_error(kv_len, page_rows, k)) return rc;
+  if (int rc = counts_error({n_per_row, kv_len_per_row, chosen})) return rc;
+  if ((causal != 0 && causal != 1) || first < 0 || recent < 0 || first > k || recent > k - first || recent < causal)
+    return NOVA_ERR_INVALID_ARG;
+  if (B == 0 || n == 0) return NOVA_OK;
+  if (!q || !chosen || !aligned16(means) || (pages > 0 && !means)) return NOVA_ERR_INVALID_ARG;
+  if (int rc = rows_error(q, dtype, B, n, heads, true)) return rc;
+  const DeviceScope device(ctx);
+  if (device.rc) return device.rc;
+  const PagedSelect s = {dtype, B, pages, kv_heads, __builtin_ctz(page_rows), dh, pitch, heads, n, kv_len, first, recent, k, causal,
+                         means, table, settled(*q, B, n, heads), n_per_row, kv_len_per_row, chosen};
+  return launch_paged_select(static_cast<hipStream_t>(stream), s) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
+}
+
+size_t nova_paged_sparse_attention_workspace_bytes(const nova_paged_cache* cache, int B, int heads, int n, int kv_len, int k) {
+  return k < 1 ? 0 : paged_workspace(cache, B, heads, n, kv_len, k);
+}
+
+int nova_paged_sparse_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch,
+                                const int32_t* chosen, int k, int heads, int n, const nova_rows* q, const int32_t* n_per_row,
+                                int kv_len, const int32_t* kv_len_per_row, int causal, float scale, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes) {
+  if (int rc = paged_error(cache)) return rc;
+  if (int rc = chosen_error(kv_len, cache->page_rows, k)) return rc;
+  if (B > 0 && n > 0 && !chosen) return NOVA_ERR_INVALID_ARG;
+  return paged_attend(ctx, stream, cache, B, table, pitch, chosen, k, heads, n, q, n_per_row, kv_len, kv_len_per_row, causal, scale,
+                      out, lse, workspace, workspace_bytes);
 }
 
 }  // extern "C"

@@ -390,7 +390,7 @@ hipError_t attend(hipStream_t st, const nova_fourbit_cache& c, int heads, int n,
   a.q = static_cast<const T*>(q.data);
   a.q_sb = q.stride_b; a.q_sr = q.stride_row; a.q_sh = q.stride_head;
   a.c = fourbit_view(c);
-  a.heads = heads; a.G = heads / c.kv_heads; a.n = n; a.P = P;
+  a.heads = heads; a.hk = c.kv_heads; a.G = heads / c.kv_heads; a.n = n; a.P = P;
   a.n_rows = n_rows; a.kv_rows = kv_rows;
   // Rows past the last have scores of -inf, which a scale of 0 would make NaN.  The smallest positive fp32 number (2^-149) in its
   // place leaves less than 2^-21 of any finite score: no two weights differ by more than that.

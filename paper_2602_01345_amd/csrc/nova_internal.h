@@ -200,3 +200,48 @@ size_t fourbit_mass_workspace_bytes(const nova_fourbit_cache& c, int heads, int 
 hipError_t launch_fourbit_mass(const nova_ctx* ctx, hipStream_t st, int dtype, const nova_fourbit_cache& c, int heads, int n,
                                const nova_rows& q, const int32_t* n_rows, int P, const int32_t* kv_rows, float scale_log2,
                                const float* lse, const float* mass_in, float* mass, void* workspace);
+
+// paged_cache.hip: page lists, slots, rows into pages, means of pages (include/nova.h: nova_paged_reserve, _append, _summarise)
+struct PagedReserve {
+  int B, shift, pages, pitch, n, kv_len;
+  int32_t* table;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  const int32_t *kv_rows, *n_rows, *keep_rows;      // or nullptr
+  int32_t *kv_next, *free_next, *slots;             // slots may be nullptr
+};
+hipError_t launch_paged_reserve(hipStream_t st, const PagedReserve& r);
+hipError_t launch_paged_append(hipStream_t st, const nova_paged_cache& c, int B, int n, const nova_rows& k, const nova_rows& v,
+                               const int32_t* slots);
+hipError_t launch_paged_summarise(hipStream_t st, const nova_paged_cache& c, int B, const int32_t* table, int pitch, int n,
+                                  const int32_t* n_rows, int kv_len, const int32_t* kv_rows, void* means);
+// paged_select.hip: the pages that score highest for each query
+struct PagedSelect {
+  int dtype, B, pages, hk, shift, dh, pitch, heads, n, kv_len, first, recent, k, causal;
+  const void* means;
+  const int32_t* table;
+  nova_rows q;
+  const int32_t *n_rows, *kv_rows;
+  int32_t* chosen;
+};
+hipError_t launch_paged_select(hipStream_t st, const PagedSelect& s);
+// paged_attention.hip: attention over such a cache; take > 0: over the pages in chosen [B, n, kv_heads, take]
+struct PagedCall {
+  const nova_paged_cache* cache;
+  int B;
+  const int32_t* table;
+  int pitch, heads, n;
+  nova_rows q;
+  const int32_t* n_rows;
+  int kv_len;
+  const int32_t* kv_rows;
+  int causal;
+  float scale_log2;         // score scale * log2 e
+  const int32_t* chosen;
+  int take;
+  void* out;
+  float* lse;
+  void* workspace;
+};
+size_t paged_attention_workspace_bytes(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take);
+hipError_t launch_paged_attention(hipStream_t st, const PagedCall& call);

@@ -1,0 +1,149 @@
+// Attention over a cache in pages: how a call is divided over workgroups, and the joining of key runs.
+#include <algorithm>
+#include <cfloat>
+
+#include "paged.h"
+
+namespace {
+
+// The runs of the cut items joined: out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  A thread has four channels of
+// one row and every SL-th run; with many runs per row the threads of a row join through LDS.  Runs that had no tiles have
+// left a sum of 0 and nothing else.
+template <typename T, int DH, int SL>
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_rows, int used_rows) {
+  constexpr int C4 = DH / 4, RPW = 256 / (C4 * SL);
+  __shared__ f32x4 part_o[SL > 1 ? 256 : 1];
+  __shared__ float part_m[SL > 1 ? 256 / C4 : 1], part_l[SL > 1 ? 256 / C4 : 1];
+  const int tid = threadIdx.x, c4 = tid % C4, sl = tid / C4 % SL;
+  const int64_t r = (int64_t)blockIdx.x * RPW + tid / (C4 * SL);
+  const int ci = (int)(r / used_rows), rr = (int)(r - (int64_t)ci * used_rows);
+  int b, j, block, g_unused;
+  a.place(min(a.n_whole + ci, a.items - 1), b, j, block);
+  const int row = block * block_rows + rr;
+  const bool there = a.n_whole + ci < a.items && row < a.n * a.G;
+  const int count = image_count(a.n_rows, b, a.n), len = image_prior(a.kv_rows, b, a.P);
+  const int s_row = div_by(there ? row : 0, a.G, a.G_inv, g_unused);
+  bool some = there && s_row < count && visible_keys(a.causal, len, count, s_row) > 0;
+  const int64_t p0 = (int64_t)ci * a.nsplit * block_rows + rr;
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s = sl; some && s < a.nsplit; s += SL) {
+    const int64_t p = p0 + (int64_t)s * block_rows;
+    const float ms = a.part_ml[p * 2], ls = a.part_ml[p * 2 + 1];
+    if (ls == 0.f) continue;
+    const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + p * DH + c4 * 4);
+    // a run without a finite score has reference -inf and a sum of NaN: it is added as it is
+    const float mn = fmaxf(m, ms);
+    const float w0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn), w1 = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - mn);
+    l = l * w0 + ls * w1;
+    acc = acc * w0 + o * w1;
+    m = mn;
+  }
+  if constexpr (SL > 1) {
+    part_o[tid] = acc;
+    if (c4 == 0) {
+      part_m[tid / C4] = m;
+      part_l[tid / C4] = l;
+    }
+    __syncthreads();
+    if (sl > 0 || !there) return;
+    const int g = tid / C4;
+    for (int s = 1; s < SL; ++s) m = fmaxf(m, part_m[g + s]);
+    l = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < SL; ++s) {
+      const float w = part_m[g + s] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(part_m[g + s] - m);
+      l = fmaf(w, part_l[g + s], l);
+      acc += w * part_o[tid + s * C4];
+    }
+  }
+  if (!there) return;
+  if (a.chosen && l == 0.f) some = false;                        // the query has chosen no page that it sees
+  const int64_t to = a.out_row(b, j, row);
+  store_four(a.out + to * DH + c4 * 4, some ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, some ? 1.0f / l : 0.f);
+  if (a.lse && c4 == 0) a.lse[to] = some ? ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+// How a call is divided: blocks of 16 mt rows, items below n_whole one workgroup each, the others nsplit runs of run_tiles tiles.
+struct Plan {
+  int mt, block_rows, blocks, items, n_whole, nsplit, run_tiles, listed;
+  int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
+};
+constexpr int kCus = 256;
+Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take) {
+  const int G = heads / c.kv_heads, rows = n * G;
+  const int tile = c.dtype == NOVA_BF16 ? paged_few_tile<bf16_t>(c.dh) : paged_few_tile<float>(c.dh);
+  Plan p = {};
+  p.mt = rows <= 16 ? 1 : 2;
+  p.block_rows = 16 * p.mt;
+  p.blocks = (rows + p.block_rows - 1) / p.block_rows;
+  p.items = B * c.kv_heads * p.blocks;
+  p.n_whole = p.items;
+  p.nsplit = 1;
+  // most keys a block goes over: all, or what its queries may have chosen
+  const int pages = (kv_len + c.page_rows - 1) / c.page_rows;
+  const int queries = std::min({p.block_rows, (p.block_rows - 1) / G + 2, n});
+  p.listed = take > 0 ? (int)std::min<int64_t>(pages, (int64_t)queries * take) : 0;
+  const int64_t keys = take > 0 ? std::min<int64_t>((int64_t)p.listed * c.page_rows, kv_len + c.page_rows) : kv_len;
+  const int ntiles = (int)((keys + tile - 1) / tile);
+  p.run_tiles = ntiles;
+  const int want = std::min((8 * kCus + p.items - 1) / p.items, ntiles);         // waves per item: eight per CU, a tile each
+  if (want > 4) {
+    p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
+    p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
+    if (p.nsplit > 1) p.n_whole = 0;
+  }
+  return p;
+}
+
+size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+template <typename T>
+hipError_t attend(hipStream_t st, const PagedCall& call) {
+  const nova_paged_cache& c = *call.cache;
+  const Plan p = plan(c, call.B, call.heads, call.n, call.kv_len, call.take);
+  PagedArgs<T> a = {};
+  a.q = static_cast<const T*>(call.q.data);
+  a.q_sb = call.q.stride_b; a.q_sr = call.q.stride_row; a.q_sh = call.q.stride_head;
+  a.heads = call.heads; a.hk = c.kv_heads; a.G = call.heads / c.kv_heads; a.n = call.n; a.P = call.kv_len;
+  a.n_rows = call.n_rows; a.kv_rows = call.kv_rows;
+  // Keys that a row does not see have scores of -inf, which a scale of 0 would make NaN.  The smallest positive fp32 number
+  // (2^-149) in its place leaves less than 2^-21 of any finite score: no two weights differ by more than that.
+  a.scale_log2 = call.scale_log2 == 0.f ? FLT_TRUE_MIN : call.scale_log2;
+  a.out = static_cast<T*>(call.out);
+  a.lse = call.lse;
+  a.keys = static_cast<const T*>(c.k_pages);
+  a.values = static_cast<const T*>(c.v_pages);
+  a.table = call.table; a.pitch = call.pitch; a.pages = c.pages; a.shift = __builtin_ctz(c.page_rows); a.causal = call.causal;
+  a.chosen = call.chosen; a.take = call.take;
+  a.most_pages = (call.kv_len + c.page_rows - 1) / c.page_rows;
+  a.most_listed = p.listed;
+  a.blocks = p.blocks; a.items = p.items; a.dealt = p.items / (8 * p.blocks) * 8 * p.blocks;
+  a.blocks_inv = div_inv(p.blocks); a.hk_inv = div_inv(c.kv_heads); a.G_inv = div_inv(a.G); a.nsplit_inv = div_inv(p.nsplit);
+  a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles;
+  a.part_o = static_cast<float*>(call.workspace);
+  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(call.workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
+  const hipError_t e = launch_paged_few<T>(st, c.dh, p.mt, (unsigned)(p.n_whole + p.runs()), a);
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const int used = std::min(p.block_rows, call.n * a.G);         // rows of a block that there are, where it is the only one
+  const int64_t rows = (int64_t)(p.items - p.n_whole) * used;
+#define GO(DH, SL) join_kernel<T, DH, SL><<<(unsigned)((rows * (DH / 4 * SL) + 255) / 256), 256, 0, st>>>(a, p.block_rows, used)
+  if (c.dh == 64) { if (p.nsplit > 4) GO(64, 8); else GO(64, 1); }
+  else { if (p.nsplit > 4) GO(128, 8); else GO(128, 1); }
+#undef GO
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t paged_attention_workspace_bytes(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take) {
+  const Plan p = plan(c, B, heads, n, kv_len, take);
+  if (p.nsplit == 1) return 0;
+  const size_t rows = (size_t)p.runs() * p.block_rows;
+  return up256(rows * c.dh * 4) + up256(rows * 8);
+}
+
+hipError_t launch_paged_attention(hipStream_t st, const PagedCall& call) {
+  return call.cache->dtype == NOVA_BF16 ? attend<bf16_t>(st, call) : attend<float>(st, call);
+}

@@ -1,0 +1,195 @@
+"""Arguments that the entry points of the cache in pages refuse, on the host and before anything looks into the context or touches
+a GPU: a block of zeros stands in for the context, numbers for the device pointers."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2602_01345_amd import PagedCache, load_library
+from paper_2602_01345_amd import binding as Bn
+
+INVALID, UNSUPPORTED, WORKSPACE = -1, -2, -3
+BASE = 1 << 24
+MAX = 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return load_library()
+
+
+_CTX = C.create_string_buffer(4096)
+
+
+def _cache(dtype=1, pages=100, kv_heads=2, page_rows=16, dh=64, k=BASE, v=2 * BASE):
+    return Bn._PagedCache(k, v, dtype, pages, kv_heads, page_rows, dh)
+
+
+def _rows(n=3, heads=2, dh=64, at=40, **kw):
+    r = Bn._Rows(BASE * at, n * heads * dh, heads * dh, dh, 1)
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+def _ref(x):
+    return None if x is None else C.byref(x)
+
+
+def _reserve(lib, ctx=_CTX, B=2, table=BASE, pitch=10, page_rows=16, pages=100, n=3, n_rows=None, keep=None, kv_len=50, kv_rows=None,
+             free=2 * BASE, count=3 * BASE, free_next=4 * BASE, kv_next=5 * BASE, slots=6 * BASE):
+    return lib.nova_paged_reserve(ctx, None, B, table, pitch, page_rows, pages, n, n_rows, keep, kv_len, kv_rows, free, count, free_next,
+                                  kv_next, slots)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(ctx=None), INVALID), (dict(n=-1), INVALID), (dict(B=-1), INVALID), (dict(pitch=-1), INVALID), (dict(kv_len=-1), INVALID),
+    (dict(kv_len=158), INVALID), (dict(n=111), INVALID), (dict(n=MAX, kv_len=MAX), INVALID), (dict(pages=-1), INVALID),
+    (dict(page_rows=24), UNSUPPORTED), (dict(page_rows=8), UNSUPPORTED), (dict(page_rows=512), UNSUPPORTED), (dict(page_rows=0), UNSUPPORTED),
+    (dict(page_rows=-16), UNSUPPORTED), (dict(pages=(1 << 26) + 1), UNSUPPORTED), (dict(B=4097), UNSUPPORTED),
+    (dict(pitch=1 << 30), UNSUPPORTED), (dict(pitch=1 << 27, n=1 << 30), UNSUPPORTED),
+    (dict(table=0), INVALID), (dict(table=BASE + 2), INVALID), (dict(free=0), INVALID), (dict(count=0), INVALID), (dict(free_next=0), INVALID),
+    (dict(kv_next=0), INVALID), (dict(n_rows=BASE * 9 + 1), INVALID), (dict(keep=BASE * 9 + 2), INVALID), (dict(kv_rows=BASE * 9 + 3), INVALID),
+    (dict(free=2 * BASE + 1), INVALID), (dict(slots=BASE * 6 + 2), INVALID),
+    (dict(slots=BASE + 4), INVALID), (dict(free=BASE + 40), INVALID), (dict(slots=2 * BASE), INVALID), (dict(kv_next=BASE), INVALID),
+    (dict(n_rows=2 * BASE + 396), INVALID), (dict(kv_rows=6 * BASE), INVALID), (dict(count=BASE + 76), INVALID), (dict(free_next=6 * BASE), INVALID),
+    (dict(free_next=5 * BASE + 4), INVALID), (dict(keep=BASE + 76), INVALID),
+])
+def test_reserve(lib, kw, rc):
+    assert _reserve(lib, **kw) == rc
+
+
+def _append(lib, ctx=_CTX, cache=None, B=2, n=3, k=None, v=None, slots=BASE * 9):
+    return lib.nova_paged_append(ctx, None, _ref(cache or _cache()), B, n, _ref(k or _rows()), _ref(v or _rows(at=41)), slots)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(ctx=None), INVALID), (dict(B=-1), INVALID), (dict(n=-1), INVALID), (dict(slots=None), INVALID), (dict(slots=BASE + 2), INVALID),
+    (dict(B=70000), UNSUPPORTED), (dict(B=2, n=MAX), UNSUPPORTED), (dict(k=_rows(data=0)), INVALID), (dict(v=_rows(data=BASE + 1)), INVALID),
+    (dict(k=_rows(stride_row=-64)), INVALID), (dict(v=_rows(stride_channel=-1)), INVALID), (dict(v=_rows(stride_b=(1 << 40) + 1)), INVALID),
+])
+def test_append(lib, kw, rc):
+    assert _append(lib, **kw) == rc
+
+
+def _attend(lib, ctx=_CTX, cache=None, B=2, table=BASE * 3, pitch=10, heads=4, n=3, q=None, n_rows=None, kv_len=50, kv_rows=None, causal=0,
+            out=BASE * 8, lse=None, ws=BASE * 16, ws_bytes=1 << 40, chosen=None, k=0):
+    q = _rows(heads=4) if q is None else q
+    lists = () if chosen is None else (chosen, k)
+    f = lib.nova_paged_attention if chosen is None else lib.nova_paged_sparse_attention
+    return f(ctx, None, _ref(cache or _cache()), B, table, pitch, *lists, heads, n, _ref(q), n_rows, kv_len, kv_rows, causal, 0.125, out, lse,
+             ws, ws_bytes)
+
+
+def _sparse(lib, chosen=BASE * 7, k=4, **kw):
+    return _attend(lib, chosen=chosen, k=k, **kw)
+
+
+def _select(lib, ctx=_CTX, dtype=1, means=BASE, pages=100, kv_heads=2, page_rows=16, dh=64, B=2, table=BASE * 3, pitch=10, heads=4, n=3, q=None,
+            n_rows=None, kv_len=50, kv_rows=None, causal=0, first=1, recent=1, k=4, chosen=BASE * 7):
+    q = _rows(heads=4) if q is None else q
+    return lib.nova_paged_select(ctx, None, dtype, means, pages, kv_heads, page_rows, dh, B, table, pitch, heads, n, _ref(q), n_rows, kv_len,
+                                 kv_rows, causal, first, recent, k, chosen)
+
+
+def _summarise(lib, ctx=_CTX, cache=None, B=2, table=BASE * 3, pitch=10, n=3, n_rows=None, kv_len=50, kv_rows=None, means=BASE * 5):
+    return lib.nova_paged_summarise(ctx, None, _ref(cache or _cache()), B, table, pitch, n, n_rows, kv_len, kv_rows, means)
+
+
+@pytest.mark.parametrize("call", [_append, _attend, _sparse, _summarise])
+@pytest.mark.parametrize("cache,rc", [
+    (_cache(dtype=2), UNSUPPORTED), (_cache(pages=-1), INVALID), (_cache(kv_heads=0), INVALID), (_cache(dh=96), UNSUPPORTED),
+    (_cache(page_rows=20), UNSUPPORTED), (_cache(page_rows=512), UNSUPPORTED), (_cache(kv_heads=40000), UNSUPPORTED),
+    (_cache(pages=1 << 27), UNSUPPORTED), (_cache(k=0), INVALID), (_cache(v=BASE + 8), INVALID),
+])
+def test_caches(lib, call, cache, rc):
+    assert call(lib, cache=cache) == rc
+
+
+@pytest.mark.parametrize("call", [_attend, _sparse, _select, _summarise])
+@pytest.mark.parametrize("kw,rc", [
+    (dict(ctx=None), INVALID), (dict(B=-1), INVALID), (dict(B=70000), UNSUPPORTED), (dict(pitch=-1), INVALID), (dict(pitch=3), INVALID),
+    (dict(kv_len=-1), INVALID), (dict(kv_len=161), INVALID), (dict(n=-1), INVALID), (dict(table=0), INVALID), (dict(table=BASE + 1), INVALID),
+    (dict(n_rows=BASE + 1), INVALID), (dict(kv_rows=BASE + 2), INVALID), (dict(kv_len=(1 << 30) + 1, pitch=1 << 28), UNSUPPORTED),
+])
+def test_tables(lib, call, kw, rc):
+    assert call(lib, **kw) == rc
+
+
+@pytest.mark.parametrize("call", [_attend, _sparse, _select])
+@pytest.mark.parametrize("kw,rc", [
+    (dict(heads=0), INVALID), (dict(heads=3), INVALID), (dict(n=1 << 28), UNSUPPORTED), (dict(B=16, heads=1 << 30, n=1 << 30), UNSUPPORTED),
+    (dict(B=65535, heads=MAX - 1, n=MAX), UNSUPPORTED), (dict(causal=2), INVALID), (dict(causal=-1), INVALID),
+    (dict(q=_rows(heads=4, data=0)), INVALID), (dict(q=_rows(heads=4, data=BASE + 8)), INVALID), (dict(q=_rows(heads=4, stride_channel=2)), INVALID),
+    (dict(q=_rows(heads=4, stride_row=260)), INVALID), (dict(q=_rows(heads=4, stride_head=65)), INVALID), (dict(q=_rows(heads=4, stride_b=-768)), INVALID),
+])
+def test_queries(lib, call, kw, rc):
+    assert call(lib, **kw) == rc
+
+
+@pytest.mark.parametrize("call", [_attend, _sparse])
+def test_outputs(lib, call):
+    assert call(lib, out=0) == INVALID and call(lib, out=BASE + 8) == INVALID and call(lib, lse=BASE + 2) == INVALID
+    assert call(lib, out=_rows(heads=4).data) == INVALID
+
+
+@pytest.mark.parametrize("call", [_sparse, _select])
+@pytest.mark.parametrize("kw,rc", [
+    (dict(k=0), INVALID), (dict(k=-3), INVALID), (dict(k=257), UNSUPPORTED), (dict(kv_len=16 * 16384 + 1, pitch=20000), UNSUPPORTED),
+    (dict(chosen=BASE + 2), INVALID), (dict(chosen=0), INVALID),
+])
+def test_choices(lib, call, kw, rc):
+    assert call(lib, **kw) == rc
+
+
+@pytest.mark.parametrize("kw", [dict(first=-1), dict(recent=-1), dict(first=4), dict(first=2, recent=3), dict(recent=0, causal=1), dict(means=0),
+                                dict(means=BASE + 8), dict(first=MAX, recent=MAX)])
+def test_select(lib, kw):
+    assert _select(lib, **kw) == INVALID
+
+
+def test_select_types(lib):
+    for kw in (dict(dtype=2), dict(dh=32), dict(page_rows=48), dict(kv_heads=40000, heads=40000)):
+        assert _select(lib, **kw) == UNSUPPORTED
+    assert _summarise(lib, means=0) == INVALID and _summarise(lib, means=BASE + 4) == INVALID
+
+
+def test_nothing_to_do_is_no_error(lib):
+    for call in (_append, _attend, _sparse, _select, _summarise):
+        assert call(lib, B=0) == 0 and call(lib, n=0) == 0
+    assert _reserve(lib, B=0) == 0 and _append(lib, cache=_cache(pages=0, k=0, v=0)) == 0 and _summarise(lib, kv_len=0) == 0
+
+
+@pytest.mark.parametrize("shape", [dict(n=1, kv_len=4000), dict(n=40, kv_len=4000), dict(n=700, kv_len=20)])
+def test_workspaces_too_small(lib, shape):
+    c = _cache(pages=1000)
+    for call, need in ((_attend, lib.nova_paged_attention_workspace_bytes(C.byref(c), 2, 4, shape["n"], shape["kv_len"])),
+                       (_sparse, lib.nova_paged_sparse_attention_workspace_bytes(C.byref(c), 2, 4, shape["n"], shape["kv_len"], 4))):
+        if need:
+            for ws, nbytes in ((None, 0), (BASE * 16, need - 1), (BASE * 16 + 8, need)):
+                assert call(lib, cache=c, pitch=250, ws=ws, ws_bytes=nbytes, **shape) == WORKSPACE
+    assert lib.nova_paged_attention_workspace_bytes(C.byref(c), 2, 4, 1, 4000) > 0
+
+
+def test_no_workspace_for_sizes_that_the_calls_refuse(lib):
+    a, s = lib.nova_paged_attention_workspace_bytes, lib.nova_paged_sparse_attention_workspace_bytes
+    for c, B, heads, n, kv_len in ((None, 2, 4, 1, 9000), (_cache(), 2, 3, 1, 9000), (_cache(), 2, 4, 0, 9000), (_cache(dh=80), 2, 4, 1, 9000),
+                                   (_cache(), -1, 4, 1, 9000), (_cache(), 65536, 4, 1, 9000), (_cache(), 2, 4, 1, -1), (_cache(), 2, 4, 1, MAX),
+                                   (_cache(), 16, 1 << 30, 1 << 30, 9000), (_cache(page_rows=7), 2, 4, 1, 9000), (_cache(), 65535, MAX - 1, MAX, 9)):
+        assert a(_ref(c), B, heads, n, kv_len) == 0 and s(_ref(c), B, heads, n, kv_len, 4) == 0
+    for k, kv_len in ((0, 9000), (-1, 9000), (257, 9000), (4, 16 * 16384 + 1)):
+        assert s(_ref(_cache()), 2, 4, 1, kv_len, k) == 0
+
+
+def test_binding_looks_at_shapes_and_types():
+    t = torch.zeros(4, 2, 16, 64)
+    with pytest.raises(ValueError):
+        PagedCache(t, t[:3]).c_struct()
+    with pytest.raises(ValueError):
+        PagedCache(t, t.bfloat16()).c_struct()
+    with pytest.raises(ValueError):
+        PagedCache(t[0], t[0]).c_struct()
+    with pytest.raises(AssertionError):
+        PagedCache(t, t).c_struct()                              # not on a device
+    c = PagedCache.empty(3, 2, 32, 128, device="cpu")
+    assert c.page_rows == 32 and c.k_pages.dtype == torch.bfloat16 and c.v_pages.shape == (3, 2, 32, 128)
