@@ -18,7 +18,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
   const int64_t r = (int64_t)blockIdx.x * RPW + tid / (C4 * SL);
   const int ci = (int)(r / used_rows), rr = (int)(r - (int64_t)ci * used_rows);
   int b, j, block, g_unused;
-  a.place(min(a.n_whole + ci, a.items - 1), b, j, block);
+  a.place_block(min(a.n_whole + ci, a.items - 1), b, j, block);
   const int row = block * block_rows + rr;
   const bool there = a.n_whole + ci < a.items && row < a.n * a.G;
   const int count = image_count(a.n_rows, b, a.n), len = image_prior(a.kv_rows, b, a.P);
@@ -65,34 +65,54 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
   if (a.lse && c4 == 0) a.lse[to] = some ? ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
-// How a call is divided: blocks of 16 mt rows, items below n_whole one workgroup each, the others nsplit runs of run_tiles tiles.
+// How a call is divided: mt > 0: blocks of 16 mt rows (paged_few.hip), else blocks of kPagedRows (paged_many.hip); items below n_whole
+// are one workgroup each, the others nsplit runs (of run_tiles tiles where that is not 0).
 struct Plan {
-  int mt, block_rows, blocks, items, n_whole, nsplit, run_tiles, listed;
+  int mt, block_rows, blocks, items, n_whole, nsplit, run_tiles, ranked, listed;
   int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
 };
 constexpr int kCus = 256;
-Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take) {
+constexpr int kRanked = 32;          // most images that are ranked: every workgroup does it for itself, a step per image
+Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take, bool ragged) {
   const int G = heads / c.kv_heads, rows = n * G;
-  const int tile = c.dtype == NOVA_BF16 ? paged_few_tile<bf16_t>(c.dh) : paged_few_tile<float>(c.dh);
+  const bool wide = c.dtype == NOVA_F32;
   Plan p = {};
-  p.mt = rows <= 16 ? 1 : 2;
-  p.block_rows = 16 * p.mt;
+  p.mt = rows <= 16 ? 1 : rows <= 32 || take > 0 || wide ? 2 : 0;
+  const int64_t blocks32 = (int64_t)B * c.kv_heads * ((rows + 31) / 32);
+  if (p.mt == 0 && blocks32 <= 2 * kCus && kv_len <= 2048) p.mt = 2;
+  p.block_rows = p.mt ? 16 * p.mt : kPagedRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;
   p.items = B * c.kv_heads * p.blocks;
   p.n_whole = p.items;
   p.nsplit = 1;
-  // most keys a block goes over: all, or what its queries may have chosen
-  const int pages = (kv_len + c.page_rows - 1) / c.page_rows;
-  const int queries = std::min({p.block_rows, (p.block_rows - 1) / G + 2, n});
-  p.listed = take > 0 ? (int)std::min<int64_t>(pages, (int64_t)queries * take) : 0;
-  const int64_t keys = take > 0 ? std::min<int64_t>((int64_t)p.listed * c.page_rows, kv_len + c.page_rows) : kv_len;
-  const int ntiles = (int)((keys + tile - 1) / tile);
-  p.run_tiles = ntiles;
-  const int want = std::min((8 * kCus + p.items - 1) / p.items, ntiles);         // waves per item: eight per CU, a tile each
-  if (want > 4) {
-    p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
-    p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
-    if (p.nsplit > 1) p.n_whole = 0;
+  if (p.mt) {
+    const int tile = wide ? paged_few_tile<float>(c.dh) : paged_few_tile<bf16_t>(c.dh);
+    // most keys a block goes over: all, or what its queries may have chosen
+    const int pages = (kv_len + c.page_rows - 1) / c.page_rows;
+    const int queries = std::min({p.block_rows, (p.block_rows - 1) / G + 2, n});
+    p.listed = take > 0 ? (int)std::min<int64_t>(pages, (int64_t)queries * take) : 0;
+    const int64_t keys = take > 0 ? (int64_t)p.listed * c.page_rows : kv_len;
+    const int ntiles = (int)((keys + tile - 1) / tile);
+    p.run_tiles = ntiles;
+    const int want = std::min((8 * kCus + p.items - 1) / p.items, ntiles);       // waves per item: eight per CU, a tile each
+    if (want > 4) {
+      p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
+      p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
+      if (p.nsplit > 1) p.n_whole = 0;
+    }
+    return p;
+  }
+  const int ntiles = (kv_len + 63) / 64, slots = 2 * kCus, rest = p.items % slots;
+  // Images with lengths of their own: the longest first, so that short ones fill up the end; from two rounds of items on that is
+  // enough and none is cut.
+  p.ranked = ragged && p.items > slots && B > 1 && B <= kRanked ? B : 0;
+  if (rest == 0 || (p.ranked && p.items >= 2 * slots)) return p;
+  // A few more items than CUs, and long ones: most CUs would have one, which is little to hide anything behind, and the others two.
+  const bool in_three = p.items > kCus && p.items <= kCus + kCus / 4 && ntiles >= 64;
+  const int s = in_three ? 3 : std::min(slots / rest, ntiles / 4);
+  if (s >= 2) {
+    p.n_whole = p.items - rest;
+    p.nsplit = s;
   }
   return p;
 }
@@ -102,7 +122,7 @@ size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 template <typename T>
 hipError_t attend(hipStream_t st, const PagedCall& call) {
   const nova_paged_cache& c = *call.cache;
-  const Plan p = plan(c, call.B, call.heads, call.n, call.kv_len, call.take);
+  const Plan p = plan(c, call.B, call.heads, call.n, call.kv_len, call.take, call.kv_rows != nullptr);
   PagedArgs<T> a = {};
   a.q = static_cast<const T*>(call.q.data);
   a.q_sb = call.q.stride_b; a.q_sr = call.q.stride_row; a.q_sh = call.q.stride_head;
@@ -121,10 +141,13 @@ hipError_t attend(hipStream_t st, const PagedCall& call) {
   a.most_listed = p.listed;
   a.blocks = p.blocks; a.items = p.items; a.dealt = p.items / (8 * p.blocks) * 8 * p.blocks;
   a.blocks_inv = div_inv(p.blocks); a.hk_inv = div_inv(c.kv_heads); a.G_inv = div_inv(a.G); a.nsplit_inv = div_inv(p.nsplit);
-  a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles;
+  a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles; a.ranked = p.ranked;
   a.part_o = static_cast<float*>(call.workspace);
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(call.workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
-  const hipError_t e = launch_paged_few<T>(st, c.dh, p.mt, (unsigned)(p.n_whole + p.runs()), a);
+  const unsigned grid = (unsigned)(p.n_whole + p.runs());
+  hipError_t e;
+  if constexpr (sizeof(T) == 2) e = p.mt ? launch_paged_few<T>(st, c.dh, p.mt, grid, a) : launch_paged_many(st, c.dh, grid, a);
+  else e = launch_paged_few<T>(st, c.dh, p.mt, grid, a);
   if (e != hipSuccess || p.nsplit == 1) return e;
   const int used = std::min(p.block_rows, call.n * a.G);         // rows of a block that there are, where it is the only one
   const int64_t rows = (int64_t)(p.items - p.n_whole) * used;
@@ -138,7 +161,7 @@ hipError_t attend(hipStream_t st, const PagedCall& call) {
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take) {
-  const Plan p = plan(c, B, heads, n, kv_len, take);
+  const Plan p = plan(c, B, heads, n, kv_len, take, false);      // of the two the one that asks for more
   if (p.nsplit == 1) return 0;
   const size_t rows = (size_t)p.runs() * p.block_rows;
   return up256(rows * c.dh * 4) + up256(rows * 8);

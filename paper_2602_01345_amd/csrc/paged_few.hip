@@ -18,10 +18,6 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// some bf16 number of the two in w is no finite one: an exponent of ones carries into the bit above it
-__device__ __forceinline__ uint32_t odd_pair(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
-__device__ __forceinline__ uint32_t odd_one(uint32_t w) { return (w & 0x7F800000u) + 0x00800000u & 0x80000000u; }
-
 template <typename T, int DH, int MT, bool CHOSEN>
 __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
   constexpr bool WIDE = sizeof(T) == 4;
@@ -41,7 +37,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
   const int col = lane & 15, grp = lane >> 4;
   const int piece = blockIdx.x, nparts = a.nsplit;
   int split_i, b, j, block;
-  a.place(div_by(piece, nparts, a.nsplit_inv, split_i), b, j, block);
+  a.place_block(div_by(piece, nparts, a.nsplit_inv, split_i), b, j, block);
   const int row0 = block * 16 * MT;
   const int rows = a.n * a.G, count = image_count(a.n_rows, b, a.n), live = count * a.G, len = image_prior(a.kv_rows, b, a.P);
   const int last = min(row0 + 16 * MT, live) - 1;                // last live row of the block

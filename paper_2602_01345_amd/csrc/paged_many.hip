@@ -1,0 +1,257 @@
+// Attention over a cache in pages for many rows per key head (whole scales, chunks of prompts).
+//
+// As in fourbit_attention.hip everything is computed transposed, a lane owning one row (query):
+//   S^T = K Q^T    A operand = key rows from LDS, B operand = the row's channels, held in registers
+//   O^T += V^T P^T A operand = value rows from LDS, read transposed, B operand = the probabilities as they come out of the softmax
+// A workgroup is four waves of 32 rows.  Tiles of 64 keys go from the pages into LDS without passing through registers, each wave its
+// 16 keys (which lie in one page, wherever pages end) of K and of V, a line per row, the swizzle made by which chunk of its row a lane
+// asks for.  Two stages of LDS, two workgroups per CU (three with heads of 64), so that one wave's softmax runs next to another's
+// MFMAs; a wave asks for priority while it issues MFMAs.
+#include "paged.h"
+
+namespace {
+
+constexpr int kWaves = 4, kTile = 64, kRows = kPagedRows;
+
+__device__ __forceinline__ void wait_all() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);                      // vmcnt(0) lgkmcnt(0): own loads into LDS have landed, own reads are done
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int DH>
+__global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(PagedArgs<bf16_t> a) {
+  constexpr int ROWB = DH * 2;
+  constexpr int HALF = kTile * ROWB, STAGE = 2 * HALF;     // K rows, V rows
+  constexpr int KS = DH / 16;                  // MFMAs along dh for a score block
+  constexpr int DB = DH / 32;                  // 32-channel blocks of the output
+  constexpr int NL = 16 * ROWB / 1024, RPL = 1024 / ROWB;  // loads of a wave's 16 rows, rows per load
+  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const bool whole = (int)blockIdx.x < a.n_whole;
+  const int run = blockIdx.x - a.n_whole;
+  const int split_i = whole ? 0 : run % a.nsplit;
+  const int nparts = whole ? 1 : a.nsplit;
+  int b, j, block, unused;
+  a.place_block(whole ? blockIdx.x : a.n_whole + run / a.nsplit, b, j, block);
+  b = __builtin_amdgcn_readfirstlane(b);
+  const int row0 = block * kRows;
+  const int rows = a.n * a.G, count = image_count(a.n_rows, b, a.n), live = count * a.G, len = image_prior(a.kv_rows, b, a.P);
+  const int last = min(row0 + kRows, live) - 1;            // last live row of the block
+  const int seen_block = last < row0 ? 0 : visible_keys(a.causal, len, count, div_by(last, a.G, a.G_inv, unused));
+  const int ntiles = (seen_block + kTile - 1) / kTile;
+  const int per = (ntiles + nparts - 1) / nparts;
+  const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
+  // keys that the wave's first and last live row see
+  const int wrow = row0 + wave * 32, wlast = min(wrow + 31, live - 1);
+  const bool wave_live = wrow < live;
+  const int seen_least = wave_live ? visible_keys(a.causal, len, count, div_by(wrow, a.G, a.G_inv, unused)) : 0;
+  const int seen_most = wave_live ? visible_keys(a.causal, len, count, div_by(wlast, a.G, a.G_inv, unused)) : 0;
+
+  // this lane's part of a load of RPL rows: the chunk of its row that the swizzle puts where the lane's 16 bytes go
+  uint32_t part[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) part[i] = swizzled_source<ROWB>(i * RPL + lane / (64 / RPL), lane % (64 / RPL));
+  const int32_t* table = a.table + (int64_t)b * a.pitch;
+  const int last_page = max(seen_block - 1, 0) >> a.shift;
+  auto page_of = [&](int t) { return load_scalar(table + min((t * kTile + wave * 16) >> a.shift, last_page)); };
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((lptr_t)lds);
+  auto request = [&](int t, int page) {
+    const int key0 = t * kTile + wave * 16, ordinal = key0 >> a.shift;
+    const int there = min(max(len - (ordinal << a.shift), 0), 1 << a.shift);
+    const uint32_t at = (key0 & ((1 << a.shift) - 1)) * ROWB;
+    const u32x4 ks = page_words<bf16_t, DH>(a.keys, page, a.pages, a.hk, j, a.shift, there);
+    const u32x4 vs = page_words<bf16_t, DH>(a.values, page, a.pages, a.hk, j, a.shift, there);
+    const uint32_t to = lds0 + (t & 1) * STAGE + wave * 16 * ROWB;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) load_to_lds(ks, vs, to + i * 1024, to + HALF + i * 1024, part[i], at);
+  };
+
+  int page = t0 < t1 ? page_of(t0) : -1;
+  if (t0 < t1) {
+    request(t0, page);
+    page = page_of(t0 + 1);
+  }
+  const int row = wrow + col;
+  bf16x8 qf[KS];                                           // channels 16 t + 8 half .. + 7 of this lane's row
+  const int row_live = max(min(row, live - 1), 0);         // past the last live row its copies: what lies in padding is nobody's
+  {
+    const bf16_t* qp = a.query(b, j, row_live) + half * 8;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) qf[t] = *reinterpret_cast<const bf16x8*>(qp + t * 16);
+  }
+  const int seen = visible_keys(a.causal, len, count, div_by(row_live, a.G, a.G_inv, unused));
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  // probabilities are 2^(score - m_run); m_run is a reference, not necessarily the largest score (-inf: none yet)
+  float m_run = -INFINITY, l_run = 0.f;
+  // this lane's places in a tile: its key's chunks, and for transposed reads of values the 8-byte piece lane % 4 of 16 channels of
+  // key 4 half + (lane % 16) / 4 and of the one 8 behind it.  The swizzle repeats after 16 rows.
+  int ka[KS], va[DB][2];
+#pragma unroll
+  for (int t = 0; t < KS; ++t) ka[t] = swz<ROWB>(col, t * 2 + half);
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      va[d][x] = swz<ROWB>(4 * half + ((lane & 15) >> 2) + 8 * x, 4 * d + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+
+  for (int t = t0; t < t1; ++t) {
+    wait_all();                                            // tile t has landed, and nobody reads the other stage any more
+    if (t + 1 < t1) {
+      request(t + 1, page);
+      page = page_of(t + 2);
+    }
+    if (t * kTile >= seen_most) continue;                  // (a whole wave's) nothing that this wave's rows see
+    const char* sk = lds + (t & 1) * STAGE;
+    const char* sv = sk + HALF;
+    f32x16 s[2];
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        s[kb] = mfma32(*reinterpret_cast<const bf16x8*>(sk + kb * 32 * ROWB + ka[ks]), qf[ks], s[kb]);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    // ---- softmax: register r of block kb is key 64 t + 32 kb + 8 (r / 4) + 4 half + r % 4
+    bool careful = false;
+    if ((t + 1) * kTile > seen_least) {                    // keys that not all of the wave's rows see
+      const float dead = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t * kTile + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= seen) s[kb][r] = dead;
+      // a weight of 0 times a value that is no number would be one of NaN: such a tile takes its values key by key
+      uint32_t odd = 0u;
+#pragma unroll
+      for (int i = 0; i < ROWB / 16; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(sv + (i * 64 + lane) * 16);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) odd |= odd_pair(w[c]);
+      }
+      careful = __any(odd != 0u);
+    }
+    float e[2][16], psum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -m_run));
+        psum += e[kb][r];
+      }
+    if (__any(!(psum <= kBig))) {
+      // some score lies far above the reference, or there is none yet: it moves to the largest score, and the sums with it
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, s[kb][r] * a.scale_log2);
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
+      const float m_new = fmaxf(m_run, tmax);
+      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      m_run = m_new;
+      const float ref = m_new == -INFINITY ? 0.f : m_new;                 // nothing but scores of -inf so far
+      psum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -ref));
+          psum += e[kb][r];
+        }
+    }
+    l_run += psum;
+    __builtin_amdgcn_s_setprio(1);
+    // ---- O^T += V^T P^T, 16 keys per MFMA: the lane's keys 16 u + 4 half .. + 3 and 8 behind them
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      bf16x8 pf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pf[i] = (bf16_t)e[u >> 1][(u & 1) * 8 + i];
+      const char* at = sv + u * 16 * ROWB;
+      if (!careful) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = mfma32(join(read_transposed(at + va[d][0]), read_transposed(at + va[d][1])), pf, o[d]);
+      } else {
+        // one key at a time: element i of the lanes of half x.  Rows whose weight for it is 0 take nothing of it.
+#pragma unroll 1
+        for (int ix = 0; ix < 16; ++ix) {
+          const int i = ix >> 1, x = ix & 1;
+          const uint32_t bits = half == x ? (i & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
+          u32x4 only;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) only[c] = c == i >> 1 ? bits : 0u;
+          const u32x4 w = __builtin_bit_cast(u32x4, pf) & only;
+          const uint32_t weight = __shfl(w[0] | w[1] | w[2] | w[3], col + 32 * x, NOVA_WAVE);
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            f32x16 one;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) one[r] = 0.f;
+            const bf16x8 vf = join(read_transposed(at + va[d][0]), read_transposed(at + va[d][1]));
+            one = mfma32(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, vf) & only), __builtin_bit_cast(bf16x8, w), one);
+            if (weight)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) o[d][r] += one[r];
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+  }
+
+  if (row >= rows) return;
+  const float l = l_run + __shfl_xor(l_run, 32, NOVA_WAVE);
+  if (nparts == 1) {
+    const bool some = row < live && seen > 0;
+    const int64_t to = a.out_row(b, j, row);
+    const float inv = some ? 1.0f / l : 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (some) v = f32x4{o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]};
+        store_four(a.out + to * DH + d * 32 + r4 * 8 + half * 4, v, inv);
+      }
+    if (a.lse && half == 0)
+      a.lse[to] = some ? ((m_run == -INFINITY ? 0.f : m_run) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  } else {
+    const int64_t to = (int64_t)run * kRows + (row - row0);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(a.part_o + to * DH + d * 32 + r4 * 8 + half * 4) =
+            f32x4{o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]};
+    if (half == 0) {
+      a.part_ml[to * 2] = m_run;
+      a.part_ml[to * 2 + 1] = l;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_many(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a) {
+  if (dh == 64) many_kernel<64><<<grid, kWaves * 64, 0, st>>>(a);
+  else many_kernel<128><<<grid, kWaves * 64, 0, st>>>(a);
+  return hipGetLastError();
+}
