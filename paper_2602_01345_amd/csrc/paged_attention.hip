@@ -25,16 +25,15 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
   const int s_row = div_by(there ? row : 0, a.G, a.G_inv, g_unused);
   bool some = there && s_row < count && visible_keys(a.causal, len, count, s_row) > 0;
   const int64_t p0 = (int64_t)ci * a.nsplit * block_rows + rr;
-  float m = -INFINITY, l = 0.f;
+  float m = kNone, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int s = sl; some && s < a.nsplit; s += SL) {
     const int64_t p = p0 + (int64_t)s * block_rows;
     const float ms = a.part_ml[p * 2], ls = a.part_ml[p * 2 + 1];
     if (ls == 0.f) continue;
     const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + p * DH + c4 * 4);
-    // a run without a finite score has reference -inf and a sum of NaN: it is added as it is
     const float mn = fmaxf(m, ms);
-    const float w0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn), w1 = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - mn);
+    const float w0 = __builtin_amdgcn_exp2f(m - mn), w1 = __builtin_amdgcn_exp2f(ms - mn);
     l = l * w0 + ls * w1;
     acc = acc * w0 + o * w1;
     m = mn;
@@ -53,7 +52,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < SL; ++s) {
-      const float w = part_m[g + s] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(part_m[g + s] - m);
+      const float w = __builtin_amdgcn_exp2f(part_m[g + s] - m);
       l = fmaf(w, part_l[g + s], l);
       acc += w * part_o[tid + s * C4];
     }
@@ -62,7 +61,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
   if (a.chosen && l == 0.f) some = false;                        // the query has chosen no page that it sees
   const int64_t to = a.out_row(b, j, row);
   store_four(a.out + to * DH + c4 * 4, some ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, some ? 1.0f / l : 0.f);
-  if (a.lse && c4 == 0) a.lse[to] = some ? ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  if (a.lse && c4 == 0) a.lse[to] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // How a call is divided: mt > 0: blocks of 16 mt rows (paged_few.hip), else blocks of kPagedRows (paged_many.hip); items below n_whole
@@ -77,20 +76,30 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   const int G = heads / c.kv_heads, rows = n * G;
   const bool wide = c.dtype == NOVA_F32;
   Plan p = {};
-  p.mt = rows <= 16 ? 1 : rows <= 32 || take > 0 || wide ? 2 : 0;
+  const int pages = (kv_len + c.page_rows - 1) / c.page_rows;
+  // pages that the queries of a block of so many rows may have chosen
+  auto listed = [&](int block_rows) {
+    return take > 0 ? (int)std::min<int64_t>(pages, (int64_t)std::min({block_rows, (block_rows - 1) / G + 2, n}) * take) : 0;
+  };
+  p.mt = rows <= 16 ? 1 : rows <= 32 || wide ? 2 : 0;
   const int64_t blocks32 = (int64_t)B * c.kv_heads * ((rows + 31) / 32);
-  if (p.mt == 0 && blocks32 <= 2 * kCus && kv_len <= 2048) p.mt = 2;
+  if (p.mt == 0 && take == 0 && blocks32 <= 2 * kCus && kv_len <= 2048) p.mt = 2;
+  // Chosen pages: blocks of 128 rows where their queries' lists together are as long as the image has pages, so that they share, and
+  // where the list leaves room for a second workgroup in the LDS (us in blocks of 128 / of 32; 32 heads of 128 on 8, 1024 queries, of
+  // 512 pages of 64 rows 128 chosen 566 / 850, 32 350 / 359, 4 79 / 60; 128 queries, 32 chosen 73 / 100; of 512 pages of 16 rows 64
+  // chosen 140 / 163; heads of 64, of 256 pages of 32 rows 20 chosen 95 / 78).
+  if (p.mt == 0 && take > 0)
+    p.mt = c.dh == 128 && (int64_t)std::min((kPagedRows - 1) / G + 2, n) * take >= pages &&
+           chosen_bytes(pages, listed(kPagedRows), kPagedRows / 32) <= 16384 ? 0 : 2;
   p.block_rows = p.mt ? 16 * p.mt : kPagedRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;
   p.items = B * c.kv_heads * p.blocks;
   p.n_whole = p.items;
   p.nsplit = 1;
+  p.listed = listed(p.block_rows);
   if (p.mt) {
     const int tile = wide ? paged_few_tile<float>(c.dh) : paged_few_tile<bf16_t>(c.dh);
     // most keys a block goes over: all, or what its queries may have chosen
-    const int pages = (kv_len + c.page_rows - 1) / c.page_rows;
-    const int queries = std::min({p.block_rows, (p.block_rows - 1) / G + 2, n});
-    p.listed = take > 0 ? (int)std::min<int64_t>(pages, (int64_t)queries * take) : 0;
     const int64_t keys = take > 0 ? (int64_t)p.listed * c.page_rows : kv_len;
     const int ntiles = (int)((keys + tile - 1) / tile);
     p.run_tiles = ntiles;
@@ -102,7 +111,7 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
     }
     return p;
   }
-  const int ntiles = (kv_len + 63) / 64, slots = 2 * kCus, rest = p.items % slots;
+  const int ntiles = (int)(((take > 0 ? (int64_t)p.listed * c.page_rows : kv_len) + 63) / 64), slots = 2 * kCus, rest = p.items % slots;
   // Images with lengths of their own: the longest first, so that short ones fill up the end; from two rounds of items on that is
   // enough and none is cut.
   p.ranked = ragged && p.items > slots && B > 1 && B <= kRanked ? B : 0;
@@ -139,6 +148,7 @@ hipError_t attend(hipStream_t st, const PagedCall& call) {
   a.chosen = call.chosen; a.take = call.take;
   a.most_pages = (call.kv_len + c.page_rows - 1) / c.page_rows;
   a.most_listed = p.listed;
+  a.take_inv = div_inv(call.take);
   a.blocks = p.blocks; a.items = p.items; a.dealt = p.items / (8 * p.blocks) * 8 * p.blocks;
   a.blocks_inv = div_inv(p.blocks); a.hk_inv = div_inv(c.kv_heads); a.G_inv = div_inv(a.G); a.nsplit_inv = div_inv(p.nsplit);
   a.n_whole = p.n_whole; a.nsplit = p.nsplit; a.run_tiles = p.run_tiles; a.ranked = p.ranked;

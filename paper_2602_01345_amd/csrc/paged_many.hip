@@ -7,6 +7,12 @@
 // 16 keys (which lie in one page, wherever pages end) of K and of V, a line per row, the swizzle made by which chunk of its row a lane
 // asks for.  Two stages of LDS, two workgroups per CU (three with heads of 64), so that one wave's softmax runs next to another's
 // MFMAs; a wave asks for priority while it issues MFMAs.
+// Chosen pages: the block goes over the union of its queries' lists, its waves over those tiles that one of their own queries has
+// chosen, each query's rows masked where it has not.
+// A weight of 0 times a value that is no number is NaN, so what a row does not see could show in its result.  A workgroup whose sums
+// end as anything but finite numbers goes over its tiles again, and takes those with such values in them key by key.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace {
@@ -20,7 +26,7 @@ __device__ __forceinline__ void wait_all() {
   asm volatile("" ::: "memory");
 }
 
-template <int DH>
+template <int DH, bool CHOSEN>
 __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(PagedArgs<bf16_t> a) {
   constexpr int ROWB = DH * 2;
   constexpr int HALF = kTile * ROWB, STAGE = 2 * HALF;     // K rows, V rows
@@ -28,6 +34,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   constexpr int DB = DH / 32;                  // 32-channel blocks of the output
   constexpr int NL = 16 * ROWB / 1024, RPL = 1024 / ROWB;  // loads of a wave's 16 rows, rows per load
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+  __shared__ uint32_t odd_waves[kWaves];
+  extern __shared__ uint32_t lists[];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -43,38 +51,74 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   const int rows = a.n * a.G, count = image_count(a.n_rows, b, a.n), live = count * a.G, len = image_prior(a.kv_rows, b, a.P);
   const int last = min(row0 + kRows, live) - 1;            // last live row of the block
   const int seen_block = last < row0 ? 0 : visible_keys(a.causal, len, count, div_by(last, a.G, a.G_inv, unused));
-  const int ntiles = (seen_block + kTile - 1) / kTile;
+  const int gshift = a.shift - 4, gmask = (1 << gshift) - 1;     // groups of 16 keys of a page
+  ChosenPages list = {};
+  int groups = (seen_block + 15) / 16;
+  if constexpr (CHOSEN) {
+    const int s_first = div_by(row0, a.G, a.G_inv, unused), s_last = last < row0 ? s_first : div_by(last, a.G, a.G_inv, unused);
+    list = list_chosen<bf16_t, kWaves * 64, kWaves>(a, lists, b, j, row0, s_first, s_last, (seen_block + (1 << a.shift) - 1) >> a.shift);
+    groups = list.count << gshift;
+  }
+  const int ntiles = (groups + 3) / 4;
   const int per = (ntiles + nparts - 1) / nparts;
   const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
   // keys that the wave's first and last live row see
   const int wrow = row0 + wave * 32, wlast = min(wrow + 31, live - 1);
   const bool wave_live = wrow < live;
-  const int seen_least = wave_live ? visible_keys(a.causal, len, count, div_by(wrow, a.G, a.G_inv, unused)) : 0;
-  const int seen_most = wave_live ? visible_keys(a.causal, len, count, div_by(wlast, a.G, a.G_inv, unused)) : 0;
+  const int s_wave = div_by(min(wrow, max(live - 1, 0)), a.G, a.G_inv, unused), s_wlast = div_by(max(wlast, 0), a.G, a.G_inv, unused);
+  const int seen_least = wave_live ? visible_keys(a.causal, len, count, s_wave) : 0;
+  const int seen_most = wave_live ? visible_keys(a.causal, len, count, s_wlast) : 0;
+  const uint32_t all = 0xFFFFFFFFu >> max(31 - (s_wlast - s_wave), 0);       // a bit for each of the wave's queries
 
   // this lane's part of a load of RPL rows: the chunk of its row that the swizzle puts where the lane's 16 bytes go
   uint32_t part[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) part[i] = swizzled_source<ROWB>(i * RPL + lane / (64 / RPL), lane % (64 / RPL));
   const int32_t* table = a.table + (int64_t)b * a.pitch;
-  const int last_page = max(seen_block - 1, 0) >> a.shift;
-  auto page_of = [&](int t) { return load_scalar(table + min((t * kTile + wave * 16) >> a.shift, last_page)); };
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((lptr_t)lds);
-  auto request = [&](int t, int page) {
-    const int key0 = t * kTile + wave * 16, ordinal = key0 >> a.shift;
-    const int there = min(max(len - (ordinal << a.shift), 0), 1 << a.shift);
-    const uint32_t at = (key0 & ((1 << a.shift) - 1)) * ROWB;
+  // The wave's 16 keys of a tile lie in one page.  Its place in the pool: from the list, or from 64 tiles' places that the lanes hold.
+  struct Sixteen { int ordinal, page; };
+  int held = 0, held_first = 0;
+  auto hold = [&](int t) {
+    held_first = t;
+    held = groups > 0 ? table[min((t + lane) * 4 + wave, groups - 1) >> gshift] : -1;
+  };
+  auto look_up = [&](int t) {
+    const int u = min(t * 4 + wave, max(groups, 1) - 1) >> gshift;
+    if constexpr (CHOSEN) {
+      if (groups == 0) return Sixteen{0, -1};
+      return Sixteen{(int)list.listed[u], list.page[u]};
+    } else {
+      if (t - held_first >= 64) hold(t);
+      return Sixteen{u, __builtin_amdgcn_readlane(held, t - held_first)};
+    }
+  };
+  auto request = [&](int t, const Sixteen& p) {
+    const int x = t * 4 + wave, page = __builtin_amdgcn_readfirstlane(p.page), ordinal = __builtin_amdgcn_readfirstlane(p.ordinal);
+    const int there = x < groups ? min(max(len - (ordinal << a.shift), 0), 1 << a.shift) : 0;
+    const uint32_t at = (x & gmask) * 16 * ROWB;
     const u32x4 ks = page_words<bf16_t, DH>(a.keys, page, a.pages, a.hk, j, a.shift, there);
     const u32x4 vs = page_words<bf16_t, DH>(a.values, page, a.pages, a.hk, j, a.shift, there);
     const uint32_t to = lds0 + (t & 1) * STAGE + wave * 16 * ROWB;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) load_to_lds(ks, vs, to + i * 1024, to + HALF + i * 1024, part[i], at);
+    load_to_lds(ks, to, part, at);
+    load_to_lds(vs, to + HALF, part, at);
   };
 
-  int page = t0 < t1 ? page_of(t0) : -1;
+  // lanes i, i + 4 ..: first key of a tile's i-th 16 and which of the wave's queries have chosen its page
+  struct Four { int key0; uint32_t who; };
+  auto four = [&](int t) {
+    const int x = t * 4 + (lane & 3), u = min(x, max(groups, 1) - 1) >> gshift;
+    if constexpr (!CHOSEN) return Four{x * 16, all};
+    if (groups == 0) return Four{0, 0u};
+    return Four{(list.listed[u] << a.shift) + (x & gmask) * 16, x < groups ? list.member[u * kWaves + wave] : 0u};
+  };
+
+  if constexpr (!CHOSEN) hold(t0);
+  Sixteen next = look_up(t0);
+  Four four_next = four(t0);
   if (t0 < t1) {
-    request(t0, page);
-    page = page_of(t0 + 1);
+    request(t0, next);
+    next = look_up(t0 + 1);
   }
   const int row = wrow + col;
   bf16x8 qf[KS];                                           // channels 16 t + 8 half .. + 7 of this lane's row
@@ -84,14 +128,9 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
 #pragma unroll
     for (int t = 0; t < KS; ++t) qf[t] = *reinterpret_cast<const bf16x8*>(qp + t * 16);
   }
-  const int seen = visible_keys(a.causal, len, count, div_by(row_live, a.G, a.G_inv, unused));
-  f32x16 o[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-  // probabilities are 2^(score - m_run); m_run is a reference, not necessarily the largest score (-inf: none yet)
-  float m_run = -INFINITY, l_run = 0.f;
+  const int s_row = div_by(row_live, a.G, a.G_inv, unused);
+  const int seen = visible_keys(a.causal, len, count, s_row);
+  const uint32_t bit = 1u << ((s_row - s_wave) & 31);
   // this lane's places in a tile: its key's chunks, and for transposed reads of values the 8-byte piece lane % 4 of 16 channels of
   // key 4 half + (lane % 16) / 4 and of the one 8 behind it.  The swizzle repeats after 16 rows.
   int ka[KS], va[DB][2];
@@ -103,13 +142,37 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
     for (int x = 0; x < 2; ++x)
       va[d][x] = swz<ROWB>(4 * half + ((lane & 15) >> 2) + 8 * x, 4 * d + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
 
+  f32x16 o[DB];
+  // probabilities are 2^(score - m_run); m_run is a reference, not necessarily the largest score
+  float m_run, l_run;
+  auto clear = [&] {
+    m_run = kNone;
+    l_run = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  };
+  clear();
+
+  auto over_tiles = [&](auto strict_tag) {
+  constexpr bool STRICT = decltype(strict_tag)::value;     // the second time
   for (int t = t0; t < t1; ++t) {
     wait_all();                                            // tile t has landed, and nobody reads the other stage any more
     if (t + 1 < t1) {
-      request(t + 1, page);
-      page = page_of(t + 2);
+      request(t + 1, next);
+      next = look_up(t + 2);
     }
-    if (t * kTile >= seen_most) continue;                  // (a whole wave's) nothing that this wave's rows see
+    int key0[4];
+    uint32_t who[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      key0[i] = CHOSEN ? __builtin_amdgcn_readlane(four_next.key0, i) : t * kTile + i * 16;
+      who[i] = CHOSEN ? (uint32_t)__builtin_amdgcn_readlane((int)four_next.who, i) : all;
+    }
+    four_next = four(t + 1);
+    const bool mine = key0[0] < seen_most && (!CHOSEN || (who[0] | who[1] | who[2] | who[3]) != 0u);
+    if (mine) {                                            // (a whole wave's) something that its rows see
     const char* sk = lds + (t & 1) * STAGE;
     const char* sv = sk + HALF;
     f32x16 s[2];
@@ -125,22 +188,25 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
     __builtin_amdgcn_s_setprio(0);
     // ---- softmax: register r of block kb is key 64 t + 32 kb + 8 (r / 4) + 4 half + r % 4
     bool careful = false;
-    if ((t + 1) * kTile > seen_least) {                    // keys that not all of the wave's rows see
+    if (key0[3] + 16 > seen_least || (CHOSEN && (who[0] & who[1] & who[2] & who[3]) != all)) {     // keys that not all of its rows see
       const float dead = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (t * kTile + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= seen) s[kb][r] = dead;
-      // a weight of 0 times a value that is no number would be one of NaN: such a tile takes its values key by key
-      uint32_t odd = 0u;
+        for (int r = 0; r < 16; ++r) {
+          const int g = kb * 2 + (r >> 3);
+          if (key0[g] + 8 * ((r >> 2) & 1) + 4 * half + (r & 3) >= seen || (CHOSEN && !(who[g] & bit))) s[kb][r] = dead;
+        }
+      if constexpr (STRICT) {
+        uint32_t odd = 0u;
+#pragma unroll 1
+        for (int i = 0; i < ROWB / 16; ++i) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(sv + (i * 64 + lane) * 16);
 #pragma unroll
-      for (int i = 0; i < ROWB / 16; ++i) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(sv + (i * 64 + lane) * 16);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) odd |= odd_pair(w[c]);
+          for (int c = 0; c < 4; ++c) odd |= odd_pair(w[c]);
+        }
+        careful = __any(odd != 0u);
       }
-      careful = __any(odd != 0u);
     }
     float e[2][16], psum = 0.f;
 #pragma unroll
@@ -151,7 +217,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
         psum += e[kb][r];
       }
     if (__any(!(psum <= kBig))) {
-      // some score lies far above the reference, or there is none yet: it moves to the largest score, and the sums with it
+      // some score lies far above the reference, as any does above the first one: it moves to the largest score, and the sums with it
       float tmax = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -159,20 +225,19 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
         for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, s[kb][r] * a.scale_log2);
       tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
       const float m_new = fmaxf(m_run, tmax);
-      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
       m_run = m_new;
-      const float ref = m_new == -INFINITY ? 0.f : m_new;                 // nothing but scores of -inf so far
       psum = 0.f;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -ref));
+          e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -m_new));
           psum += e[kb][r];
         }
     }
@@ -185,7 +250,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
 #pragma unroll
       for (int i = 0; i < 8; ++i) pf[i] = (bf16_t)e[u >> 1][(u & 1) * 8 + i];
       const char* at = sv + u * 16 * ROWB;
-      if (!careful) {
+      if (!STRICT || !careful) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = mfma32(join(read_transposed(at + va[d][0]), read_transposed(at + va[d][1])), pf, o[d]);
       } else {
@@ -215,12 +280,32 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
       }
     }
     __builtin_amdgcn_s_setprio(0);
+    }
+  }
+  };
+  over_tiles(std::false_type{});
+  if (t0 < t1) {
+    float sum = 0.f;                                       // 0, or NaN where some number is none
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum = fmaf(o[d][r], 0.f, sum);
+    odd_waves[wave] = __any(sum != 0.f);
+    wait_all();
+    if (odd_waves[0] | odd_waves[1] | odd_waves[2] | odd_waves[3]) {
+      clear();
+      if constexpr (!CHOSEN) hold(t0);
+      request(t0, look_up(t0));
+      next = look_up(t0 + 1);
+      four_next = four(t0);
+      over_tiles(std::true_type{});
+    }
   }
 
   if (row >= rows) return;
   const float l = l_run + __shfl_xor(l_run, 32, NOVA_WAVE);
   if (nparts == 1) {
-    const bool some = row < live && seen > 0;
+    const bool some = row < live && seen > 0 && !(CHOSEN && l == 0.f);
     const int64_t to = a.out_row(b, j, row);
     const float inv = some ? 1.0f / l : 0.f;
 #pragma unroll
@@ -232,7 +317,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
         store_four(a.out + to * DH + d * 32 + r4 * 8 + half * 4, v, inv);
       }
     if (a.lse && half == 0)
-      a.lse[to] = some ? ((m_run == -INFINITY ? 0.f : m_run) + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+      a.lse[to] = some ? (m_run + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
   } else {
     const int64_t to = (int64_t)run * kRows + (row - row0);
 #pragma unroll
@@ -251,7 +336,10 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
 }  // namespace
 
 hipError_t launch_paged_many(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a) {
-  if (dh == 64) many_kernel<64><<<grid, kWaves * 64, 0, st>>>(a);
-  else many_kernel<128><<<grid, kWaves * 64, 0, st>>>(a);
+  const size_t lists = a.chosen ? (chosen_bytes(a.most_pages, a.most_listed, kWaves) + 15) / 16 * 16 : 0;
+#define GO(DH, CHOSEN) many_kernel<DH, CHOSEN><<<grid, kWaves * 64, lists, st>>>(a)
+  if (dh == 64) { if (a.chosen) GO(64, true); else GO(64, false); }
+  else { if (a.chosen) GO(128, true); else GO(128, false); }
+#undef GO
   return hipGetLastError();
 }
