@@ -15,6 +15,8 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kHeads = 4;                // heads whose queries are held in registers at a time
+constexpr int kAhead = 2;                // groups of 16 pages whose means a wave asks for at a time
+constexpr int kMostKeys = 32;            // keys a lane holds while the k-th largest is looked for
 constexpr uint32_t kTaken = 0xFFFFFFFFu; // key of a page that is taken whatever its score; 0: one that the query does not see
 
 struct SelectArgs {
@@ -25,6 +27,7 @@ struct SelectArgs {
   int pitch, pages, hk, G, shift, n, P, causal, first, recent, k, queries, row;     // queries per workgroup, keys of one in LDS
   const int32_t *n_rows, *kv_rows;
   int32_t* chosen;
+  int sharing;                           // waves that choose for one query together
 };
 
 __device__ __forceinline__ uint32_t score_key(float s) {
@@ -34,10 +37,12 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-template <typename T, int DH>
+// R: keys a lane holds
+template <typename T, int DH, int R>
 __global__ __launch_bounds__(kWaves * 64, 2) void select_kernel(SelectArgs a) {
   constexpr int KC = DH / 32;                  // MFMAs per score: chunk 4 e + grp of eight channels
   extern __shared__ uint32_t keys[];           // [queries][row]
+  __shared__ int counts[2][kWaves], equals[kWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
@@ -50,23 +55,46 @@ __global__ __launch_bounds__(kWaves * 64, 2) void select_kernel(SelectArgs a) {
   const int seen = (visible_keys(a.causal, len, count, mine) + up) >> a.shift;  // pages this lane's query sees
 
   if (npages > 0) {
+    const int32_t* table = a.table + (int64_t)b * a.pitch;
+    // means of kAhead groups of pages: places in the pool first, asked for one round ahead
+    int page[kAhead];
+    auto look_up = [&](int x0) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) page[i] = table[min((x0 + i * kWaves) * 16 + col, npages - 1)];
+    };
+    look_up(wave);
     // the query's scale: one for all heads that share the key head
     const T* q = static_cast<const T*>(a.q) + b * a.q_sb + mine * a.q_sr + (int64_t)j * a.G * a.q_sh + grp * 8;
     float top = 0.f;
     bool odd = false;
-    for (int g = 0; g < a.G; ++g)
+    bf16x8 qf[kHeads][KC];                     // queries as they are (bf16), then rounded
+    auto load_heads = [&](int g0, auto use) {
 #pragma unroll
-      for (int e = 0; e < KC; ++e)
+      for (int g = 0; g < kHeads; ++g)
 #pragma unroll
-        for (int c = 0; c < 8; c += Vec16<T>::N) {
-          Vec16<T> v;
-          v.load(q + g * a.q_sh + e * 32 + c);
+        for (int e = 0; e < KC; ++e) {
+          const T* p = q + min(g0 + g, a.G - 1) * a.q_sh + e * 32;
+          if constexpr (sizeof(T) == 2) {
+            qf[g][e] = *reinterpret_cast<const bf16x8*>(p);
+          } else {
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll
-          for (int i = 0; i < Vec16<T>::N; ++i) {
-            top = fmaxf(top, fabsf(v.get(i)));
-            odd |= !(fabsf(v.get(i)) < INFINITY);
+            for (int i = 0; i < 8; ++i) use(g, e, i, i < 4 ? lo[i & 3] : hi[i & 3]);
           }
         }
+      if constexpr (sizeof(T) == 2)
+#pragma unroll
+        for (int g = 0; g < kHeads; ++g)
+#pragma unroll
+          for (int e = 0; e < KC; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) use(g, e, i, (float)qf[g][e][i]);
+    };
+    for (int g0 = 0; g0 < a.G; g0 += kHeads)
+      load_heads(g0, [&](int, int, int, float v) {
+        top = fmaxf(top, fabsf(v));
+        odd |= !(fabsf(v) < INFINITY);
+      });
     top = fmaxf(top, __shfl_xor(top, 16, NOVA_WAVE));
     top = fmaxf(top, __shfl_xor(top, 32, NOVA_WAVE));
     odd |= __shfl_xor((int)odd, 16, NOVA_WAVE);
@@ -78,31 +106,38 @@ __global__ __launch_bounds__(kWaves * 64, 2) void select_kernel(SelectArgs a) {
     const float unit = odd ? 0.f : __uint_as_float((uint32_t)(127 - e2) << 23);
 
     for (int g0 = 0; g0 < a.G; g0 += kHeads) {
-      bf16x8 qf[kHeads][KC];
+      auto rounded = [&](int g, int e, int i, float v) {
+        qf[g][e][i] = (bf16_t)(odd ? 0.f : fminf(fmaxf(rintf(v * unit), -127.f), 127.f));
+      };
+      if (sizeof(T) == 4 || a.G > kHeads) {
+        load_heads(g0, rounded);
+      } else {
 #pragma unroll
-      for (int g = 0; g < kHeads; ++g)
+        for (int g = 0; g < kHeads; ++g)
 #pragma unroll
-        for (int e = 0; e < KC; ++e)
+          for (int e = 0; e < KC; ++e)
 #pragma unroll
-          for (int c = 0; c < 8; c += Vec16<T>::N) {
-            Vec16<T> v;
-            v.load(q + min(g0 + g, a.G - 1) * a.q_sh + e * 32 + c);
+            for (int i = 0; i < 8; ++i) rounded(g, e, i, (float)qf[g][e][i]);
+      }
+      if (g0 > 0) look_up(wave);
+      for (int x0 = wave; x0 * 16 < npages; x0 += kAhead * kWaves) {
+        bf16x8 means[kAhead][KC];
 #pragma unroll
-            for (int i = 0; i < Vec16<T>::N; ++i) {
-              const float w = odd ? 0.f : fminf(fmaxf(rintf(v.get(i) * unit), -127.f), 127.f);
-              qf[g][e][c + i] = (bf16_t)w;
-            }
+        for (int i = 0; i < kAhead; ++i) {
+          const bool there = (unsigned)page[i] < (unsigned)a.pages;
+          const bf16_t* mp = a.means + ((int64_t)(there ? page[i] : 0) * a.hk + j) * DH + grp * 8;
+#pragma unroll
+          for (int e = 0; e < KC; ++e) {
+            means[i][e] = bf16x8{};
+            if (there) means[i][e] = *reinterpret_cast<const bf16x8*>(mp + e * 32);
           }
-      for (int x = wave; x * 16 < npages; x += kWaves) {
-        const int ordinal = min(x * 16 + col, npages - 1), page = a.table[(int64_t)b * a.pitch + ordinal];
-        const bool there = (unsigned)page < (unsigned)a.pages;
-        bf16x8 m[KC];
-        const bf16_t* mp = a.means + ((int64_t)(there ? page : 0) * a.hk + j) * DH + grp * 8;
-#pragma unroll
-        for (int e = 0; e < KC; ++e) {
-          m[e] = *reinterpret_cast<const bf16x8*>(mp + e * 32);
-          if (!there) m[e] = bf16x8{};
         }
+        look_up(x0 + kAhead * kWaves);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+        const int x = x0 + i * kWaves;
+        if (x * 16 >= npages) break;
+        const auto& m = means[i];
         f32x4 best;
 #pragma unroll
         for (int g = 0; g < kHeads; ++g) {
@@ -120,55 +155,92 @@ __global__ __launch_bounds__(kWaves * 64, 2) void select_kernel(SelectArgs a) {
         const u32x4 before = g0 > 0 && keep ? *reinterpret_cast<const u32x4*>(at) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int i = x * 16 + grp * 4 + r;
-          const bool taken = i < a.first || i >= seen - a.recent;
+          const int at_page = x * 16 + grp * 4 + r;
+          const bool taken = at_page < a.first || at_page >= seen - a.recent;
           const uint32_t w = max(score_key(best[r]), before[r]);
-          key[r] = i >= seen ? 0u : taken ? kTaken : w;
+          key[r] = at_page >= seen ? 0u : taken ? kTaken : w;
         }
         if (keep) *reinterpret_cast<u32x4*>(at) = key;
+        }
       }
     }
   }
   __syncthreads();
 
-  for (int i = wave; i < a.queries; i += kWaves) {
-    const int s = s0 + i;
-    if (s >= a.n) break;
-    int32_t* to = a.chosen + (((int64_t)b * a.n + s) * a.hk + j) * a.k;
-    const int sees = s < count ? (visible_keys(a.causal, len, count, s) + up) >> a.shift : 0;
-    const int take = min(a.k, sees);
-    const uint32_t* key = keys + i * a.row;
-    // pages with a key of at least t
+  // `sharing` waves per query, each with R keys per lane running.  The k-th largest key bit by bit from the top: the largest t of
+  // which at least `take` keys are none the smaller, or, earlier, a t of which exactly `take` are.
+  const int part = wave % a.sharing;
+  const uint64_t below = (1ull << lane) - 1;
+  for (int i0 = 0; i0 < a.queries; i0 += kWaves / a.sharing) {
+    const int i = i0 + wave / a.sharing, s = s0 + i;
+    const bool live = i < a.queries && s < a.n;
+    const int sees = live && s < count ? (visible_keys(a.causal, len, count, s) + up) >> a.shift : 0;
+    const int take = min(a.k, sees), x0 = part * R * 64 + lane;
+    uint32_t w[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[r] = x0 + r * 64 < sees ? keys[i * a.row + x0 + r * 64] : 0u;
     auto at_least = [&](uint32_t t) {
       int c = 0;
-      for (int x = lane; x < (sees + 63) / 64 * 64; x += 64) c += __popcll(__ballot(x < sees && key[x] >= t));
+#pragma unroll
+      for (int r = 0; r < R; ++r) c += (int)__popcll(__ballot(w[r] >= t));
       return c;
     };
     uint32_t t = 0u;
     int over = sees;                                             // pages with a key of at least t
-    if (take < sees)
-      for (int bit = 31; bit >= 0 && over != take; --bit) {
+    if (a.sharing == 1) {
+      if (take < sees)
+        for (int bit = 31; bit >= 0 && over != take; --bit) {
+          const uint32_t higher = t | 1u << bit;
+          const int c = at_least(higher);
+          if (c >= take) { t = higher; over = c; }
+        }
+    } else {
+      for (int bit = 31; bit >= 0; --bit) {                      // all waves alike: they meet at a barrier for every bit
         const uint32_t higher = t | 1u << bit;
-        const int c = at_least(higher);
-        if (c >= take) { t = higher; over = c; }
+        const int own = at_least(higher);                        // of all lanes of the wave
+        if (lane == 0) counts[bit & 1][wave] = own;
+        __syncthreads();
+        int c = 0;
+        for (int p = 0; p < a.sharing; ++p) c += counts[bit & 1][wave - part + p];
+        if (take < sees && over != take && c >= take) { t = higher; over = c; }
       }
-    // t is the take-th largest key, or `take` pages have one of at least t
-    int equal = 0;                                               // pages of key t that are taken
-    if (over > take) equal = take - (t == kTaken ? 0 : at_least(t + 1));
-    else equal = over;
-    int at = 0;
-    for (int x0 = 0; x0 < sees; x0 += 64) {
-      const int x = x0 + lane;
-      const uint32_t w = x < sees ? key[x] : 0u;
-      const bool above = x < sees && w > t, same = x < sees && w == t;
-      const uint64_t sames = __ballot(same), below = (1ull << lane) - 1;
-      const bool mine_too = above || (same && (int)__popcll(sames & below) < equal);
-      const uint64_t all = __ballot(mine_too);
-      if (mine_too) to[at + (int)__popcll(all & below)] = x;
-      at += (int)__popcll(all);
-      equal -= min(equal, (int)__popcll(sames));
     }
-    for (int x = at + lane; x < a.k; x += 64) to[x] = -1;
+    t = max(t, 1u);                                              // 0: every page that is seen
+    // pages above t, of those that equal it the first ones
+    int above = 0, equal = 0, in_front = 0, equal_in_front = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      above += (int)__popcll(__ballot(w[r] > t));
+      equal += (int)__popcll(__ballot(w[r] == t));
+    }
+    int more = take - above;                                     // pages of key t that are taken
+    if (a.sharing > 1) {
+      __syncthreads();
+      if (lane == 0) { counts[0][wave] = above; equals[wave] = equal; }
+      __syncthreads();
+      int all = 0;
+      for (int p = 0; p < a.sharing; ++p) {
+        all += counts[0][wave - part + p];
+        if (p < part) { in_front += counts[0][wave - part + p]; equal_in_front += equals[wave - part + p]; }
+      }
+      more = take - all;
+      __syncthreads();
+    }
+    if (!live) continue;
+    int32_t* to = a.chosen + (((int64_t)b * a.n + s) * a.hk + j) * a.k;
+    int at = in_front + min(equal_in_front, more), left = max(more - equal_in_front, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint64_t same = __ballot(w[r] == t);
+      const bool taken = w[r] > t || (w[r] == t && (int)__popcll(same & below) < left);
+      const uint64_t all = __ballot(taken);
+      const int place = at + (int)__popcll(all & below);
+      if (taken && place < take) to[place] = x0 + r * 64;        // `take` pages are
+      at += (int)__popcll(all);
+      left = max(left - (int)__popcll(same), 0);
+    }
+    if (part == 0)
+      for (int x = take + lane; x < a.k; x += 64) to[x] = -1;
   }
 }
 
@@ -187,9 +259,16 @@ hipError_t launch_paged_select(hipStream_t st, const PagedSelect& s) {
   // as many queries as there are, and have room in a part of a CU's LDS
   a.queries = 16;
   while (a.queries > 1 && ((size_t)a.queries * a.row * 4 > 65536 || a.queries / 2 >= s.n)) a.queries /= 2;
+  a.sharing = 1;
+  while (pages > a.sharing * kMostKeys * 64) a.sharing *= 2;     // 2048 pages per wave, 16384 in all
   const dim3 grid((s.n + a.queries - 1) / a.queries, s.hk, s.B);
   const size_t lds = (size_t)a.queries * a.row * 4;
-#define GO(T, DH) select_kernel<T, DH><<<grid, kWaves * 64, lds, st>>>(a)
+#define GO(T, DH)                                                                                                 \
+  do {                                                                                                            \
+    if (pages <= 256) select_kernel<T, DH, 4><<<grid, kWaves * 64, lds, st>>>(a);                                 \
+    else if (pages <= 512) select_kernel<T, DH, 8><<<grid, kWaves * 64, lds, st>>>(a);                            \
+    else select_kernel<T, DH, kMostKeys><<<grid, kWaves * 64, lds, st>>>(a);                                      \
+  } while (0)
   if (s.dtype == NOVA_BF16) { if (s.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
   else { if (s.dh == 64) GO(float, 64); else GO(float, 128); }
 #undef GO
