@@ -166,10 +166,10 @@ __device__ __forceinline__ uint32_t swizzled_source(int r, int p) {
   return r * ROWB + ((x ^ x >> (ROWB == 256 ? 3 : 2)) << 4);
 }
 
-// paged_few.hip: blocks of 16 mt rows, four waves that each take tiles of so many keys of their own
+// paged_few.hip: blocks of 16 mt rows, 4 or 8 waves (8: mt 1) that each take tiles of so many keys of their own
 template <typename T> constexpr int paged_few_tile(int dh) { return 8192 / (dh * (int)sizeof(T)); }
 template <typename T>
-hipError_t launch_paged_few(hipStream_t st, int dh, int mt, unsigned grid, const PagedArgs<T>& a);
+hipError_t launch_paged_few(hipStream_t st, int dh, int mt, int waves, unsigned grid, const PagedArgs<T>& a);
 
 // paged_many.hip: blocks of so many rows, bf16
 constexpr int kPagedRows = 128;

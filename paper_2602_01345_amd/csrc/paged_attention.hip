@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
 // How a call is divided: mt > 0: blocks of 16 mt rows (paged_few.hip), else blocks of kPagedRows (paged_many.hip); items below n_whole
 // are one workgroup each, the others nsplit runs (of run_tiles tiles where that is not 0).
 struct Plan {
-  int mt, block_rows, blocks, items, n_whole, nsplit, run_tiles, ranked, listed;
+  int mt, waves, block_rows, blocks, items, n_whole, nsplit, run_tiles, ranked, listed;
   int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
 };
 constexpr int kCus = 256;
@@ -96,6 +96,7 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   p.items = B * c.kv_heads * p.blocks;
   p.n_whole = p.items;
   p.nsplit = 1;
+  p.waves = 4;
   p.listed = listed(p.block_rows);
   if (p.mt) {
     const int tile = wide ? paged_few_tile<float>(c.dh) : paged_few_tile<bf16_t>(c.dh);
@@ -104,7 +105,14 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
     const int ntiles = (int)((keys + tile - 1) / tile);
     p.run_tiles = ntiles;
     const int want = std::min((8 * kCus + p.items - 1) / p.items, ntiles);       // waves per item: eight per CU, a tile each
-    if (want > 4) {
+    // Blocks of 16 rows that stay whole, eight waves of one workgroup, so that nothing is joined by a second launch: up to 12 tiles,
+    // more of them the more blocks there are, whose tiles the chip can only read one after the other anyway (us in runs and joined /
+    // in one launch, tiles of 32 keys, heads of 128 in bf16: 32 blocks 8 tiles 8.0 / 6.5, 16 9.2 / 8.1, 24 7.9 / 10.2; 128 blocks 16
+    // 11.8 / 8.9, 48 22.3 / 19.2, 96 35.9 / 33.2; fp32, tiles of 16: 32 blocks 8 8.3 / 7.0, 16 9.7 / 10.0; 128 blocks 48 23.8 / 22.4, 96
+    // 37.7 / 38.1)
+    if (want > 4 && p.mt == 1 && ntiles <= std::max(12, p.items * 3 / 8)) {
+      p.waves = 8;
+    } else if (want > 4) {
       p.run_tiles = std::max((ntiles + want / 4 - 1) / (want / 4), 4);
       p.nsplit = (ntiles + p.run_tiles - 1) / p.run_tiles;
       if (p.nsplit > 1) p.n_whole = 0;
@@ -156,8 +164,8 @@ hipError_t attend(hipStream_t st, const PagedCall& call) {
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(call.workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
   const unsigned grid = (unsigned)(p.n_whole + p.runs());
   hipError_t e;
-  if constexpr (sizeof(T) == 2) e = p.mt ? launch_paged_few<T>(st, c.dh, p.mt, grid, a) : launch_paged_many(st, c.dh, grid, a);
-  else e = launch_paged_few<T>(st, c.dh, p.mt, grid, a);
+  if constexpr (sizeof(T) == 2) e = p.mt ? launch_paged_few<T>(st, c.dh, p.mt, p.waves, grid, a) : launch_paged_many(st, c.dh, grid, a);
+  else e = launch_paged_few<T>(st, c.dh, p.mt, p.waves, grid, a);
   if (e != hipSuccess || p.nsplit == 1) return e;
   const int used = std::min(p.block_rows, call.n * a.G);         // rows of a block that there are, where it is the only one
   const int64_t rows = (int64_t)(p.items - p.n_whole) * used;

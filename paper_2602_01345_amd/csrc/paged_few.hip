@@ -2,7 +2,7 @@
 // tokens, a handful of queries, and queries that have chosen pages each for themselves.  What bounds it is reading the keys and
 // values once.
 //
-// A workgroup is four waves and one block of rows; tiles of keys are dealt to the waves, which share nothing until their results
+// A workgroup is four or eight waves and one block of rows; tiles of keys are dealt to the waves, which share nothing until their results
 // are joined at the end, so no tile waits at a barrier.  A tile is made of groups of 16 keys; a group lies in one page, wherever a
 // page ends.  Everything is computed transposed, a lane owning one row of 16 (col) and the four lane groups (grp) parts of the keys:
 //   S^T = K Q^T    16 keys x 16 rows per MFMA.  The order of the channels in that product is free, so the four lanes of a key take
@@ -17,10 +17,8 @@
 
 namespace {
 
-constexpr int kWaves = 4;
-
-template <typename T, int DH, int MT, bool CHOSEN>
-__global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
+template <typename T, int DH, int MT, int NW, bool CHOSEN>
+__global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
   constexpr bool WIDE = sizeof(T) == 4;
   constexpr int TG = paged_few_tile<T>(DH) / kPageGroup;         // groups per tile
   constexpr int TG_SHIFT = TG == 4 ? 2 : TG == 2 ? 1 : 0;
@@ -30,8 +28,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
   constexpr int DT = DH / 16;                  // 16-channel blocks of the output
   constexpr int TILE = TG * 16 * ROWB, MINE = 2 * TILE;          // values of a tile; LDS of a wave, in the end its 16 x DH results
   static_assert(TILE == 8192 && TG * (KC + VG) == 16, "the wait for values counts sixteen loads behind them");
-  __shared__ __attribute__((aligned(1024))) char lds[kWaves * MINE];
-  __shared__ float part_m[kWaves][16], part_l[kWaves][16];
+  __shared__ __attribute__((aligned(1024))) char lds[NW * MINE];
+  __shared__ float part_m[NW][16], part_l[NW][16];
   extern __shared__ uint32_t lists[];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -55,14 +53,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
   ChosenPages list = {};
   int groups = (seen_most + 15) / 16;
   if constexpr (CHOSEN) {
-    list = list_chosen<T, kWaves * 64, 1>(a, lists, b, j, row0, s_first, s_last, (seen_most + (1 << a.shift) - 1) >> a.shift);
+    list = list_chosen<T, NW * 64, 1>(a, lists, b, j, row0, s_first, s_last, (seen_most + (1 << a.shift) - 1) >> a.shift);
     groups = list.count << gshift;
   }
   const int ntiles = (groups + TG - 1) / TG;
   // runs of one length whatever the image has, so that an image of any length is spread like the others
   const int t0 = split_i * a.run_tiles, t1 = min(ntiles, t0 + a.run_tiles);
   if (nparts > 1 && t0 >= t1) {                                  // nothing for this one: nothing to be joined
-    for (int rr = tid; rr < 16 * MT; rr += kWaves * 64) {
+    for (int rr = tid; rr < 16 * MT; rr += NW * 64) {
       const int64_t to = (int64_t)piece * 16 * MT + rr;
       a.part_ml[to * 2] = kNone;
       a.part_ml[to * 2 + 1] = 0.f;
@@ -142,7 +140,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
   };
 
   const int first = t0 + wave;
-  Pages pages = look_up(first), pages_next = look_up(first + kWaves);
+  Pages pages = look_up(first), pages_next = look_up(first + NW);
   if (first < t1) {
     load_v(first, 0, pages);
     load_k(first, pages);
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
   bool strict = false;                                           // the second time over the tiles
   int stage = 0;
   for (int t = first; t < t1;) {
-    const bool more = t + kWaves < t1;
+    const bool more = t + NW < t1;
     const char* sv = mine + stage * TILE;
 #pragma unroll
     for (int i = 0; i < TG; ++i) key0[i] = group_key(pages, t, i);
@@ -208,8 +206,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
         }
       }
     if (more) {
-      load_v(t + kWaves, stage ^ 1, pages_next);
-      load_k(t + kWaves, pages_next);
+      load_v(t + NW, stage ^ 1, pages_next);
+      load_k(t + NW, pages_next);
     }
 
     // ---- keys that not every row of the block sees
@@ -370,8 +368,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
       }
     }
     pages = pages_next;
-    if (t + 2 * kWaves < t1) pages_next = look_up(t + 2 * kWaves);
-    t += kWaves;
+    if (t + 2 * NW < t1) pages_next = look_up(t + 2 * NW);
+    t += NW;
     stage ^= 1;
     if (t >= t1 && !strict) {
       float sum = 0.f;                                           // 0, or NaN where some number is none
@@ -386,7 +384,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
         clear();
         t = first;
         pages = look_up(first);
-        pages_next = look_up(first + kWaves);
+        pages_next = look_up(first + NW);
         load_v(first, stage, pages);
         load_k(first, pages);
       }
@@ -415,15 +413,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
       *reinterpret_cast<f32x4*>(mine + (c4 * 16 + col) * 16) = v;
     }
     __syncthreads();
-    for (int i = tid; i < 16 * (DH / 4); i += kWaves * 64) {
+    for (int i = tid; i < 16 * (DH / 4); i += NW * 64) {
       const int c4 = i % (DH / 4), rr = i / (DH / 4), row = row0 + mt * 16 + rr;
       if (row >= rows) continue;
       float m = kNone, lt = 0.f;
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, part_m[w][rr]);
+      for (int w = 0; w < NW; ++w) m = fmaxf(m, part_m[w][rr]);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < NW; ++w) {
         const float f = __builtin_amdgcn_exp2f(part_m[w][rr] - m);
         lt = fmaf(f, part_l[w][rr], lt);
         acc += f * *reinterpret_cast<const f32x4*>(lds + w * MINE + (c4 * 16 + rr) * 16);
@@ -449,17 +447,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void few_kernel(PagedArgs<T> a) {
 }  // namespace
 
 template <typename T>
-hipError_t launch_paged_few(hipStream_t st, int dh, int mt, unsigned grid, const PagedArgs<T>& a) {
+hipError_t launch_paged_few(hipStream_t st, int dh, int mt, int waves, unsigned grid, const PagedArgs<T>& a) {
   const size_t lists = a.chosen ? chosen_bytes(a.most_pages, a.most_listed, 1) : 0;
-#define GO(DH, MT)                                                                                     \
-  do {                                                                                                 \
-    if (a.chosen) few_kernel<T, DH, MT, true><<<grid, kWaves * 64, (lists + 15) / 16 * 16, st>>>(a);   \
-    else few_kernel<T, DH, MT, false><<<grid, kWaves * 64, 0, st>>>(a);                                \
+#define GO(DH, MT, NW)                                                                                       \
+  do {                                                                                                       \
+    if (a.chosen) few_kernel<T, DH, MT, NW, true><<<grid, NW * 64, (lists + 15) / 16 * 16, st>>>(a);         \
+    else few_kernel<T, DH, MT, NW, false><<<grid, NW * 64, 0, st>>>(a);                                      \
   } while (0)
-  if (dh == 64) { if (mt == 2) GO(64, 2); else GO(64, 1); }
-  else { if (mt == 2) GO(128, 2); else GO(128, 1); }
+  if (dh == 64) { if (mt == 2) GO(64, 2, 4); else if (waves == 8) GO(64, 1, 8); else GO(64, 1, 4); }
+  else { if (mt == 2) GO(128, 2, 4); else if (waves == 8) GO(128, 1, 8); else GO(128, 1, 4); }
 #undef GO
   return hipGetLastError();
 }
-template hipError_t launch_paged_few<bf16_t>(hipStream_t, int, int, unsigned, const PagedArgs<bf16_t>&);
-template hipError_t launch_paged_few<float>(hipStream_t, int, int, unsigned, const PagedArgs<float>&);
+template hipError_t launch_paged_few<bf16_t>(hipStream_t, int, int, int, unsigned, const PagedArgs<bf16_t>&);
+template hipError_t launch_paged_few<float>(hipStream_t, int, int, int, unsigned, const PagedArgs<float>&);
