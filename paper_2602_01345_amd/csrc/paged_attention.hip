@@ -81,15 +81,24 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   auto listed = [&](int block_rows) {
     return take > 0 ? (int)std::min<int64_t>(pages, (int64_t)std::min({block_rows, (block_rows - 1) / G + 2, n}) * take) : 0;
   };
-  p.mt = rows <= 16 ? 1 : rows <= 32 || wide ? 2 : 0;
-  const int64_t blocks32 = (int64_t)B * c.kv_heads * ((rows + 31) / 32);
-  if (p.mt == 0 && take == 0 && blocks32 <= 2 * kCus && kv_len <= 2048) p.mt = 2;
-  // Chosen pages: blocks of 128 rows where their queries' lists together are as long as the image has pages, so that they share, and
-  // where the list leaves room for a second workgroup in the LDS (us in blocks of 128 / of 32; 32 heads of 128 on 8, 1024 queries, of
-  // 512 pages of 64 rows 128 chosen 566 / 850, 32 350 / 359, 4 79 / 60; 128 queries, 32 chosen 73 / 100; of 512 pages of 16 rows 64
-  // chosen 140 / 163; heads of 64, of 256 pages of 32 rows 20 chosen 95 / 78).
-  if (p.mt == 0 && take > 0)
-    p.mt = c.dh == 128 && (int64_t)std::min((kPagedRows - 1) / G + 2, n) * take >= pages &&
+  // Rows that share what is read of a page, and registers of rows against waves:
+  //   fp32   16 with heads of 128 and where pages are chosen, else up to 32 (us in blocks of 16 / of 32; 1024 queries, 4096 keys, 16 heads
+  //          of 128 320 / 352, of 64 178 / 150; 512 queries over 16 of 128 pages, 32 heads of 128 on 8 227 / 329, of 64 130 / 152)
+  //   bf16   128 from 33 on, but up to two blocks of 32 per CU over up to 2048 keys are left as they are: no tile waits for the others,
+  //          and nothing is joined afterwards
+  //   bf16, chosen pages   128 where the lists of a block's queries together hold twice the pages there are, so that they must share
+  //          (heads of 128: with 64 the softmax is most of the time), if there are enough blocks and the list leaves room for a second
+  //          workgroup in the LDS; 16 where blocks are few (16 / 32 / 128; 32 heads of 128 on 8, 1024 queries, of 512 pages 128 chosen 1300 /
+  //          853 / 509, 32 437 / 352 / 327, 8 121 / 113 / 139; 128 queries, 32 chosen 66 / 62 / 70; 2 images of 20, 16 chosen 25 / 31 / 33;
+  //          16 heads of 64, 2000 queries, 32 of 256 pages 326 / 228 / 238)
+  const int64_t heads_all = (int64_t)B * c.kv_heads, blocks32 = heads_all * ((rows + 31) / 32);
+  if (rows <= 16 || (wide && (c.dh == 128 || take > 0))) p.mt = 1;
+  else if (rows <= 32 || wide) p.mt = 2;
+  else if (take == 0) p.mt = blocks32 <= 2 * kCus && kv_len <= 2048 ? 2 : 0;
+  else if (blocks32 <= kCus / 4) p.mt = 1;
+  else
+    p.mt = c.dh == 128 && heads_all * ((rows + kPagedRows - 1) / kPagedRows) >= kCus / 2 &&
+           (int64_t)std::min((kPagedRows - 1) / G + 2, n) * take >= 2 * (int64_t)pages &&
            chosen_bytes(pages, listed(kPagedRows), kPagedRows / 32) <= 16384 ? 0 : 2;
   p.block_rows = p.mt ? 16 * p.mt : kPagedRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;

@@ -57,8 +57,10 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
     groups = list.count << gshift;
   }
   const int ntiles = (groups + TG - 1) / TG;
-  // runs of one length whatever the image has, so that an image of any length is spread like the others
-  const int t0 = split_i * a.run_tiles, t1 = min(ntiles, t0 + a.run_tiles);
+  // runs of one length whatever the image has, so that an image of any length is spread like the others; lists of chosen pages in
+  // equal parts, since how long the union of several is nobody knows beforehand
+  const int run = CHOSEN ? (ntiles + nparts - 1) / nparts : a.run_tiles;
+  const int t0 = split_i * run, t1 = min(ntiles, t0 + run);
   if (nparts > 1 && t0 >= t1) {                                  // nothing for this one: nothing to be joined
     for (int rr = tid; rr < 16 * MT; rr += NW * 64) {
       const int64_t to = (int64_t)piece * 16 * MT + rr;

@@ -431,6 +431,99 @@ def test_pools_past_32_bits(nova, dtype):
     assert np.array_equal(_np(means[pages - 7]), np.array(want))
 
 
+# ---- blocks of 128 rows, long lists, shared pages -------------------------------------------------------------------
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("H,hk,n,L,p", [(4, 2, 140, 2300, 16), (3, 1, 200, 2500, 64), (40, 20, 90, 600, 32)])
+def test_what_a_query_does_not_see_in_blocks_of_128_rows(nova, dh, H, hk, n, L, p):
+    """NaN and infinities among the keys and values of rows behind a query's own: blocks that end as NaN are gone over again."""
+    B = 1 if L > 2048 else 4
+    cache, table = _fill("bf16", B, hk, p, dh, [L] * B, -(-L // p), 3)
+    for b in range(B):
+        for r in range(L - n + n // 2, L, 3):
+            pool = (cache.v_pages, cache.k_pages)[r % 2]
+            pool[int(table[b, r // p]), r % hk, r % p, r % dh] = (float("nan"), float("inf"), -float("inf"))[r % 3]
+    cache.v_pages[int(table[0, (L - n // 2) // p]), 0, (L - n // 2) % p, 5] = float("-inf")
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    pools = [_np(cache.k_pages), _np(cache.v_pages)]
+    K, V = ([P.image_rows(pool, table[b], L) for b in range(B)] for pool in pools)
+    out, lse = _run(nova, cache, table, q, L, causal=True)
+    ref = P.attention(_np(q), K, V, dh ** -0.5, [n] * B, True)
+    good = np.isfinite(ref[0]).all((0, 2, 3))
+    assert good[:n // 2].all() and not good.all()
+    pick = torch.from_numpy(good).cuda()
+    _compare(out[:, pick], lse[:, pick], [t[:, good] for t in ref], "bf16", dh, L)
+    # an infinity or a NaN that is seen shows where it should
+    bad = ~np.isfinite(ref[0])
+    assert not np.isfinite(_np(out)[bad]).any()
+
+
+@pytest.mark.parametrize("H,hk,n,L,p,take", [(16, 8, 260, 1100, 16, 20), (24, 8, 200, 1500, 64, 12), (40, 8, 130, 900, 32, 9), (130, 2, 70, 700, 16, 30),
+                                             (8, 8, 2050, 640, 64, 2)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_sparse_in_blocks_of_128_rows(nova, H, hk, n, L, p, take, causal):
+    """Lists that overlap; heads that share a key head in threes and fives, so that a query's rows lie in two waves, or in two blocks."""
+    B = max(1, 128 // (hk * -(-n * (H // hk) // 128)) + 1)
+    L = max(L, n)
+    _check(nova, "bf16", B, H, hk, 128, p, n, L, take=take, causal=causal, lens=None if B == 1 else [L - 13 * (b % 3) if L - 26 >= n else L for b in range(B)])
+
+
+@pytest.mark.parametrize("G", [1, 3])
+def test_chosen_pages_of_nan_in_blocks_of_128_rows(nova, G):
+    """A page of NaN that only some queries have chosen.  The others' results are within the same bounds as without it: tiles with such
+    a page are summed key by key, in another order (their logarithms are the same bits), and the bounds hold for any order."""
+    B, hk, dh, p, n, L, take = 3, 16, 128, 16, 400 // G, 640, 12
+    H = hk * G
+    cache, table = _fill("bf16", B, hk, p, dh, [L] * B, 40, 8)
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    g = np.random.default_rng(1)
+    chosen = np.sort(np.stack([g.permutation(39)[:take] for _ in range(B * n * hk)]).reshape(B, n, hk, take) + 1, axis=-1)
+    clean, clean_lse = _run(nova, cache, table, q, L, chosen=chosen)
+    for b in range(B):
+        cache.v_pages[int(table[b, 7]), :, 3] = float("nan")
+    out, lse = _run(nova, cache, table, q, L, chosen=chosen)
+    seen = torch.from_numpy((chosen == 7).any(-1).repeat(G, 2)).cuda()
+    assert seen.any() and not seen.all()
+    assert torch.isnan(out[seen]).all() and torch.equal(lse, clean_lse)
+    K, V = ([P.image_rows(_np(pool), table[b], L) for b in range(B)] for pool in (cache.k_pages, cache.v_pages))
+    ref = P.attention(_np(q), K, V, dh ** -0.5, [n] * B, False, chosen, p)
+    t_out, _ = _bounds(ref, "bf16", dh, take * p)
+    other = ~seen.cpu().numpy()
+    for got in (out, clean):
+        assert (np.abs(_np(got) - ref[0])[other] <= t_out[other]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hk,n,take", [(22, 96, 256), (1, 33, 256), (1, 1, 256)])
+def test_longest_lists_of_the_longest_page_lists(nova, dtype, hk, n, take):
+    """256 of 16384 pages for every query; the table names the same few pages over and over, as images with one beginning do."""
+    p, dh, pages, L = 16, 64, 48, 16384 * 16 - 5
+    g = np.random.default_rng(3)
+    cache, _ = _fill(dtype, 1, hk, p, dh, [pages * p], pages, 3, spare=0)
+    table = g.integers(0, pages, (1, 16384))
+    q = torch.randn((1, n, hk, dh), generator=torch.Generator().manual_seed(5)).to(DTYPES[dtype]).cuda()
+    chosen = np.sort(np.stack([g.permutation(16384)[:take] for _ in range(n * hk)]).reshape(1, n, hk, take), axis=-1)
+    chosen[0, 0, 0, -1] = 16383
+    out, lse = _run(nova, cache, table, q, L, chosen=chosen)
+    pools = [_np(cache.k_pages), _np(cache.v_pages)]
+    heads = [(0, 0), (n - 1, hk - 1), (n // 2, hk // 2)]
+    for s, h in heads:                                           # the chosen pages, one after the other, as an image of their own
+        K, V = ([P.image_rows(pool[:, h:h + 1], table[0, chosen[0, s, h]], take * p)] for pool in pools)
+        rows = np.where(chosen[0, s, h][:, None] * p + np.arange(p) < L)
+        K, V = ([x[0].reshape(1, take, p, dh)[:, rows[0], rows[1]]] for x in (K, V))
+        ref = P.attention(_np(q)[:, s:s + 1, h:h + 1], K, V, dh ** -0.5, [1], False)
+        _compare(out[:, s:s + 1, h:h + 1], lse[:, s:s + 1, h:h + 1], ref, dtype, dh, take * p)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("hk,n,L", [(32, 1, 200), (32, 1, 300), (32, 1, 777), (100, 1, 900), (130, 1, 1600), (64, 3, 500)])
+def test_few_rows_whole_and_in_runs(nova, dtype, dh, hk, n, L):
+    """One workgroup of eight waves per block, and runs that a second launch joins."""
+    _check(nova, dtype, 1, hk, hk, dh, 16, n, L)
+    _check(nova, dtype, 2, hk, hk // 2, dh, 64, n, L, lens=[L, max(L // 3, n)], causal=True)
+    _check(nova, dtype, 1, hk, hk, dh, 16, n, L, take=5)
+
+
 # ---- means and choices ----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("dh", [64, 128])
