@@ -74,6 +74,16 @@ struct PagedArgs : AttentionItems<T> {
   }
 };
 
+// The larger of a lane's number and that of the lane 32, or 16, away, on the vector unit.
+__device__ __forceinline__ float max_across_32(float v) {
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float max_across_16(float v) {
+  const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+
 // some bf16 number of the two in w is no finite one: an exponent of ones carries into the bit above it
 __device__ __forceinline__ uint32_t odd_pair(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 __device__ __forceinline__ uint32_t odd_one(uint32_t w) { return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u; }

@@ -70,50 +70,56 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
     return;
   }
 
-  // Pages of a tile, one lane per group: loaded a tile ahead of what is loaded through them.
-  struct Pages { int ordinal, page; };
+  // A tile's groups, one per lane: first key (one that nobody sees where there is no such group), where its rows begin in a pool, and
+  // how many bytes of rows of its page there are from there on (none where the page is none).  Looked up a tile ahead of the loads.
+  struct Groups { int key0; uint32_t bytes, lo, hi; };
+  const int64_t page_bytes = ((int64_t)a.hk << a.shift) * ROWB, head_at = ((int64_t)j << a.shift) * ROWB;
   auto look_up = [&](int t) {
-    const int x = min(t * TG + (lane & (TG - 1)), max(groups, 1) - 1);
-    Pages p;
-    p.ordinal = x >> gshift;
-    p.page = -1;
-    if (groups == 0) return p;
-    if constexpr (CHOSEN) {
-      p.page = list.page[p.ordinal];
-      p.ordinal = list.listed[p.ordinal];
-    } else {
-      p.page = table[p.ordinal];
+    const int x = t * TG + (lane & (TG - 1)), u = min(x, max(groups, 1) - 1) >> gshift;
+    Groups g = {1 << 30, 0u, 0u, 0u};
+    int ordinal = u, page = -1;
+    if (groups > 0) {
+      if constexpr (CHOSEN) {
+        page = list.page[u];
+        ordinal = list.listed[u];
+      } else {
+        page = table[u];
+      }
     }
-    return p;
+    const int row = (x & gmask) * 16;
+    const bool there = (unsigned)page < (unsigned)a.pages;
+    const int64_t at = (there ? page : 0) * page_bytes + head_at + row * ROWB;
+    if (x < groups) {
+      g.key0 = (ordinal << a.shift) + row;
+      if (there) g.bytes = min(max(len - g.key0, 0), (1 << a.shift) - row) * ROWB;
+    }
+    g.lo = (uint32_t)at;
+    g.hi = (uint32_t)(at >> 32);
+    return g;
+  };
+  // group i of a tile as a buffer: loads from where its page's rows end give zeros
+  auto from = [&](const T* pool, const Groups& g, int i) {
+    const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(g.hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane(g.lo, i);
+    const uint64_t base = reinterpret_cast<uint64_t>(pool) + at;
+    return u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, (uint32_t)__builtin_amdgcn_readlane(g.bytes, i), 0x00020000u};
   };
   u32x4 kw[TG][KC];
-  int key0[TG];                                                  // first key of the tile's groups
-  auto group_key = [&](const Pages& p, int t, int i) {
-    const int x = t * TG + i;
-    const int first = (__builtin_amdgcn_readlane(p.ordinal, i) << a.shift) + ((x & gmask) << 4);
-    return x < groups ? first : 1 << 30;                         // no such group: its keys are seen by nobody
-  };
-  auto rows_there = [&](const Pages& p, int t, int i) {
-    const int ordinal = __builtin_amdgcn_readlane(p.ordinal, i);
-    return t * TG + i < groups ? min(max(len - (ordinal << a.shift), 0), 1 << a.shift) : 0;
+  int key0[TG];                                                  // first keys of the tile's groups
+  auto keys_of = [&](const Groups& g) {
+#pragma unroll
+    for (int i = 0; i < TG; ++i) key0[i] = __builtin_amdgcn_readlane(g.key0, i);
   };
   // a tile of one page is loaded through one buffer, otherwise each group through its own
   const bool one_page = gshift >= TG_SHIFT;
-  auto load_k = [&](int t, const Pages& p) {
-    auto from = page_buffer<T, DH>(a.keys, __builtin_amdgcn_readlane(p.page, 0), a.pages, a.hk, j, a.shift, rows_there(p, t, 0));
-    uint32_t at = ((t * TG) & gmask) * 16 * ROWB;
+  auto load_k = [&](const Groups& g) {
+    u32x4 w = from(a.keys, g, 0);
 #pragma unroll
     for (int i = 0; i < TG; ++i) {
-      if (i > 0) {
-        at += 16 * ROWB;
-        if (!one_page) {
-          from = page_buffer<T, DH>(a.keys, __builtin_amdgcn_readlane(p.page, i), a.pages, a.hk, j, a.shift, rows_there(p, t, i));
-          at = ((t * TG + i) & gmask) * 16 * ROWB;
-        }
-      }
+      if (i > 0 && !one_page) w = from(a.keys, g, i);
+      const auto buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)w[1] << 32 | w[0]), 0, w[2], w[3]);
+      const uint32_t at = one_page ? i * 16 * ROWB : 0;
 #pragma unroll
-      for (int e = 0; e < KC; ++e)
-        kw[i][e] = __builtin_amdgcn_raw_buffer_load_b128(from, col * ROWB + (e * 4 + grp) * 16, at, 0);
+      for (int e = 0; e < KC; ++e) kw[i][e] = __builtin_amdgcn_raw_buffer_load_b128(buffer, col * ROWB + (e * 4 + grp) * 16, at, 0);
     }
   };
   // bf16: the swizzle is made by which chunk of its row a lane asks for; fp32: rows as they are
@@ -125,27 +131,22 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
     if constexpr (WIDE) part[e] = e * 1024 + lane * 16;
     else part[e] = swizzled_source<ROWB>(e * RPL + lane / (64 / RPL), lane % (64 / RPL));
   }
-  auto load_v = [&](int t, int stage, const Pages& p) {
-    u32x4 from = page_words<T, DH>(a.values, __builtin_amdgcn_readlane(p.page, 0), a.pages, a.hk, j, a.shift, rows_there(p, t, 0));
-    uint32_t at = ((t * TG) & gmask) * 16 * ROWB;
+  auto load_v = [&](int stage, const Groups& g) {
+    u32x4 w = from(a.values, g, 0);
 #pragma unroll
     for (int i = 0; i < TG; ++i) {
-      if (i > 0) {
-        at += 16 * ROWB;
-        if (!one_page) {
-          from = page_words<T, DH>(a.values, __builtin_amdgcn_readlane(p.page, i), a.pages, a.hk, j, a.shift, rows_there(p, t, i));
-          at = ((t * TG + i) & gmask) * 16 * ROWB;
-        }
-      }
-      load_to_lds(from, mine0 + stage * TILE + i * VG * 1024, part, at);
+      if (i > 0 && !one_page) w = from(a.values, g, i);
+      load_to_lds(w, mine0 + stage * TILE + i * VG * 1024, part, one_page ? i * 16 * ROWB : 0);
     }
   };
 
   const int first = t0 + wave;
-  Pages pages = look_up(first), pages_next = look_up(first + NW);
+  Groups next = look_up(first);
+  keys_of(next);
   if (first < t1) {
-    load_v(first, 0, pages);
-    load_k(first, pages);
+    load_v(0, next);
+    load_k(next);
+    next = look_up(first + NW);
   }
   // chunk grp + 4 e of row col; past the last live row its copies (padding is nobody's)
   u32x4 qf[MT][KC];
@@ -183,8 +184,6 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
   for (int t = first; t < t1;) {
     const bool more = t + NW < t1;
     const char* sv = mine + stage * TILE;
-#pragma unroll
-    for (int i = 0; i < TG; ++i) key0[i] = group_key(pages, t, i);
     uint32_t who[TG];
     if constexpr (CHOSEN)
 #pragma unroll
@@ -208,8 +207,8 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
         }
       }
     if (more) {
-      load_v(t + NW, stage ^ 1, pages_next);
-      load_k(t + NW, pages_next);
+      load_v(stage ^ 1, next);
+      load_k(next);
     }
 
     // ---- keys that not every row of the block sees
@@ -249,35 +248,36 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float psum = 0.f;
+      auto probabilities = [&] {
+        psum = 0.f;
 #pragma unroll
-      for (int i = 0; i < TG; ++i)
+        for (int i = 0; i < TG; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          pr[mt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][i][r], a.scale_log2, -m_run[mt]));
-          psum += pr[mt][i][r];
-        }
-      if (__any(!(psum <= kBig))) {
+          for (int r = 0; r < 4; ++r) {
+            pr[mt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][i][r], a.scale_log2, -m_run[mt]));
+            psum += pr[mt][i][r];
+          }
+      };
+      auto largest = [&] {
         float tmax = -INFINITY;
 #pragma unroll
         for (int i = 0; i < TG; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r) tmax = fmaxf(tmax, s[mt][i][r] * a.scale_log2);
-        tmax = fmaxf(tmax, __shfl_xor(tmax, 16, NOVA_WAVE));
-        tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
+        return max_across_32(max_across_16(tmax));
+      };
+      auto move = [&](float tmax) {
         const float m_new = fmaxf(m_run[mt], tmax);
         const float alpha = __builtin_amdgcn_exp2f(m_run[mt] - m_new);
         l_run[mt] *= alpha;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[mt][d] *= alpha;
         m_run[mt] = m_new;
-        psum = 0.f;
-#pragma unroll
-        for (int i = 0; i < TG; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            pr[mt][i][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][i][r], a.scale_log2, -m_new));
-            psum += pr[mt][i][r];
-          }
+      };
+      probabilities();
+      if (__any(!(psum <= kBig))) {
+        move(largest());
+        probabilities();
       }
       l_run[mt] += psum;
     }
@@ -369,8 +369,8 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
         }
       }
     }
-    pages = pages_next;
-    if (t + 2 * NW < t1) pages_next = look_up(t + 2 * NW);
+    keys_of(next);
+    if (t + 2 * NW < t1) next = look_up(t + 2 * NW);
     t += NW;
     stage ^= 1;
     if (t >= t1 && !strict) {
@@ -385,10 +385,11 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
         strict = true;
         clear();
         t = first;
-        pages = look_up(first);
-        pages_next = look_up(first + NW);
-        load_v(first, stage, pages);
-        load_k(first, pages);
+        next = look_up(first);
+        keys_of(next);
+        load_v(stage, next);
+        load_k(next);
+        next = look_up(first + NW);
       }
     }
   }
@@ -451,13 +452,19 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
 template <typename T>
 hipError_t launch_paged_few(hipStream_t st, int dh, int mt, int waves, unsigned grid, const PagedArgs<T>& a) {
   const size_t lists = a.chosen ? chosen_bytes(a.most_pages, a.most_listed, 1) : 0;
-#define GO(DH, MT, NW)                                                                                       \
-  do {                                                                                                       \
-    if (a.chosen) few_kernel<T, DH, MT, NW, true><<<grid, NW * 64, (lists + 15) / 16 * 16, st>>>(a);         \
-    else few_kernel<T, DH, MT, NW, false><<<grid, NW * 64, 0, st>>>(a);                                      \
-  } while (0)
-  if (dh == 64) { if (mt == 2) GO(64, 2, 4); else if (waves == 8) GO(64, 1, 8); else GO(64, 1, 4); }
-  else { if (mt == 2) GO(128, 2, 4); else if (waves == 8) GO(128, 1, 8); else GO(128, 1, 4); }
+#define GO(DH, MT, NW, CHOSEN) few_kernel<T, DH, MT, NW, CHOSEN><<<grid, NW * 64, CHOSEN ? (lists + 15) / 16 * 16 : 0, st>>>(a)
+#define ONE(DH, CHOSEN) do { if (waves == 8) GO(DH, 1, 8, CHOSEN); else GO(DH, 1, 4, CHOSEN); } while (0)
+  if (mt == 1) {
+    if (dh == 64) { if (a.chosen) ONE(64, true); else ONE(64, false); }
+    else { if (a.chosen) ONE(128, true); else ONE(128, false); }
+  } else if constexpr (sizeof(T) == 4) {
+    if (dh != 64 || a.chosen) return hipErrorInvalidValue;       // 16 rows there
+    GO(64, 2, 4, false);
+  } else {
+    if (dh == 64) { if (a.chosen) GO(64, 2, 4, true); else GO(64, 2, 4, false); }
+    else { if (a.chosen) GO(128, 2, 4, true); else GO(128, 2, 4, false); }
+  }
+#undef ONE
 #undef GO
   return hipGetLastError();
 }

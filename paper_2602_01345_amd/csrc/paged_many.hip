@@ -215,21 +215,25 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
       }
     }
     float e[2][16], psum = 0.f;
+    auto probabilities = [&] {
+      psum = 0.f;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -m_run));
-        psum += e[kb][r];
-      }
-    if (__any(!(psum <= kBig))) {
-      // some score lies far above the reference, as any does above the first one: it moves to the largest score, and the sums with it
+        for (int r = 0; r < 16; ++r) {
+          e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -m_run));
+          psum += e[kb][r];
+        }
+    };
+    auto largest = [&] {
       float tmax = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, s[kb][r] * a.scale_log2);
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, NOVA_WAVE));
+      return max_across_32(tmax);
+    };
+    auto move = [&](float tmax) {
       const float m_new = fmaxf(m_run, tmax);
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
@@ -238,14 +242,12 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
       m_run = m_new;
-      psum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          e[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -m_new));
-          psum += e[kb][r];
-        }
+    };
+    probabilities();
+    if (__any(!(psum <= kBig))) {
+      // some score lies far above the reference, as any does above the first one: it moves to the largest score, and the sums with it
+      move(largest());
+      probabilities();
     }
     l_run += psum;
     __builtin_amdgcn_s_setprio(1);
