@@ -39,7 +39,7 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 
 // R: keys a lane holds
 template <typename T, int DH, int R>
-__global__ __launch_bounds__(kWaves * 64, 2) void select_kernel(SelectArgs a) {
+__global__ __launch_bounds__(kWaves * 64, 4) void select_kernel(SelectArgs a) {
   constexpr int KC = DH / 32;                  // MFMAs per score: chunk 4 e + grp of eight channels
   extern __shared__ uint32_t keys[];           // [queries][row]
   __shared__ int counts[2][kWaves], equals[kWaves];
@@ -65,60 +65,67 @@ __global__ __launch_bounds__(kWaves * 64, 2) void select_kernel(SelectArgs a) {
     look_up(wave);
     // the query's scale: one for all heads that share the key head
     const T* q = static_cast<const T*>(a.q) + b * a.q_sb + mine * a.q_sr + (int64_t)j * a.G * a.q_sh + grp * 8;
-    float top = 0.f;
-    bool odd = false;
+    uint32_t top = 0u;                         // largest magnitude, as the bits of an fp32 number: those that are none come last
     bf16x8 qf[kHeads][KC];                     // queries as they are (bf16), then rounded
+    // (a head's fp32 numbers at a time: the compiler would have all of them in registers at once, for half the waves)
     auto load_heads = [&](int g0, auto use) {
-#pragma unroll
-      for (int g = 0; g < kHeads; ++g)
-#pragma unroll
-        for (int e = 0; e < KC; ++e) {
-          const T* p = q + min(g0 + g, a.G - 1) * a.q_sh + e * 32;
-          if constexpr (sizeof(T) == 2) {
-            qf[g][e] = *reinterpret_cast<const bf16x8*>(p);
-          } else {
-            const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) use(g, e, i, i < 4 ? lo[i & 3] : hi[i & 3]);
-          }
-        }
       if constexpr (sizeof(T) == 2)
 #pragma unroll
-        for (int g = 0; g < kHeads; ++g)
+        for (int g = 0; g < kHeads; ++g) {
+          if (g0 + g >= a.G) break;
+#pragma unroll
+          for (int e = 0; e < KC; ++e) qf[g][e] = *reinterpret_cast<const bf16x8*>(q + (g0 + g) * a.q_sh + e * 32);
+        }
+#pragma unroll
+      for (int g = 0; g < kHeads; ++g) {
+        if (g0 + g >= a.G) break;
+        f32x4 w[KC][2];
+        if constexpr (sizeof(T) == 4)
 #pragma unroll
           for (int e = 0; e < KC; ++e)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) use(g, e, i, (float)qf[g][e][i]);
+            for (int c = 0; c < 2; ++c) w[e][c] = *reinterpret_cast<const f32x4*>(q + (g0 + g) * a.q_sh + e * 32 + c * 4);
+#pragma unroll
+        for (int e = 0; e < KC; ++e)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) use(g, e, i, sizeof(T) == 2 ? (float)qf[g][e][i] : w[e][i >> 2][i & 3]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
     for (int g0 = 0; g0 < a.G; g0 += kHeads)
-      load_heads(g0, [&](int, int, int, float v) {
-        top = fmaxf(top, fabsf(v));
-        odd |= !(fabsf(v) < INFINITY);
-      });
-    top = fmaxf(top, __shfl_xor(top, 16, NOVA_WAVE));
-    top = fmaxf(top, __shfl_xor(top, 32, NOVA_WAVE));
-    odd |= __shfl_xor((int)odd, 16, NOVA_WAVE);
-    odd |= __shfl_xor((int)odd, 32, NOVA_WAVE);
+      load_heads(g0, [&](int, int, int, float v) { top = max(top, __float_as_uint(v) & 0x7FFFFFFFu); });
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, NOVA_WAVE));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, NOVA_WAVE));
     // the smallest power of two of which 127 reach the largest: as in summarise_kernel
-    const uint32_t bits = __float_as_uint(top);
-    int e2 = (int)(bits >> 23) - 127 - 6 + ((bits & 0x7FFFFFu) > 0x7E0000u);    // 127 / 64 = 1.984375
-    e2 = min(max(e2, -100), 100);
-    const float unit = odd ? 0.f : __uint_as_float((uint32_t)(127 - e2) << 23);
+    const int e2 = (int)(top >> 23) - 127 - 6 + ((top & 0x7FFFFFu) > 0x7E0000u);                // 127 / 64 = 1.984375
+    const bool odd = top >= 0x7F800000u, held = !odd && e2 <= 100;                              // held: nothing passes 127
+    const float unit = __uint_as_float((uint32_t)(127 - min(max(e2, -100), 100)) << 23);
 
     for (int g0 = 0; g0 < a.G; g0 += kHeads) {
-      auto rounded = [&](int g, int e, int i, float v) {
-        qf[g][e][i] = (bf16_t)(odd ? 0.f : fminf(fmaxf(rintf(v * unit), -127.f), 127.f));
-      };
+      auto rounded = [&](int g, int e, int i, float v) { qf[g][e][i] = (bf16_t)rintf(v * unit); };
       if (sizeof(T) == 4 || a.G > kHeads) {
         load_heads(g0, rounded);
       } else {
 #pragma unroll
-        for (int g = 0; g < kHeads; ++g)
+        for (int g = 0; g < kHeads; ++g) {
+          if (g0 + g >= a.G) break;
 #pragma unroll
           for (int e = 0; e < KC; ++e)
 #pragma unroll
             for (int i = 0; i < 8; ++i) rounded(g, e, i, (float)qf[g][e][i]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      if (__any(!held))                        // (rare) a query with a NaN or an infinity: zeros; past 127 * 2^100: that
+#pragma unroll
+        for (int g = 0; g < kHeads; ++g) {
+          if (g0 + g >= a.G) break;
+#pragma unroll
+          for (int e = 0; e < KC; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qf[g][e][i] = odd ? (bf16_t)0.f : (bf16_t)fminf(fmaxf((float)qf[g][e][i], -127.f), 127.f);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       if (g0 > 0) look_up(wave);
       for (int x0 = wave; x0 * 16 < npages; x0 += kAhead * kWaves) {
         bf16x8 means[kAhead][KC];
