@@ -493,7 +493,7 @@ int nova_pruned_block_fourbit(nova_ctx* ctx, void* stream, const nova_block_shap
  *                      an image's last page on are not looked at; an entry that is no page of the pool reads as rows of zeros
  * page_rows is 16, 32, 64, 128 or 256, dh 64 or 128; pages * page_rows <= 2^30; heads that attend share a key head in runs of
  * heads / kv_heads.  Nothing reads what lies behind an image's rows.  Per-image arrays (..._per_row) are DEVICE int32 [B] or NULL,
- * clamped on the device like those of nova_pruned_block_rows; kv_len <= pitch * page_rows.
+ * clamped on the device like those of nova_pruned_block_rows; kv_len <= pitch * page_rows and <= 2^29.
  */
 typedef struct nova_paged_cache {
   void* k_pages;
@@ -520,7 +520,7 @@ typedef struct nova_paged_cache {
  *   kv_len_next  out DEVICE int32 [B]: rows of the images afterwards; may be kv_len_per_row (or another input) itself
  *   slots        out DEVICE int32 [B, n] or NULL: where image b's new row s goes, page * page_rows + row of the page; -1 where none
  *                comes.  One map serves all blocks whose pools share the table
- * kv_len + n <= pitch * page_rows, B <= 4096, B * max(n, pitch) <= 2^30, pages * page_rows <= 2^30.  The table's other entries are
+ * kv_len + n <= pitch * page_rows and <= 2^29, B <= 4096, B * max(n, pitch) <= 2^30, pages * page_rows <= 2^30.  The table's other entries are
  * untouched.  free_pages, table, slots and the rest must not overlap but as said.
  */
 int nova_paged_reserve(nova_ctx* ctx, void* stream, int B, int32_t* table, int pitch, int page_rows, int pages, int n,
@@ -529,7 +529,7 @@ int nova_paged_reserve(nova_ctx* ctx, void* stream, int B, int32_t* table, int p
 
 /* Rows k, v [B, n, kv_heads, dh] of the cache's dtype and any strides (rows of a projection's output, or the dense caches of
  * nova_pruned_block) to the slots [B, n]: one launch.  A slot outside [0, pages * page_rows) takes no row; two rows with one slot
- * leave either. */
+ * leave either.  B * n < 2^27. */
 int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, int n, const nova_rows* k,
                       const nova_rows* v, const int32_t* slots);
 
@@ -543,8 +543,8 @@ int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache
  *   lse        out fp32 [B, n, heads] or NULL: ln of the sum of e^(scale * score)
  *   workspace  of at least nova_paged_attention_workspace_bytes, 16-byte aligned (may be NULL where that is 0); calls that overlap,
  *              captured graphs among them, need one each.  0 bytes for sizes that the call refuses
- * B * heads * n <= 2^30, B <= 65535.  Queries past n_per_row[b], and queries that see no row, get zeros and lse = -inf.  A row that a
- * query does not see has no part in its result, whatever its key and value are (NaN among them).  NOVA_F32: products of fp32
+ * B * heads * n <= 2^30, B * kv_heads * ceil(n * heads / kv_heads / 16) < 2^24, B <= 65535.  Queries past n_per_row[b], and queries
+ * that see no row, get zeros and lse = -inf.  A row that a query does not see has no part in its result, whatever its key and value are (NaN among them).  NOVA_F32: products of fp32
  * numbers, summed in fp32; NOVA_BF16: probabilities are rounded to bf16 in front of the second product.
  */
 size_t nova_paged_attention_workspace_bytes(const nova_paged_cache* cache, int B, int heads, int n, int kv_len);
@@ -571,7 +571,7 @@ int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* ca
  * is in the call.
  *   chosen  out DEVICE int32 [B, n, kv_heads, k]: ordinals in the image's page list, ascending, then -1
  *   q       as in nova_paged_attention, of type dtype
- * 1 <= k <= 256, first + recent <= k, kv_len <= 16384 * page_rows; with causal 1 recent >= 1 (the page a query lies in may hold rows
+ * 1 <= k <= 256, first + recent <= k, kv_len <= 16384 * page_rows, n < 2^23; with causal 1 recent >= 1 (the page a query lies in may hold rows
  * behind it, in its mean too).
  *
  * nova_paged_sparse_attention is nova_paged_attention over the rows of the chosen pages alone (those of them that the query sees).

@@ -151,9 +151,10 @@ int paged_error(const nova_paged_cache* c) {
   return NOVA_OK;
 }
 // Page lists of B images that have kv_len rows at most.
+constexpr int kMostPagedRows = 1 << 29;
 int table_error(const int32_t* table, int B, int pitch, int page_rows, int64_t kv_len) {
   if (B < 0 || pitch < 0 || kv_len < 0 || kv_len > (int64_t)pitch * page_rows) return NOVA_ERR_INVALID_ARG;
-  if (B > 65535 || kv_len > 1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (B > 65535 || kv_len > kMostPagedRows) return NOVA_ERR_UNSUPPORTED;
   if (!aligned(table, 4) || (B > 0 && pitch > 0 && !table)) return NOVA_ERR_INVALID_ARG;
   return NOVA_OK;
 }
@@ -168,10 +169,12 @@ int paged_query_sizes_error(int B, int kv_heads, int heads, int n) {
   if (heads < 1 || n < 0 || heads % kv_heads != 0) return NOVA_ERR_INVALID_ARG;
   constexpr int kMost = 1 << 30;
   if (B > 0 && (heads > kMost / B || n > kMost / (B * heads))) return NOVA_ERR_UNSUPPORTED;
+  // a launch has under 2^32 threads: 256 for at least 16 of the rows that share a key head
+  if ((int64_t)B * kv_heads * (((int64_t)n * (heads / kv_heads) + 15) / 16) >= 1 << 24) return NOVA_ERR_UNSUPPORTED;
   return NOVA_OK;
 }
 size_t paged_workspace(const nova_paged_cache* c, int B, int heads, int n, int kv_len, int k) {
-  if (paged_sizes_error(c) != NOVA_OK || B < 1 || B > 65535 || n < 1 || kv_len < 0 || kv_len > 1 << 30) return 0;
+  if (paged_sizes_error(c) != NOVA_OK || B < 1 || B > 65535 || n < 1 || kv_len < 0 || kv_len > kMostPagedRows) return 0;
   if (paged_query_sizes_error(B, c->kv_heads, heads, n) != NOVA_OK) return 0;
   if (k != 0 && chosen_error(kv_len, c->page_rows, k) != NOVA_OK) return 0;
   return paged_attention_workspace_bytes(*c, B, heads, n, kv_len, k);
@@ -855,7 +858,7 @@ int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache
   if (!ctx || B < 0 || n < 0) return NOVA_ERR_INVALID_ARG;
   if (int rc = paged_error(cache)) return rc;
   if (int rc = counts_error({slots})) return rc;
-  if (B > 65535 || (int64_t)B * n > 1 << 30) return NOVA_ERR_UNSUPPORTED;
+  if (B > 65535 || (int64_t)B * n >= 1 << 27) return NOVA_ERR_UNSUPPORTED;        // 32 threads a row at most, under 2^32 in a launch
   if (B == 0 || n == 0 || cache->pages == 0) return NOVA_OK;
   if (!k || !v || !slots) return NOVA_ERR_INVALID_ARG;
   for (const nova_rows* r : {k, v})
@@ -901,6 +904,7 @@ int nova_paged_select(nova_ctx* ctx, void* stream, int dtype, const void* means,
   if (int rc = table_error(table, B, pitch, page_rows, kv_len)) return rc;
   if (int rc = paged_query_sizes_error(B, kv_heads, heads, n)) return rc;
   if (int rc = chosen_error(kv_len, page_rows, k)) return rc;
+  if (n >= 1 << 23) return NOVA_ERR_UNSUPPORTED;                 // 512 threads for one query at worst, under 2^32 in a launch
   if (int rc = counts_error({n_per_row, kv_len_per_row, chosen})) return rc;
   if ((causal != 0 && causal != 1) || first < 0 || recent < 0 || first > k || recent > k - first || recent < causal)
     return NOVA_ERR_INVALID_ARG;

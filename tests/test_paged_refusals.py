@@ -154,6 +154,28 @@ def test_select_types(lib):
     assert _summarise(lib, means=0) == INVALID and _summarise(lib, means=BASE + 4) == INVALID
 
 
+# more threads than a launch has, rows than a table: at the limits and one beyond them, where nothing else is wrong
+@pytest.mark.parametrize("call,kw", [
+    (_attend, dict(B=1 << 15, n=1, cache=_cache(kv_heads=512), heads=512)), (_sparse, dict(B=1 << 15, n=1, cache=_cache(kv_heads=512), heads=512)),
+    (_select, dict(B=1 << 15, n=1, kv_heads=512, heads=512)), (_attend, dict(B=1, n=(1 << 27) - 15, cache=_cache(kv_heads=2), heads=2)),
+    (_select, dict(B=1, n=1 << 23, kv_heads=1, heads=1)), (_append, dict(B=4, n=1 << 25)), (_append, dict(B=1, n=1 << 27)),
+    (_attend, dict(kv_len=(1 << 29) + 1, pitch=1 << 26)), (_summarise, dict(kv_len=(1 << 29) + 1, pitch=1 << 26)),
+    (_reserve, dict(B=1, n=2, kv_len=(1 << 29) - 1, pitch=1 << 26)),
+])
+def test_launches_too_large(lib, call, kw):
+    assert call(lib, **kw) == UNSUPPORTED
+
+
+def test_largest_sizes_are_not_refused(lib):
+    # a missing argument is what these end at
+    for call, kw in ((_attend, dict(B=1 << 15, n=1, cache=_cache(kv_heads=511), heads=511)), (_attend, dict(kv_len=1 << 29, pitch=1 << 25)),
+                     (_attend, dict(B=1, n=(1 << 27) - 16, cache=_cache(kv_heads=1), heads=1)), (_select, dict(B=1, n=(1 << 23) - 1, kv_heads=1, heads=1))):
+        assert call(lib, q=_rows(heads=4, data=0), **kw) == INVALID
+    assert _append(lib, B=1, n=(1 << 27) - 1, slots=0) == INVALID
+    assert _summarise(lib, kv_len=1 << 29, pitch=1 << 25, means=0) == INVALID
+    assert _reserve(lib, B=1, n=1, kv_len=(1 << 29) - 1, pitch=1 << 25, free_next=0) == INVALID
+
+
 def test_nothing_to_do_is_no_error(lib):
     for call in (_append, _attend, _sparse, _select, _summarise):
         assert call(lib, B=0) == 0 and call(lib, n=0) == 0
