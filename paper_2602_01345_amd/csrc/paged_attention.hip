@@ -84,8 +84,10 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   // Rows that share what is read of a page, and registers of rows against waves:
   //   fp32   16 with heads of 128 and where pages are chosen, else up to 32 (us in blocks of 16 / of 32; 1024 queries, 4096 keys, 16 heads
   //          of 128 320 / 352, of 64 178 / 150; 512 queries over 16 of 128 pages, 32 heads of 128 on 8 227 / 329, of 64 130 / 152)
-  //   bf16   128 from 33 on, but up to two blocks of 32 per CU over up to 2048 keys are left as they are: no tile waits for the others,
-  //          and nothing is joined afterwards
+  //   bf16   128 from 33 on, but with heads of 64 up to two blocks of 32 per CU over up to 2048 keys are left as they are: no tile waits
+  //          for the others, and nothing is joined afterwards (us in blocks of 32 / of 128; 8 images of 128 queries, 16 heads of 64:
+  //          256 keys 9.5 / 9.2, 512 12.0 / 17.4, 1024 17.0 / 21.9, 2048 26.7 / 29.0, 4096 47.3 / 41.5; 4 images of 256, 16 heads of 128:
+  //          256 16.4 / 12.9, 512 20.9 / 22.6, 1024 30.7 / 30.0, 2048 47.9 / 38.8)
   //   bf16, chosen pages   128 where the lists of a block's queries together hold twice the pages there are, so that they must share
   //          (heads of 128: with 64 the softmax is most of the time), if there are enough blocks and the list leaves room for a second
   //          workgroup in the LDS; 16 where blocks are few (16 / 32 / 128; 32 heads of 128 on 8, 1024 queries, of 512 pages 128 chosen 1300 /
@@ -94,7 +96,7 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   const int64_t heads_all = (int64_t)B * c.kv_heads, blocks32 = heads_all * ((rows + 31) / 32);
   if (rows <= 16 || (wide && (c.dh == 128 || take > 0))) p.mt = 1;
   else if (rows <= 32 || wide) p.mt = 2;
-  else if (take == 0) p.mt = blocks32 <= 2 * kCus && kv_len <= 2048 ? 2 : 0;
+  else if (take == 0) p.mt = c.dh == 64 && blocks32 <= 2 * kCus && kv_len <= 2048 ? 2 : 0;
   else if (blocks32 <= kCus / 4) p.mt = 1;
   else
     p.mt = c.dh == 128 && heads_all * ((rows + kPagedRows - 1) / kPagedRows) >= kCus / 2 &&
@@ -130,11 +132,14 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   }
   const int ntiles = (int)(((take > 0 ? (int64_t)p.listed * c.page_rows : kv_len) + 63) / 64), slots = 2 * kCus, rest = p.items % slots;
   // Images with lengths of their own: the longest first, so that short ones fill up the end; from two rounds of items on that is
-  // enough and none is cut.
+  // enough and none is cut (us in this order / in that of the images, the rest cut; 8 images of 512 queries, 36 heads of 64, up to 2048
+  // keys 84 / 90; of 700, 16 heads of 128, up to 8000 303 / 302; 16 of 300, 32 heads of 128 on 8, up to 8000 460 / 452).
   p.ranked = ragged && p.items > slots && B > 1 && B <= kRanked ? B : 0;
   if (rest == 0 || (p.ranked && p.items >= 2 * slots)) return p;
-  // A few more items than CUs, and long ones: most CUs would have one, which is little to hide anything behind, and the others two.
-  const bool in_three = p.items > kCus && p.items <= kCus + kCus / 4 && ntiles >= 64;
+  // A few more items than CUs, and long ones: most CUs would have one, which is little to hide anything behind, and the others two
+  // (us in three runs each / whole; 272 items of 8000 keys, heads of 128, 174 / 201, 306 186 / 230, 280 of 16 000 318 / 399; heads of 64,
+  // of which three items share a CU: 272 of 4096 72 / 71).
+  const bool in_three = c.dh == 128 && p.items > kCus && p.items <= kCus + kCus / 4 && ntiles >= 64;
   const int s = in_three ? 3 : std::min(slots / rest, ntiles / 4);
   if (s >= 2) {
     p.n_whole = p.items - rest;
