@@ -184,3 +184,6 @@ hipError_t launch_paged_few(hipStream_t st, int dh, int mt, int waves, unsigned 
 // paged_many.hip: blocks of so many rows, bf16
 constexpr int kPagedRows = 128;
 hipError_t launch_paged_many(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a);
+
+// paged_chosen.hip: the same, chosen pages
+hipError_t launch_paged_chosen(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a);

@@ -88,19 +88,20 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   //          for the others, and nothing is joined afterwards (us in blocks of 32 / of 128; 8 images of 128 queries, 16 heads of 64:
   //          256 keys 9.5 / 9.2, 512 12.0 / 17.4, 1024 17.0 / 21.9, 2048 26.7 / 29.0, 4096 47.3 / 41.5; 4 images of 256, 16 heads of 128:
   //          256 16.4 / 12.9, 512 20.9 / 22.6, 1024 30.7 / 30.0, 2048 47.9 / 38.8)
-  //   bf16, chosen pages   128 where the lists of a block's queries together hold twice the pages there are, so that they must share
-  //          (heads of 128: with 64 the softmax is most of the time), if there are enough blocks and the list leaves room for a second
-  //          workgroup in the LDS; 16 where blocks are few (16 / 32 / 128; 32 heads of 128 on 8, 1024 queries, of 512 pages 128 chosen 1300 /
-  //          853 / 509, 32 437 / 352 / 327, 8 121 / 113 / 139; 128 queries, 32 chosen 66 / 62 / 70; 2 images of 20, 16 chosen 25 / 31 / 33;
-  //          16 heads of 64, 2000 queries, 32 of 256 pages 326 / 228 / 238)
+  //   bf16, chosen pages   128 (paged_chosen.hip) where the lists of a block's queries together hold half as many pages as there are, so
+  //          that they share some, if there are blocks for a quarter of the CUs and the list leaves room for a second workgroup in the
+  //          LDS (us in blocks of 32 / of 128; 32 heads of 128 on 8, 1024 queries, of 512 pages 128 chosen 853 / 439, 32 352 / 252, 8
+  //          113 / 107, 4 60 / 64; 4 images of 64, 8 of 128 pages, 64 blocks of 128, 39 / 45; 2 of 500, 12 heads on 4, 20 of 256 pages, 96
+  //          blocks, 74 / 67; 16 heads of 64, 2000 queries, 32 of 256 pages 224 / 174); 16 where blocks are few (in blocks of 16 / of 32;
+  //          32 heads of 128 on 8, 2 images of 20 queries, 16 of 512 pages 25 / 31; 128 queries, 32 of 512 66 / 62)
   const int64_t heads_all = (int64_t)B * c.kv_heads, blocks32 = heads_all * ((rows + 31) / 32);
   if (rows <= 16 || (wide && (c.dh == 128 || take > 0))) p.mt = 1;
   else if (rows <= 32 || wide) p.mt = 2;
   else if (take == 0) p.mt = c.dh == 64 && blocks32 <= 2 * kCus && kv_len <= 2048 ? 2 : 0;
   else if (blocks32 <= kCus / 4) p.mt = 1;
   else
-    p.mt = c.dh == 128 && heads_all * ((rows + kPagedRows - 1) / kPagedRows) >= kCus / 2 &&
-           (int64_t)std::min((kPagedRows - 1) / G + 2, n) * take >= 2 * (int64_t)pages &&
+    p.mt = heads_all * ((rows + kPagedRows - 1) / kPagedRows) > kCus / 4 &&
+           2 * (int64_t)std::min((kPagedRows - 1) / G + 2, n) * take >= (int64_t)pages &&
            chosen_bytes(pages, listed(kPagedRows), kPagedRows / 32) <= 16384 ? 0 : 2;
   p.block_rows = p.mt ? 16 * p.mt : kPagedRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;
@@ -178,8 +179,9 @@ hipError_t attend(hipStream_t st, const PagedCall& call) {
   a.part_ml = reinterpret_cast<float*>(static_cast<char*>(call.workspace) + up256((size_t)p.runs() * p.block_rows * c.dh * 4));
   const unsigned grid = (unsigned)(p.n_whole + p.runs());
   hipError_t e;
-  if constexpr (sizeof(T) == 2) e = p.mt ? launch_paged_few<T>(st, c.dh, p.mt, p.waves, grid, a) : launch_paged_many(st, c.dh, grid, a);
-  else e = launch_paged_few<T>(st, c.dh, p.mt, p.waves, grid, a);
+  if constexpr (sizeof(T) == 4) e = launch_paged_few<T>(st, c.dh, p.mt, p.waves, grid, a);
+  else if (p.mt) e = launch_paged_few<T>(st, c.dh, p.mt, p.waves, grid, a);
+  else e = a.chosen ? launch_paged_chosen(st, c.dh, grid, a) : launch_paged_many(st, c.dh, grid, a);
   if (e != hipSuccess || p.nsplit == 1) return e;
   const int used = std::min(p.block_rows, call.n * a.G);         // rows of a block that there are, where it is the only one
   const int64_t rows = (int64_t)(p.items - p.n_whole) * used;

@@ -7,8 +7,6 @@
 // 16 keys (which lie in one page, wherever pages end) of K and of V, a line per row, the swizzle made by which chunk of its row a lane
 // asks for.  Two stages of LDS, two workgroups per CU (three with heads of 64), so that one wave's softmax runs next to another's
 // MFMAs; a wave asks for priority while it issues MFMAs.
-// Chosen pages: the block goes over the union of its queries' lists, its waves over those tiles that one of their own queries has
-// chosen, each query's rows masked where it has not.
 // A weight of 0 times a value that is no number is NaN, so what a row does not see could show in its result.  A workgroup whose sums
 // end as anything but finite numbers goes over its tiles again, and takes those with such values in them key by key.
 #include <type_traits>
@@ -26,7 +24,7 @@ __device__ __forceinline__ void wait_all() {
   asm volatile("" ::: "memory");
 }
 
-template <int DH, bool CHOSEN>
+template <int DH>
 __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(PagedArgs<bf16_t> a) {
   constexpr int ROWB = DH * 2;
   constexpr int HALF = kTile * ROWB, STAGE = 2 * HALF;     // K rows, V rows
@@ -35,7 +33,6 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   constexpr int NL = 16 * ROWB / 1024, RPL = 1024 / ROWB;  // loads of a wave's 16 rows, rows per load
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
   __shared__ uint32_t odd_waves[kWaves];
-  extern __shared__ uint32_t lists[];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -52,13 +49,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   const int last = min(row0 + kRows, live) - 1;            // last live row of the block
   const int seen_block = last < row0 ? 0 : visible_keys(a.causal, len, count, div_by(last, a.G, a.G_inv, unused));
   const int gshift = a.shift - 4, gmask = (1 << gshift) - 1;     // groups of 16 keys of a page
-  ChosenPages list = {};
-  int groups = (seen_block + 15) / 16;
-  if constexpr (CHOSEN) {
-    const int s_first = div_by(row0, a.G, a.G_inv, unused), s_last = last < row0 ? s_first : div_by(last, a.G, a.G_inv, unused);
-    list = list_chosen<bf16_t, kWaves * 64, kWaves>(a, lists, b, j, row0, s_first, s_last, (seen_block + (1 << a.shift) - 1) >> a.shift);
-    groups = list.count << gshift;
-  }
+  const int groups = (seen_block + 15) / 16;
   const int ntiles = (groups + 3) / 4;
   const int per = (ntiles + nparts - 1) / nparts;
   const int t0 = split_i * per, t1 = min(ntiles, t0 + per);
@@ -68,7 +59,6 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   const int s_wave = div_by(min(wrow, max(live - 1, 0)), a.G, a.G_inv, unused), s_wlast = div_by(max(wlast, 0), a.G, a.G_inv, unused);
   const int seen_least = wave_live ? visible_keys(a.causal, len, count, s_wave) : 0;
   const int seen_most = wave_live ? visible_keys(a.causal, len, count, s_wlast) : 0;
-  const uint32_t all = 0xFFFFFFFFu >> max(31 - (s_wlast - s_wave), 0);       // a bit for each of the wave's queries
 
   // this lane's part of a load of RPL rows: the chunk of its row that the swizzle puts where the lane's 16 bytes go
   uint32_t part[NL];
@@ -76,26 +66,19 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   for (int i = 0; i < NL; ++i) part[i] = swizzled_source<ROWB>(i * RPL + lane / (64 / RPL), lane % (64 / RPL));
   const int32_t* table = a.table + (int64_t)b * a.pitch;
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((lptr_t)lds);
-  // The wave's 16 keys of a tile lie in one page.  Its place in the pool: from the list, or from 64 tiles' places that the lanes hold.
-  struct Sixteen { int ordinal, page; };
+  // The wave's 16 keys of a tile lie in one page, the u-th of the image; lanes hold 64 tiles' places in the pool.
   int held = 0, held_first = 0;
   auto hold = [&](int t) {
     held_first = t;
     held = groups > 0 ? table[min((t + lane) * 4 + wave, groups - 1) >> gshift] : -1;
   };
   auto look_up = [&](int t) {
-    const int u = min(t * 4 + wave, max(groups, 1) - 1) >> gshift;
-    if constexpr (CHOSEN) {
-      if (groups == 0) return Sixteen{0, -1};
-      return Sixteen{(int)list.listed[u], list.page[u]};
-    } else {
-      if (t - held_first >= 64) hold(t);
-      return Sixteen{u, __builtin_amdgcn_readlane(held, t - held_first)};
-    }
+    if (t - held_first >= 64) hold(t);
+    return __builtin_amdgcn_readlane(held, t - held_first);
   };
-  auto request = [&](int t, const Sixteen& p) {
-    const int x = t * 4 + wave, page = __builtin_amdgcn_readfirstlane(p.page), ordinal = __builtin_amdgcn_readfirstlane(p.ordinal);
-    const int there = x < groups ? min(max(len - (ordinal << a.shift), 0), 1 << a.shift) : 0;
+  auto request = [&](int t, int page) {
+    const int x = t * 4 + wave, u = x >> gshift;
+    const int there = x < groups ? min(max(len - (u << a.shift), 0), 1 << a.shift) : 0;
     const uint32_t at = (x & gmask) * 16 * ROWB;
     const u32x4 ks = page_words<bf16_t, DH>(a.keys, page, a.pages, a.hk, j, a.shift, there);
     const u32x4 vs = page_words<bf16_t, DH>(a.values, page, a.pages, a.hk, j, a.shift, there);
@@ -104,18 +87,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
     load_to_lds(vs, to + HALF, part, at);
   };
 
-  // lanes i, i + 4 ..: first key of a tile's i-th 16 and which of the wave's queries have chosen its page
-  struct Four { int key0; uint32_t who; };
-  auto four = [&](int t) {
-    const int x = t * 4 + (lane & 3), u = min(x, max(groups, 1) - 1) >> gshift;
-    if constexpr (!CHOSEN) return Four{x * 16, all};
-    if (groups == 0) return Four{0, 0u};
-    return Four{(list.listed[u] << a.shift) + (x & gmask) * 16, x < groups ? list.member[u * kWaves + wave] : 0u};
-  };
-
-  if constexpr (!CHOSEN) hold(t0);
-  Sixteen next = look_up(t0);
-  Four four_next = four(t0);
+  hold(t0);
+  int next = look_up(t0);
   if (t0 < t1) {
     request(t0, next);
     next = look_up(t0 + 1);
@@ -130,7 +103,6 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   }
   const int s_row = div_by(row_live, a.G, a.G_inv, unused);
   const int seen = visible_keys(a.causal, len, count, s_row);
-  const uint32_t bit = 1u << ((s_row - s_wave) & 31);
   // this lane's places in a tile: its key's chunks, and for transposed reads of values the 8-byte piece lane % 4 of 16 channels of
   // key 4 half + (lane % 16) / 4 and of the one 8 behind it.  The swizzle repeats after 16 rows.
   int ka[KS], va[DB][2];
@@ -159,15 +131,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   constexpr bool STRICT = decltype(strict_tag)::value;     // the second time
   for (int t = t0; t < t1; ++t) {
     wait_all();                                            // tile t has landed, and nobody reads the other stage any more
-    int key0[4];
-    uint32_t who[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      key0[i] = CHOSEN ? __builtin_amdgcn_readlane(four_next.key0, i) : t * kTile + i * 16;
-      who[i] = CHOSEN ? (uint32_t)__builtin_amdgcn_readlane((int)four_next.who, i) : all;
-    }
-    four_next = four(t + 1);
-    const bool mine = key0[0] < seen_most && (!CHOSEN || (who[0] | who[1] | who[2] | who[3]) != 0u);
+    const int key0 = t * kTile;
+    const bool mine = key0 < seen_most;
     // the next tile is asked for behind the first MFMAs, which then start at once (67 us at the barrier, 65 here: 8 images of 512
     // queries, 36 heads of 64)
     auto ahead = [&] {
@@ -194,15 +159,13 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
     ahead();
     // ---- softmax: register r of block kb is key 64 t + 32 kb + 8 (r / 4) + 4 half + r % 4
     bool careful = false;
-    if (key0[3] + 16 > seen_least || (CHOSEN && (who[0] & who[1] & who[2] & who[3]) != all)) {     // keys that not all of its rows see
+    if (key0 + kTile > seen_least) {                       // keys that not all of its rows see
       const float dead = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int g = kb * 2 + (r >> 3);
-          if (key0[g] + 8 * ((r >> 2) & 1) + 4 * half + (r & 3) >= seen || (CHOSEN && !(who[g] & bit))) s[kb][r] = dead;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (key0 + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3) >= seen) s[kb][r] = dead;
       if constexpr (STRICT) {
         uint32_t odd = 0u;
 #pragma unroll 1
@@ -302,10 +265,9 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
     wait_all();
     if (odd_waves[0] | odd_waves[1] | odd_waves[2] | odd_waves[3]) {
       clear();
-      if constexpr (!CHOSEN) hold(t0);
+      hold(t0);
       request(t0, look_up(t0));
       next = look_up(t0 + 1);
-      four_next = four(t0);
       over_tiles(std::true_type{});
     }
   }
@@ -313,7 +275,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
   if (row >= rows) return;
   const float l = l_run + __shfl_xor(l_run, 32, NOVA_WAVE);
   if (nparts == 1) {
-    const bool some = row < live && seen > 0 && !(CHOSEN && l == 0.f);
+    const bool some = row < live && seen > 0;
     const int64_t to = a.out_row(b, j, row);
     const float inv = some ? 1.0f / l : 0.f;
 #pragma unroll
@@ -344,10 +306,7 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
 }  // namespace
 
 hipError_t launch_paged_many(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a) {
-  const size_t lists = a.chosen ? (chosen_bytes(a.most_pages, a.most_listed, kWaves) + 15) / 16 * 16 : 0;
-#define GO(DH, CHOSEN) many_kernel<DH, CHOSEN><<<grid, kWaves * 64, lists, st>>>(a)
-  if (dh == 64) { if (a.chosen) GO(64, true); else GO(64, false); }
-  else { if (a.chosen) GO(128, true); else GO(128, false); }
-#undef GO
+  if (dh == 64) many_kernel<64><<<grid, kWaves * 64, 0, st>>>(a);
+  else many_kernel<128><<<grid, kWaves * 64, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -492,6 +492,43 @@ def test_chosen_pages_of_nan_in_blocks_of_128_rows(nova, G):
         assert (np.abs(_np(got) - ref[0])[other] <= t_out[other]).all()
 
 
+@pytest.mark.parametrize("H,hk,n,L,p,take", [(16, 8, 260, 1100, 16, 20), (24, 8, 200, 1500, 64, 12), (40, 8, 130, 900, 256, 2), (130, 2, 70, 700, 32, 15)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_sparse_in_blocks_of_128_rows_of_64_channels(nova, H, hk, n, L, p, take, causal):
+    B = max(1, 128 // (hk * -(-n * (H // hk) // 128)) + 1)
+    _check(nova, "bf16", B, H, hk, 64, p, n, L, take=take, causal=causal, lens=None if B == 1 else [L - 13 * (b % 3) if L - 26 >= n else L for b in range(B)])
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("G,n", [(1, 300), (3, 100), (20, 15)])
+def test_infinities_of_chosen_pages_in_blocks_of_128_rows(nova, dh, G, n):
+    """Infinities of both signs and NaN among the values of pages that some queries have chosen, some of them behind a query's own row: an
+    infinity shows with its sign, two of both signs and a NaN as NaN, and nothing of it in rows or channels that have none."""
+    B, hk, p, L, take = 3, 16, 32, 640, 6
+    cache, table = _fill("bf16", B, hk, p, dh, [L] * B, 20, 8)
+    g = np.random.default_rng(4)
+    chosen = np.stack([g.permutation(19)[:take] for _ in range(B * n * hk)]).reshape(B, n, hk, take)
+    chosen[:, :, :, 0] = np.where(g.random((B, n, hk)) < 0.5, 19, chosen[:, :, :, 0])
+    odd = (float("inf"), -float("inf"), float("nan"))
+    for b in range(B):
+        for i, (page, row) in enumerate([(2, 5), (2, 20), (7, 31), (11, 0), (19, 12), (19, 31), (18, 3)]):
+            for c, kind in ((3, 0), (dh - 1, 1), (17, i % 2), (40, i % 3)):
+                cache.v_pages[int(table[b, page]), i % hk:, row, c] = odd[kind]
+    q = torch.randn((B, n, hk * G, dh), generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    out, lse = _run(nova, cache, table, q, L, chosen=chosen, causal=True)
+    K, V = ([P.image_rows(_np(pool), table[b], L) for b in range(B)] for pool in (cache.k_pages, cache.v_pages))
+    with np.errstate(invalid="ignore"):
+        ref = P.attention(_np(q), K, V, dh ** -0.5, [n] * B, True, chosen, p)
+    got = _np(out)
+    assert (np.isnan(got) == np.isnan(ref[0])).all() and np.isnan(got).any()
+    for sign in (np.inf, -np.inf):
+        assert ((got == sign) == (ref[0] == sign)).all() and (got == sign).any()
+    fine = np.isfinite(ref[0])
+    ref = [np.where(np.isfinite(t), t, 0.0) for t in ref]
+    t_out, t_lse = _bounds(ref, "bf16", dh, take * p)
+    assert (np.abs(np.where(fine, got, 0.0) - ref[0]) <= t_out)[fine].all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hk,n,take", [(22, 96, 256), (1, 33, 256), (1, 1, 256)])
 def test_longest_lists_of_the_longest_page_lists(nova, dtype, hk, n, take):
