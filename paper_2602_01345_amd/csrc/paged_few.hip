@@ -1,6 +1,7 @@
 // Attention over a cache in pages, blocks of 16 or 32 rows (a row: a query of one of the heads that share a key head): single
 // tokens, a handful of queries, and queries that have chosen pages each for themselves.  What bounds it is reading the keys and
-// values once.
+// values once: a token of four images, 32 heads of 128 on 8, up to 32 768 rows, 386 MB, 72 us or 5.4 TB/s; 41 MB of fp32 (two images of
+// 2521 rows, 16 heads of 64, 5 queries) 13 us, which is the first latency and the joins.
 //
 // A workgroup is four or eight waves and one block of rows; tiles of keys are dealt to the waves, which share nothing until their results
 // are joined at the end, so no tile waits at a barrier.  A tile is made of groups of 16 keys; a group lies in one page, wherever a

@@ -7,6 +7,10 @@
 // A workgroup has up to 16 queries of one key head.  Scores on the matrix cores, 16 pages x 16 queries per MFMA, one after the other
 // for the heads that share the key head, their largest kept; as order-preserving 32-bit keys in LDS.  Then a wave per query: the
 // k-th largest key bit by bit, by counting, and the pages above it and the first of those that equal it, in ascending order.
+// What bounds it: the scalar units that count (two instructions per 64 keys and bit) for many queries, 1024 of 32 heads of 128 on 8 and 512
+// pages 32 us of which the scores' products are 3; for one the chain table, means, 32 bits, 13 us.  Registers are bounded so that two
+// workgroups share a CU, for some spills outside of the loops (bf16, heads of 128: 47 -> 37 us with the means; fp32 4000 queries, 16
+// heads of 128 171 -> 129, 1024 of 32 on 8 63 -> 62, but one token over four images 18.1 -> 21.3).
 #include <algorithm>
 
 #include "paged.h"
@@ -266,14 +270,19 @@ hipError_t launch_paged_select(hipStream_t st, const PagedSelect& s) {
   // as many queries as there are, and have room in a part of a CU's LDS
   a.queries = 16;
   while (a.queries > 1 && ((size_t)a.queries * a.row * 4 > 65536 || a.queries / 2 >= s.n)) a.queries /= 2;
+  // Keys a lane holds: the fewest that do (us with 4 / 8 / 16 / 32 of them: 1024 queries, 64 pages 25.6 / 30.2 / - / 57, 512 pages - /
+  // 36 / - / 63, 1024 pages - / - / 70 / 88; one query, 256 pages 13.8 / 15.0 / - / 23, 1024 pages - / - / 24 / 29).  Several waves per
+  // query only where one cannot hold its keys: they meet at a barrier for every bit (one query, 1024 pages, two waves 29 / one 24).
   a.sharing = 1;
   while (pages > a.sharing * kMostKeys * 64) a.sharing *= 2;     // 2048 pages per wave, 16384 in all
+  const int each = (pages + a.sharing - 1) / a.sharing;
   const dim3 grid((s.n + a.queries - 1) / a.queries, s.hk, s.B);
   const size_t lds = (size_t)a.queries * a.row * 4;
 #define GO(T, DH)                                                                                                 \
   do {                                                                                                            \
-    if (pages <= 256) select_kernel<T, DH, 4><<<grid, kWaves * 64, lds, st>>>(a);                                 \
-    else if (pages <= 512) select_kernel<T, DH, 8><<<grid, kWaves * 64, lds, st>>>(a);                            \
+    if (each <= 256) select_kernel<T, DH, 4><<<grid, kWaves * 64, lds, st>>>(a);                                  \
+    else if (each <= 512) select_kernel<T, DH, 8><<<grid, kWaves * 64, lds, st>>>(a);                             \
+    else if (each <= 1024) select_kernel<T, DH, 16><<<grid, kWaves * 64, lds, st>>>(a);                           \
     else select_kernel<T, DH, kMostKeys><<<grid, kWaves * 64, lds, st>>>(a);                                      \
   } while (0)
   if (s.dtype == NOVA_BF16) { if (s.dh == 64) GO(bf16_t, 64); else GO(bf16_t, 128); }
