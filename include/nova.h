@@ -492,8 +492,10 @@ int nova_pruned_block_fourbit(nova_ctx* ctx, void* stream, const nova_block_shap
  *   table              DEVICE int32 [B, pitch]: row r of image b is row r % page_rows of page table[b][r / page_rows].  Entries from
  *                      an image's last page on are not looked at; an entry that is no page of the pool reads as rows of zeros
  * page_rows is 16, 32, 64, 128 or 256, dh 64 or 128; pages * page_rows <= 2^30; heads that attend share a key head in runs of
- * heads / kv_heads.  Nothing reads what lies behind an image's rows.  Per-image arrays (..._per_row) are DEVICE int32 [B] or NULL,
- * clamped on the device like those of nova_pruned_block_rows; kv_len <= pitch * page_rows and <= 2^29.
+ * heads / kv_heads.  A page may be in several lists where it is only read (images with one beginning); nova_paged_reserve takes every
+ * page to be in one place, a list or the stack of free ones.  Nothing reads what lies behind an image's rows.  Per-image arrays
+ * (..._per_row) are DEVICE int32 [B] or NULL, clamped on the device like those of nova_pruned_block_rows; kv_len <= pitch * page_rows
+ * and <= 2^29.
  */
 typedef struct nova_paged_cache {
   void* k_pages;
@@ -529,7 +531,7 @@ int nova_paged_reserve(nova_ctx* ctx, void* stream, int B, int32_t* table, int p
 
 /* Rows k, v [B, n, kv_heads, dh] of the cache's dtype and any strides (rows of a projection's output, or the dense caches of
  * nova_pruned_block) to the slots [B, n]: one launch.  A slot outside [0, pages * page_rows) takes no row; two rows with one slot
- * leave either.  B * n < 2^27. */
+ * leave 16-byte pieces of either.  B * n < 2^27. */
 int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, int n, const nova_rows* k,
                       const nova_rows* v, const int32_t* slots);
 

@@ -638,6 +638,13 @@ def test_select(nova, dtype, dh, n, kv_len, p, k):
         _check_select(nova, dtype, 1, 11, 1, dh, p, n, kv_len, k, first=k // 2, recent=k - k // 2)
 
 
+@pytest.mark.parametrize("pages", [256, 257, 512, 513, 1024, 1025, 2048, 2049, 4096, 4097])
+def test_select_among_any_number_of_pages(nova, pages):
+    """A lane holds 4, 8, 16 or 32 keys; one wave, two or four choose for a query."""
+    _check_select(nova, "bf16", 1, 2, 1, 64, 16, 3, pages * 16 - 7, 20, causal=True)
+    _check_select(nova, "bf16", 1, 2, 2, 64, 16, 2, pages * 16, min(pages, 250), coarse=True)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("causal", [False, True])
 def test_select_with_ties(nova, dtype, causal):
