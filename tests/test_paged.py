@@ -529,6 +529,42 @@ def test_infinities_of_chosen_pages_in_blocks_of_128_rows(nova, dh, G, n):
     assert (np.abs(np.where(fine, got, 0.0) - ref[0]) <= t_out)[fine].all()
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 4.0])
+def test_scales_and_empty_images_of_chosen_pages_in_blocks_of_128_rows(nova, dh, scale):
+    """Scores of either sign and far apart; images without rows, of one row, and without queries; keys that are no numbers in rows that
+    some of the queries see, which leave the others' results alone."""
+    B, G, hk, n, p, L, take = 5, 2, 8, 150, 16, 400, 7
+    lens, counts = [L, 0, 1, L - 7, L], [n, n, n, 0, n - 31]
+    cache, table = _fill("bf16", B, hk, p, dh, lens, 25, 8)
+    g = np.random.default_rng(6)
+    chosen = np.stack([g.permutation(25)[:take] for _ in range(B * n * hk)]).reshape(B, n, hk, take)
+    q = torch.randn((B, n, hk * G, dh), generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+
+    def reference():
+        K, V = ([P.image_rows(_np(pool), table[b], lens[b]) for b in range(B)] for pool in (cache.k_pages, cache.v_pages))
+        with np.errstate(invalid="ignore"):
+            return P.attention(_np(q), K, V, scale, counts, True, chosen, p)
+
+    kw = dict(lens=lens, counts=counts, causal=True, scale=scale, chosen=chosen)
+    ref = reference()
+    _compare(*_run(nova, cache, table, q, L, **kw), ref, "bf16", dh, take * p)
+    for page, row, odd in ((3, 4, float("nan")), (24, 9, float("inf")), (20, 15, -float("inf"))):
+        cache.k_pages[int(table[0, page]), :, row, 5] = odd
+    out, lse = _run(nova, cache, table, q, L, **kw)
+    fine = np.ones((B, n, hk * G), bool)
+    see = np.repeat((chosen[0] == 3).any(-1) | ((chosen[0] == 24).any(-1) & (np.arange(n) + L - n >= 24 * p + 9)[:, None])
+                    | ((chosen[0] == 20).any(-1) & (np.arange(n) + L - n >= 20 * p + 15)[:, None]), G, 1)
+    fine[0] = ~see
+    assert fine[0].any() and see.any()
+    t_out, t_lse = _bounds(ref, "bf16", dh, take * p)
+    assert (np.abs(_np(out) - ref[0]) <= t_out)[fine].all()
+    empty = np.isneginf(ref[1])
+    assert (np.isneginf(_np(lse)) == empty)[fine].all()
+    assert (np.abs(np.where(empty, 0.0, _np(lse)) - np.where(empty, 0.0, ref[1])) <= t_lse)[fine & ~empty].all()
+    assert np.isnan(_np(out)[0][np.repeat((chosen[0] == 3).any(-1), G, 1)]).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hk,n,take", [(22, 96, 256), (1, 33, 256), (1, 1, 256)])
 def test_longest_lists_of_the_longest_page_lists(nova, dtype, hk, n, take):
