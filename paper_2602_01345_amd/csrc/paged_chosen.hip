@@ -7,7 +7,7 @@
 //   S^T = K Q^T    16 keys x 16 rows per MFMA, keys and channels from LDS by rows, the row's channels in registers
 //   O^T += V^T P^T the scores a lane holds after two S^T products are its operand as they are, values read transposed
 // Two stages of LDS, two workgroups per CU, so that the waves that have nothing to do in one tile leave the SIMD to others.
-// What bounds it is the longest wave's way through each tile: 1024 queries, 32 heads of 128 on 8, 32 of 512 pages each, take 252 us with
+// What bounds it is the longest wave's way through each tile: 1024 queries, 32 heads of 128 on 8, 32 of 512 pages each, take 247 us with
 // the join, of which 32 queries' unions (264 pages on average) loaded and nothing else are 145, and computed without a load 240.
 // Waves of 32 rows, which do 1.6 times as many tiles' rows in vain, take 324, tiles of 32 keys in four stages 341; masks by comparing
 // every key 280.
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void chosen_kernel(PagedArgs<bf16_t
     };
     // ---- scores: register r of group i is key 4 grp + r of it, for row col
     f32x4 s[4];
-    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_s_setprio(1);                         // others wait for it (through the tile 247 us, for the products alone 252, without 255)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -193,7 +193,6 @@ __global__ __launch_bounds__(kWaves * 64, 4) void chosen_kernel(PagedArgs<bf16_t
       for (int e = 0; e < KC; ++e) s[i] = mfma16(keys(i, e), qf[e], s[i]);
       if (i & 1) __builtin_amdgcn_sched_barrier(0);        // keys of two groups on their way at a time: registers
     }
-    __builtin_amdgcn_s_setprio(0);
     ahead();
     // What a row has not chosen has no weight: -inf in place of its reference, which leaves scores that are no numbers to the second time.
     const float dead = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
@@ -238,7 +237,6 @@ __global__ __launch_bounds__(kWaves * 64, 4) void chosen_kernel(PagedArgs<bf16_t
       probabilities();
     }
     l_run += psum;
-    __builtin_amdgcn_s_setprio(1);
     // ---- O^T += V^T P^T, 32 keys per MFMA
     bf16x8 pf[2];
 #pragma unroll

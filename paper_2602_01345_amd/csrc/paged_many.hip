@@ -6,8 +6,9 @@
 // A workgroup is four waves of 32 rows.  Tiles of 64 keys go from the pages into LDS without passing through registers, each wave its
 // 16 keys (which lie in one page, wherever pages end) of K and of V, a line per row, the swizzle made by which chunk of its row a lane
 // asks for.  Two stages of LDS, two workgroups per CU (three with heads of 64), so that one wave's softmax runs next to another's
-// MFMAs; a wave asks for priority while it issues MFMAs.  What bounds it is that and power: two images, 2048 queries behind 14 336 rows,
-// 32 heads of 128 on 8 (1.03 TFLOP) 957 to 1050 us by card, 1.0 to 1.08 PFLOP/s with the matrix cores busy 55 % of the cycles; 8 images of
+// MFMAs; a wave asks for priority while it issues MFMAs (below: 930 us; in the softmax instead 966, for the second product only 951; heads
+// of 64, 4 images of 1024 over 4096 172 / 199 / 172).  What bounds it is that and power: two images, 2048 queries behind 14 336 rows,
+// 32 heads of 128 on 8 (1.03 TFLOP) 930 to 1050 us by card, 1.0 to 1.1 PFLOP/s with the matrix cores busy 55 % of the cycles; 8 images of
 // 512, 36 heads of 64 (44 GFLOP) 65 to 70, where 32 exponentials stand next to 16 MFMAs.
 // A weight of 0 times a value that is no number is NaN, so what a row does not see could show in its result.  A workgroup whose sums
 // end as anything but finite numbers goes over its tiles again, and takes those with such values in them key by key.
