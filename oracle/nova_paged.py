@@ -132,7 +132,8 @@ def summarise(pool: np.ndarray, table: np.ndarray, means: np.ndarray, lens: Sequ
 
 def select(q: np.ndarray, means: np.ndarray, table: np.ndarray, page_rows: int, lens: Sequence[int], counts: Sequence[int], causal: bool,
            first: int, recent: int, k: int) -> np.ndarray:
-    """chosen [B, n, kv_heads, k]."""
+    """chosen [B, n, kv_heads, k]: the `first` and `recent` pages in any case, then pages with a mean of NaN, then by score; of two
+    alike the lower."""
     B, n, H, dh = q.shape
     pages, hk, _ = means.shape
     G = H // hk
@@ -148,9 +149,9 @@ def select(q: np.ndarray, means: np.ndarray, table: np.ndarray, page_rows: int, 
                 m = np.where(((ids >= 0) & (ids < pages))[:, None], means[np.clip(ids, 0, pages - 1), j], 0.0)
                 w = seven_bits(q[b, s, j * G:(j + 1) * G])
                 score = (np.where(np.isnan(w), 0.0, w) @ m.T).max(0)
-                score[np.isnan(m).any(1)] = np.inf
-                score[:first] = np.inf
-                score[max(P - recent, 0):] = np.inf
-                best = sorted(range(P), key=lambda i: (-score[i], i))[:k]
+                rank = np.where(np.isnan(m).any(1), 1, 2)
+                rank[:first] = 0
+                rank[max(P - recent, 0):] = 0
+                best = sorted(range(P), key=lambda i: (rank[i], -score[i] if rank[i] == 2 else 0.0, i))[:k]
                 chosen[b, s, j, :len(best)] = sorted(best)
     return chosen

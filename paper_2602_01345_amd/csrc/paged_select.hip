@@ -21,7 +21,8 @@ constexpr int kWaves = 8;
 constexpr int kHeads = 4;                // heads whose queries are held in registers at a time
 constexpr int kAhead = 2;                // groups of 16 pages whose means a wave asks for at a time
 constexpr int kMostKeys = 32;            // keys a lane holds while the k-th largest is looked for
-constexpr uint32_t kTaken = 0xFFFFFFFFu; // key of a page that is taken whatever its score; 0: one that the query does not see
+constexpr uint32_t kTaken = 0xFFFFFFFFu; // key of a page that is taken whatever its score (`first`, `recent`); 0: one that the query does not see
+constexpr uint32_t kOdd = 0xFFFFFFFEu;   // of a page with a mean of NaN: in front of every score, behind those that are taken
 
 struct SelectArgs {
   const void* q;
@@ -36,7 +37,7 @@ struct SelectArgs {
 
 __device__ __forceinline__ uint32_t score_key(float s) {
   uint32_t b = __float_as_uint(s);
-  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return kTaken;            // a page that holds a NaN or an infinity shows in the result
+  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return kOdd;              // a page that holds a NaN or an infinity shows in the result
   if (b == 0x80000000u) b = 0u;
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }

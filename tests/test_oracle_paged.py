@@ -70,3 +70,14 @@ def test_select_takes_ends_ties_and_pages_of_nan():
     assert sel(first=0, recent=0, k=8) == [0, 1, 2, 3, 4, 5, -1, -1]
     means[2] = np.nan
     assert sel(first=0, recent=0, k=2) == [2, 4]
+
+
+def test_pages_of_nan_come_behind_first_and_recent_ones():
+    """A page whose mean is NaN is chosen before any score, but takes no place of the `first` and `recent` ones."""
+    means = np.zeros((8, 1, 2))
+    means[:, 0, 0] = [0, 1, 2, 3, 4, 5, 6, 0]
+    means[2:5] = np.nan
+    table, q = np.arange(8)[None], np.array([[[[1.0, 0.0]]]])
+    sel = lambda **kw: P.select(q, means, table, 16, [128], [1], True, **kw)[0, 0, 0].tolist()
+    assert sel(first=1, recent=1, k=3) == [0, 2, 7] and sel(first=0, recent=2, k=2) == [6, 7] and sel(first=3, recent=1, k=4) == [0, 1, 2, 7]
+    assert sel(first=1, recent=1, k=6) == [0, 2, 3, 4, 6, 7]
