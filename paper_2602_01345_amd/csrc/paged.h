@@ -7,44 +7,39 @@
 constexpr float kNone = -3.40282347e38f;
 constexpr int kPageGroup = 16;           // rows that never lie in two pages: pages have 2^shift rows, 16 at least
 
-// A (page, key head)'s rows as a buffer: `rows` of them exist, loads from there on give zeros.  A page that is none of the pool
-// has no rows, so that no table leads a load out of it.
+// A (page, key head)'s rows from `row` on as the four words of a buffer for loads that go into LDS: `rows` of them exist, loads from
+// there on give zeros.  A page that is none of the pool has no rows, so that no table leads a load out of it.  Where the rows begin
+// stands in the buffer's base and never in a load's scalar offset: whether that one counts against the buffer's length, and what comes of
+// a length that is less than it, is not said alike everywhere.
 template <typename T, int DH>
-__device__ __forceinline__ auto page_buffer(const T* pool, int page, int pages, int hk, int j, int shift, int rows) {
+__device__ __forceinline__ u32x4 page_words(const T* pool, int page, int pages, int hk, int j, int shift, int row, int rows) {
   const bool there = (unsigned)page < (unsigned)pages;
-  const T* base = pool + ((((int64_t)(there ? page : 0) * hk + j) << shift) * DH);
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, there ? rows * (int)(DH * sizeof(T)) : 0, 0x00020000);
-}
-
-// The same as the four words of a buffer, for loads that go into LDS.  They are written in assembly: the compiler, which cannot tell
-// which LDS a transposed read may meet, would make every such read wait for all of them.  They have no output registers, and who
-// reads what they bring waits for vmcnt(0) and at a barrier first.
-template <typename T, int DH>
-__device__ __forceinline__ u32x4 page_words(const T* pool, int page, int pages, int hk, int j, int shift, int rows) {
-  const bool there = (unsigned)page < (unsigned)pages;
-  const uint64_t base = reinterpret_cast<uint64_t>(pool + ((((int64_t)(there ? page : 0) * hk + j) << shift) * DH));
+  const uint64_t base = reinterpret_cast<uint64_t>(pool + (((((int64_t)(there ? page : 0) * hk + j) << shift) + row) * DH));
   return u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, there ? rows * (uint32_t)(DH * sizeof(T)) : 0u, 0x00020000u};
 }
-// 16 bytes per lane from off + lane_off[e] (off, to: of the whole wave) to the e-th KB of LDS from `to` on.  The waits in front of the
+// Loads that go into LDS are written in assembly: the compiler, which cannot tell which LDS a transposed read may meet, would make every
+// such read wait for all of them.  They have no output registers, and who reads what they bring waits for vmcnt(0) and at a
+// barrier first.
+// 16 bytes per lane from lane_off[e] of the buffer to the e-th KB of LDS from `to` on (to: of the whole wave).  The waits in front of the
 // loads are those that the hardware asks for: five states after a vector instruction that wrote a scalar register which a load
 // reads (the compiler does not look for that here), one after a write of m0.
 template <int N>
-__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t to, const uint32_t (&lane_off)[N], uint32_t off) {
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t to, const uint32_t (&lane_off)[N]) {
   static_assert(N == 2 || N == 4 || N == 8, "");
   if constexpr (N == 8) {
-    load_to_lds(buffer, to, {lane_off[0], lane_off[1], lane_off[2], lane_off[3]}, off);
-    load_to_lds(buffer, to + 4096, {lane_off[4], lane_off[5], lane_off[6], lane_off[7]}, off);
+    load_to_lds(buffer, to, {lane_off[0], lane_off[1], lane_off[2], lane_off[3]});
+    load_to_lds(buffer, to + 4096, {lane_off[4], lane_off[5], lane_off[6], lane_off[7]});
   } else if constexpr (N == 4) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %5, %6 offen lds\n\t"
-                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, %6 offen lds\n\t"
-                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, %6 offen lds\n\t"
-                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, %6 offen lds"
-                 :: "s"(to), "v"(lane_off[0]), "v"(lane_off[1]), "v"(lane_off[2]), "v"(lane_off[3]), "s"(buffer), "s"(off)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
+                 :: "s"(to), "v"(lane_off[0]), "v"(lane_off[1]), "v"(lane_off[2]), "v"(lane_off[3]), "s"(buffer)
                  : "memory", "scc");
   } else {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %3, %4 offen lds\n\t"
-                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
-                 :: "s"(to), "v"(lane_off[0]), "v"(lane_off[1]), "s"(buffer), "s"(off) : "memory", "scc");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
+                 :: "s"(to), "v"(lane_off[0]), "v"(lane_off[1]), "s"(buffer) : "memory", "scc");
   }
 }
 

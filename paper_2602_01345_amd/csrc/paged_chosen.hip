@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void chosen_kernel(PagedArgs<bf16_t
     const int w = i + (wave & 3);
     const u32x4 buffer = {(uint32_t)__builtin_amdgcn_readlane((int)held.lo, w), (uint32_t)__builtin_amdgcn_readlane((int)held.hi, w),
                           (uint32_t)__builtin_amdgcn_readlane((int)held.bytes, w), 0x00020000u};
-    load_to_lds(buffer, lds0 + (t & 1) * STAGE, part, 0);
+    load_to_lds(buffer, lds0 + (t & 1) * STAGE, part);
   };
   auto begin = [&] {
     hold(t0);

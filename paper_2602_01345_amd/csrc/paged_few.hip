@@ -112,17 +112,21 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
 #pragma unroll
     for (int i = 0; i < TG; ++i) key0[i] = __builtin_amdgcn_readlane(g.key0, i);
   };
-  // a tile of one page is loaded through one buffer, otherwise each group through its own
+  // that of the group behind i - 1's: in a tile of one page 16 rows further on
   const bool one_page = gshift >= TG_SHIFT;
+  auto following = [&](u32x4 w, const T* pool, const Groups& g, int i) {
+    if (!one_page) return from(pool, g, i);
+    const uint64_t base = ((uint64_t)w[1] << 32 | w[0]) + 16 * ROWB;
+    return u32x4{(uint32_t)base, (uint32_t)(base >> 32), (uint32_t)__builtin_amdgcn_readlane(g.bytes, i), 0x00020000u};
+  };
   auto load_k = [&](const Groups& g) {
     u32x4 w = from(a.keys, g, 0);
 #pragma unroll
     for (int i = 0; i < TG; ++i) {
-      if (i > 0 && !one_page) w = from(a.keys, g, i);
+      if (i > 0) w = following(w, a.keys, g, i);
       const auto buffer = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)w[1] << 32 | w[0]), 0, w[2], w[3]);
-      const uint32_t at = one_page ? i * 16 * ROWB : 0;
 #pragma unroll
-      for (int e = 0; e < KC; ++e) kw[i][e] = __builtin_amdgcn_raw_buffer_load_b128(buffer, col * ROWB + (e * 4 + grp) * 16, at, 0);
+      for (int e = 0; e < KC; ++e) kw[i][e] = __builtin_amdgcn_raw_buffer_load_b128(buffer, col * ROWB + (e * 4 + grp) * 16, 0, 0);
     }
   };
   // bf16: the swizzle is made by which chunk of its row a lane asks for; fp32: rows as they are
@@ -138,8 +142,8 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
     u32x4 w = from(a.values, g, 0);
 #pragma unroll
     for (int i = 0; i < TG; ++i) {
-      if (i > 0 && !one_page) w = from(a.values, g, i);
-      load_to_lds(w, mine0 + stage * TILE + i * VG * 1024, part, one_page ? i * 16 * ROWB : 0);
+      if (i > 0) w = following(w, a.values, g, i);
+      load_to_lds(w, mine0 + stage * TILE + i * VG * 1024, part);
     }
   };
 

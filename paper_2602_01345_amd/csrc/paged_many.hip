@@ -80,14 +80,13 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 3 : 2) void many_kernel(Pag
     return __builtin_amdgcn_readlane(held, t - held_first);
   };
   auto request = [&](int t, int page) {
-    const int x = t * 4 + wave, u = x >> gshift;
-    const int there = x < groups ? min(max(len - (u << a.shift), 0), 1 << a.shift) : 0;
-    const uint32_t at = (x & gmask) * 16 * ROWB;
-    const u32x4 ks = page_words<bf16_t, DH>(a.keys, page, a.pages, a.hk, j, a.shift, there);
-    const u32x4 vs = page_words<bf16_t, DH>(a.values, page, a.pages, a.hk, j, a.shift, there);
+    const int x = t * 4 + wave, u = x >> gshift, at_row = (x & gmask) * 16;
+    const int there = x < groups ? min(max(len - (u << a.shift) - at_row, 0), (1 << a.shift) - at_row) : 0;
+    const u32x4 ks = page_words<bf16_t, DH>(a.keys, page, a.pages, a.hk, j, a.shift, at_row, there);
+    const u32x4 vs = page_words<bf16_t, DH>(a.values, page, a.pages, a.hk, j, a.shift, at_row, there);
     const uint32_t to = lds0 + (t & 1) * STAGE + wave * 16 * ROWB;
-    load_to_lds(ks, to, part, at);
-    load_to_lds(vs, to + HALF, part, at);
+    load_to_lds(ks, to, part);
+    load_to_lds(vs, to + HALF, part);
   };
 
   hold(t0);

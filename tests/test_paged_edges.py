@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from oracle import nova_paged as P
-from test_paged import _ints, _np
+from paper_2602_01345_amd import PagedCache
+from test_paged import DTYPES, _compare, _fill, _ints, _np, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +46,50 @@ def test_pages_of_nan_take_no_place_of_first_and_recent_ones(nova, dtype, pages,
         sees = -(-(L - n + s + 1 if causal else L) // p)
         for j in range(hk):
             assert set(range(first)) | set(range(max(sees - recent, 0), sees)) <= set(got[0, s, j].tolist())
+
+
+# ---- tables with entries that are no pages ------------------------------------------------------------------------------
+NONE = (-1, 2 ** 31 - 1, -2 ** 31, 1 << 20)                      # and the number of pages itself
+
+
+def _choose(B, n, hk, take, pages, seed):
+    g = np.random.default_rng(seed)
+    return np.sort(np.stack([g.permutation(pages)[:take] for _ in range(B * n * hk)]).reshape(B, n, hk, take), axis=-1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("p", [16, 32, 64, 256])
+@pytest.mark.parametrize("n,H,hk,B,take", [(1, 4, 2, 1, 0), (5, 4, 2, 1, 0), (33, 2, 2, 2, 0), (140, 4, 2, 1, 0), (5, 4, 2, 1, 3), (40, 2, 2, 1, 3),
+                                           (200, 16, 16, 3, 4)])
+def test_entries_that_are_no_pages_read_as_zeros_in_every_kernel(nova, dtype, dh, p, n, H, hk, B, take):
+    """Blocks of 16, 32 and 128 rows, tiles of one page and of several, chosen pages in each."""
+    L = max(6 * p - 9, 300)
+    print(f"paged, entries that are none: {dtype} dh={dh} p={p} n={n} H={H}/{hk} B={B} take={take}", flush=True)
+    cache, table = _fill(dtype, B, hk, p, dh, [L] * B, -(-L // p) + 1, 5)
+    pages = -(-L // p)
+    for b in range(B):
+        for i in range(b % 2, pages, 2):
+            table[b, i] = (*NONE, cache.k_pages.shape[0])[(i + b) % 5]
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(5)).to(DTYPES[dtype]).cuda()
+    chosen = _choose(B, n, hk, take, pages, 3) if take else None
+    K, V = ([P.image_rows(_np(pool), table[b], L) for b in range(B)] for pool in (cache.k_pages, cache.v_pages))
+    for causal in (False, True):
+        out, lse = _run(nova, cache, table, q, L, causal=causal, chosen=chosen)
+        _compare(out, lse, P.attention(_np(q), K, V, dh ** -0.5, [n] * B, causal, chosen, p), dtype, dh, L)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("p", [16, 64, 256])
+@pytest.mark.parametrize("n,hk,B,take", [(1, 2, 1, 0), (5, 2, 1, 0), (140, 2, 1, 0), (5, 2, 1, 3), (200, 16, 3, 4)])
+def test_pools_without_pages(nova, dtype, p, n, hk, B, take):
+    """Every row is zeros: every query the mean of nothing, and the logarithm of how many rows it sees."""
+    dh, L = 128, 6 * p - 9 if p > 16 else 300
+    print(f"paged, no pages at all: {dtype} p={p} n={n} hk={hk} B={B} take={take}", flush=True)
+    pages = -(-L // p)
+    table = np.array([[(*NONE, 0)[(i + b) % 5] for i in range(pages)] for b in range(B)])
+    q = torch.randn((B, n, hk, dh), generator=torch.Generator().manual_seed(5)).to(DTYPES[dtype]).cuda()
+    chosen = _choose(B, n, hk, take, pages, 3) if take else None
+    K = [np.zeros((hk, L, dh))] * B
+    out, lse = _run(nova, PagedCache.empty(0, hk, p, dh, DTYPES[dtype]), table, q, L, chosen=chosen)
+    _compare(out, lse, P.attention(_np(q), K, K, dh ** -0.5, [n] * B, False, chosen, p), dtype, dh, L)
