@@ -69,6 +69,17 @@ struct PagedArgs : AttentionItems<T> {
   }
 };
 
+// Query s of image b, which sees `visible` keys, has chosen a page with some of them.  Asked only of queries whose weights sum to 0: scores
+// that are all -inf leave that too, and a result that is no number, as they do where nothing is chosen.
+template <typename T>
+__device__ __forceinline__ bool sees_chosen(const PagedArgs<T>& a, int b, int j, int s, int visible) {
+  const int32_t* chosen = a.chosen + (((int64_t)b * a.n + s) * a.hk + j) * a.take;
+  const unsigned npages = (unsigned)(visible + (1 << a.shift) - 1) >> a.shift;
+  for (int i = 0; i < a.take; ++i)
+    if ((unsigned)chosen[i] < npages) return true;
+  return false;
+}
+
 // The larger of a lane's number and that of the lane 32, or 16, away, on the vector unit.
 __device__ __forceinline__ float max_across_32(float v) {
   const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);

@@ -23,7 +23,8 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
   const bool there = a.n_whole + ci < a.items && row < a.n * a.G;
   const int count = image_count(a.n_rows, b, a.n), len = image_prior(a.kv_rows, b, a.P);
   const int s_row = div_by(there ? row : 0, a.G, a.G_inv, g_unused);
-  bool some = there && s_row < count && visible_keys(a.causal, len, count, s_row) > 0;
+  const int visible = visible_keys(a.causal, len, count, s_row);
+  bool some = there && s_row < count && visible > 0;
   const int64_t p0 = (int64_t)ci * a.nsplit * block_rows + rr;
   float m = kNone, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs<T> a, int block_row
     }
   }
   if (!there) return;
-  if (a.chosen && l == 0.f) some = false;                        // the query has chosen no page that it sees
+  if (a.chosen && l == 0.f) some = some && sees_chosen(a, b, j, s_row, visible);
   const int64_t to = a.out_row(b, j, row);
   store_four(a.out + to * DH + c4 * 4, some ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, some ? 1.0f / l : 0.f);
   if (a.lse && c4 == 0) a.lse[to] = some ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;

@@ -298,7 +298,12 @@ __global__ __launch_bounds__(kWaves * 64, 4) void chosen_kernel(PagedArgs<bf16_t
   float l = l_run + __shfl_xor(l_run, 16, NOVA_WAVE);
   l += __shfl_xor(l, 32, NOVA_WAVE);
   if (nparts == 1) {
-    const bool some = row < live && seen > 0 && l != 0.f;
+    bool some = row < live && seen > 0;
+    if (__builtin_expect(l == 0.f, 0)) {
+      int again = row;
+      asm("" : "+v"(again));                               // divided once more: the quotient would be held through the loop
+      some = some && sees_chosen(a, b, j, div_by(again, a.G, a.G_inv, unused), seen);
+    }
     const int64_t to = a.out_row(b, j, row);
     const float inv = some ? 1.0f / l : 0.f;
 #pragma unroll

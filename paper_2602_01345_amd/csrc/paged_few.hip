@@ -440,8 +440,9 @@ __global__ __launch_bounds__(NW * 64, 2) void few_kernel(PagedArgs<T> a) {
         acc += f * *reinterpret_cast<const f32x4*>(lds + w * MINE + (c4 * 16 + rr) * 16);
       }
       if (nparts == 1) {
-        const int s = div_by(row, a.G, a.G_inv, g_unused);
-        const bool some = row < live && visible_keys(a.causal, len, count, s) > 0 && !(CHOSEN && lt == 0.f);
+        const int s = div_by(row, a.G, a.G_inv, g_unused), visible = visible_keys(a.causal, len, count, s);
+        bool some = row < live && visible > 0;
+        if (CHOSEN && lt == 0.f) some = some && sees_chosen(a, b, j, s, visible);
         const int64_t to = a.out_row(b, j, row);
         store_four(a.out + to * DH + c4 * 4, some ? acc : f32x4{0.f, 0.f, 0.f, 0.f}, some ? 1.0f / lt : 0.f);
         if (a.lse && c4 == 0) a.lse[to] = some ? (m + __builtin_amdgcn_logf(lt)) * kLn2 : -INFINITY;

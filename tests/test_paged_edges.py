@@ -93,3 +93,51 @@ def test_pools_without_pages(nova, dtype, p, n, hk, B, take):
     K = [np.zeros((hk, L, dh))] * B
     out, lse = _run(nova, PagedCache.empty(0, hk, p, dh, DTYPES[dtype]), table, q, L, chosen=chosen)
     _compare(out, lse, P.attention(_np(q), K, K, dh ** -0.5, [n] * B, False, chosen, p), dtype, dh, L)
+
+
+# ---- scores that are all -inf -------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n,H,hk,B,L,take", [(1, 2, 2, 1, 300, 4), (1, 4, 2, 2, 4000, 40), (5, 4, 2, 1, 600, 3), (40, 4, 2, 1, 900, 6),
+                                             (200, 16, 16, 3, 640, 12), (200, 32, 16, 9, 640, 12)])
+def test_scores_of_minus_infinity_over_chosen_pages(nova, dtype, dh, n, H, hk, B, L, take):
+    """The softmax of nothing but -inf is no number, over chosen pages as over all rows; not to have chosen anything gives zeros."""
+    p = 16
+    print(f"paged, scores of -inf: {dtype} dh={dh} n={n} H={H}/{hk} B={B} L={L} take={take}", flush=True)
+    pages = -(-L // p)
+    cache, table = _fill(dtype, B, hk, p, dh, [L] * B, pages, 6)
+    g = np.random.default_rng(7)
+    dead = np.sort(g.permutation(pages)[:pages // 2])            # pages with keys of -inf in a channel where queries are positive
+    for b in range(B):
+        cache.k_pages[_ints(table[b, dead]).long(), :, :, 9] = -float("inf")
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(5)).to(DTYPES[dtype]).cuda()
+    q[..., 9] = q[..., 9].abs() + 0.5
+    live = np.setdiff1d(np.arange(pages), dead)
+    chosen = np.full((B, n, hk, take), -1)
+    kind = g.integers(0, 3, (B, n, hk))                          # nothing, dead pages alone, both
+    kind[0, 0] = np.arange(hk) % 3 + 1 if n > 1 else [1, 2][:hk]
+    kind = np.where(kind == 3, 0, kind)
+    for at in np.ndindex(B, n, hk):
+        if kind[at]:
+            m = take if kind[at] == 1 else take // 2
+            c = g.permutation(dead)[:m]
+            chosen[at][:len(c)] = c
+        if kind[at] == 2:
+            c = g.permutation(live)[:take - take // 2]
+            chosen[at][take - len(c):] = c
+    out, lse = _run(nova, cache, table, q, L, chosen=chosen)
+    K, V = ([P.image_rows(_np(pool), table[b], L) for b in range(B)] for pool in (cache.k_pages, cache.v_pages))
+    for b in range(B):                                           # what a query has chosen and can weigh: the live pages
+        K[b][:, np.isin(np.arange(L) // p, dead)] = 0.0
+    ref = P.attention(_np(q), K, V, dh ** -0.5, [n] * B, False, np.where(np.isin(chosen, live), chosen, -1), p)
+    kind = kind.repeat(H // hk, 2)
+    got, glse = _np(out), _np(lse)
+    assert np.isnan(got[kind == 1]).all() and np.isneginf(glse[kind == 1]).all() and (kind == 1).any()
+    nan = torch.from_numpy(kind == 1).cuda()
+    out[nan] = 0.0
+    _compare(out, lse, ref, dtype, dh, L)
+    # over all rows, where nothing else is
+    for b in range(B):
+        cache.k_pages[_ints(table[b]).long(), :, :, 9] = -float("inf")
+    out, lse = _run(nova, cache, table, q, L)
+    assert torch.isnan(out).all() and torch.isneginf(lse).all()
