@@ -541,10 +541,11 @@ int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache
  *   out[b, s, h] = sum_j softmax_j(scale * <q[b, s, h], K[b, g, j]>) V[b, g, j],  g = h / (heads / kv_heads),
  * over all rows j of the image (causal 0), or (causal 1) over j <= kv_len_per_row[b] - n_per_row[b] + s.
  *   q          [B, n, heads, dh] of the cache's dtype, stride_channel 1, every other stride a multiple of 16 bytes, 16-byte aligned
- *   out        out [B, n, heads, dh] dense, 16-byte aligned; must not alias q
+ *   out        out [B, n, heads, dh] dense, 16-byte aligned
  *   lse        out fp32 [B, n, heads] or NULL: ln of the sum of e^(scale * score)
  *   workspace  of at least nova_paged_attention_workspace_bytes, 16-byte aligned (may be NULL where that is 0); calls that overlap,
  *              captured graphs among them, need one each.  0 bytes for sizes that the call refuses
+ * No two of out, lse, the workspace (as far as it is needed) and the rows of q may share memory (out may lie between rows of q).
  * B * heads * n <= 2^30, B * kv_heads * ceil(n * heads / kv_heads / 16) < 2^24, B <= 65535.  Queries past n_per_row[b], and queries
  * that see no row, get zeros and lse = -inf; one whose scores are all -inf NaN and lse = -inf.  A row that a query does not see has no part in its result, whatever its key and value are (NaN among them).  NOVA_F32: products of fp32
  * numbers, summed in fp32; NOVA_BF16: probabilities are rounded to bf16 in front of the second product.

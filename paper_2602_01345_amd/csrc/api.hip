@@ -61,7 +61,7 @@ inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr
 
 // Two arrays share a byte.
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  if (!a || !b) return false;
+  if (!a || !b || na == 0 || nb == 0) return false;
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
 }
@@ -108,6 +108,30 @@ nova_rows settled(const nova_rows& r, int B, int n, int heads) {
   if (n <= 1) s.stride_row = 0;
   if (heads <= 1) s.stride_head = 0;
   return s;
+}
+
+// Some of the rows [B, n, heads, dh] (channels side by side, strides settled) lies in the bytes [at, at + bytes).  Dimensions from the
+// longest stride down: of the parts of one that reach the bytes a second one begins there, a single one is looked into.  Rows that lie
+// over one another count as filling what they span.
+bool rows_overlap(const nova_rows& r, int dtype, int B, int n, int heads, int dh, const void* at, size_t bytes) {
+  if (!at || bytes == 0) return false;
+  typedef __int128 wide;                                         // extents and strides of 30 and 40 bits
+  const wide e = (wide)esize(dtype), from = (wide)reinterpret_cast<uintptr_t>(at), to = from + (wide)bytes;
+  struct Dim { wide stride; int64_t extent; } dim[3] = {{r.stride_b * e, B}, {r.stride_row * e, n}, {r.stride_head * e, heads}};
+  std::sort(dim, dim + 3, [](const Dim& x, const Dim& y) { return x.stride > y.stride; });
+  wide base = (wide)reinterpret_cast<uintptr_t>(r.data), span = dh * e;
+  for (const Dim& d : dim) span += (d.extent - 1) * d.stride;
+  for (const Dim& d : dim) {
+    if (base >= to || base + span <= from) return false;
+    span -= (d.extent - 1) * d.stride;
+    if (d.stride == 0) continue;
+    if (span > d.stride) return true;
+    const wide first = from < base + span ? 0 : (from - base - span) / d.stride + 1;       // the first part that ends behind `from`
+    if (first >= d.extent || base + first * d.stride >= to) return false;
+    if (first + 1 < d.extent && base + (first + 1) * d.stride < to) return true;
+    base += first * d.stride;
+  }
+  return base < to && base + span > from;
 }
 
 // n queries per image of `heads` heads over kv_len rows of a cache: at most 2^30 queries of one head in all, looked at factor by
@@ -193,12 +217,18 @@ int paged_attend(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int
   if (B == 0 || n == 0) return NOVA_OK;
   if (!q) return NOVA_ERR_INVALID_ARG;
   if (int rc = rows_error(q, cache->dtype, B, n, heads, true)) return rc;
-  if (!out || !aligned16(out) || out == q->data) return NOVA_ERR_INVALID_ARG;
+  if (!out || !aligned16(out)) return NOVA_ERR_INVALID_ARG;
+  // what some workgroups write while others still read
+  const nova_rows queries = settled(*q, B, n, heads);
+  auto among_queries = [&](const void* at, size_t bytes) { return rows_overlap(queries, cache->dtype, B, n, heads, cache->dh, at, bytes); };
+  const size_t each = (size_t)B * n * heads, outs = each * cache->dh * esize(cache->dtype), lses = each * 4;
+  if (overlap(out, outs, lse, lses) || among_queries(out, outs) || among_queries(lse, lses)) return NOVA_ERR_INVALID_ARG;
   const size_t need = paged_workspace(cache, B, heads, n, kv_len, k);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace))) return NOVA_ERR_WORKSPACE;
+  if (overlap(out, outs, workspace, need) || overlap(lse, lses, workspace, need) || among_queries(workspace, need)) return NOVA_ERR_INVALID_ARG;
   const DeviceScope device(ctx);
   if (device.rc) return device.rc;
-  const PagedCall call = {cache, B, table, pitch, heads, n, settled(*q, B, n, heads), n_per_row, kv_len, kv_len_per_row, causal,
+  const PagedCall call = {cache, B, table, pitch, heads, n, queries, n_per_row, kv_len, kv_len_per_row, causal,
                           scale * kAttnLog2e, chosen, k, out, lse, workspace};
   return launch_paged_attention(static_cast<hipStream_t>(stream), call) == hipSuccess ? NOVA_OK : NOVA_ERR_HIP;
 }

@@ -215,3 +215,55 @@ def test_binding_looks_at_shapes_and_types():
         PagedCache(t, t).c_struct()                              # not on a device
     c = PagedCache.empty(3, 2, 32, 128, device="cpu")
     assert c.page_rows == 32 and c.k_pages.dtype == torch.bfloat16 and c.v_pages.shape == (3, 2, 32, 128)
+
+
+def _query_rows(rng, B, n, heads, dh):
+    """Rows in some order of dimensions, one inside the other, with room between them; where each row of channels begins, in bytes."""
+    order, stride, span = rng.sample(range(3), 3), [0, 0, 0], dh
+    for i in order:
+        stride[i] = span + 8 * rng.choice((0, 0, 1, 20, 300))
+        span = stride[i] * ((B, n, heads)[i] - 1) + span
+    at = BASE * 40
+    begins = [at + 2 * (b * stride[0] + s * stride[1] + h * stride[2]) for b in range(B) for s in range(n) for h in range(heads)]
+    return _rows(heads=heads, stride_b=stride[0], stride_row=stride[1], stride_head=stride[2]), begins, 2 * span
+
+
+def test_results_may_lie_between_the_rows_of_queries_but_not_among_them(lib):
+    """out, and the logarithms, at places in and about the queries: refused where a byte is shared, and only there.  (What is not refused
+    for that ends at a workspace that is too small.)"""
+    import random
+    rng, met = random.Random(3), {INVALID: 0, WORKSPACE: 0}
+    c = _cache(pages=1000)
+    for _ in range(3000):
+        B, n, heads, dh = rng.randint(1, 3), rng.randint(1, 4), rng.choice((2, 4)), 64
+        assert lib.nova_paged_attention_workspace_bytes(C.byref(c), B, heads, n, 4000) > 0
+        q, begins, span = _query_rows(rng, B, n, heads, dh)
+        outs, lses = B * n * heads * dh * 2, B * n * heads * 4
+        for kw, bytes_ in ((dict(out=BASE * 40 + 16 * rng.randint(-outs // 16 - 2, span // 16 + 2)), outs),
+                           (dict(lse=BASE * 40 + 4 * rng.randint(-lses // 4 - 2, span // 4 + 2)), lses)):
+            at, = kw.values()
+            rc = INVALID if any(x < at + bytes_ and at < x + 2 * dh for x in begins) else WORKSPACE
+            assert _attend(lib, cache=c, pitch=250, B=B, n=n, heads=heads, q=q, kv_len=4000, ws=0, ws_bytes=0, **kw) == rc, (q.stride_b, kw)
+            met[rc] += 1
+    assert min(met.values()) > 1000
+
+
+@pytest.mark.parametrize("call", [_attend, _sparse])
+def test_results_that_share_memory(lib, call):
+    c = _cache(pages=1000)
+    kw = dict(cache=c, pitch=250, kv_len=4000)
+    need = lib.nova_paged_attention_workspace_bytes(C.byref(c), 2, 4, 3, 4000) if call is _attend else \
+        lib.nova_paged_sparse_attention_workspace_bytes(C.byref(c), 2, 4, 3, 4000, 4)
+    outs = 2 * 3 * 4 * 64 * 2
+    assert call(lib, lse=BASE * 8 + outs - 4, **kw) == INVALID and call(lib, lse=BASE * 8 - 92, **kw) == INVALID
+    q = BASE * 40
+    assert call(lib, out=q + 16, **kw) == INVALID and call(lib, out=q - outs + 16, **kw) == INVALID and call(lib, lse=q + outs - 4, **kw) == INVALID
+    # one query for all: its only row is what is read
+    one = _rows(heads=4, stride_b=0, stride_row=0, stride_head=0)
+    assert call(lib, q=one, out=q + 112, **kw) == INVALID and call(lib, q=one, out=q - outs + 16, **kw) == INVALID
+    # rows that overlap one another
+    assert call(lib, q=_rows(heads=4, stride_b=64, stride_row=32, stride_head=8), out=q + 64, **kw) == INVALID
+    if need:
+        assert call(lib, ws=BASE * 8 + outs - 16, **kw) == INVALID and call(lib, ws=q + outs - 16, **kw) == INVALID
+        assert call(lib, ws=BASE * 9 - need + 16, lse=BASE * 9, **kw) == INVALID
+        assert call(lib, q=one, out=q + 128, ws=0, **kw) == WORKSPACE
