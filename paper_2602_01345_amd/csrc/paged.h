@@ -191,5 +191,6 @@ hipError_t launch_paged_few(hipStream_t st, int dh, int mt, int waves, unsigned 
 constexpr int kPagedRows = 128;
 hipError_t launch_paged_many(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a);
 
-// paged_chosen.hip: the same, chosen pages
+// paged_chosen.hip: the same, chosen pages.  LDS besides the list: two stages of keys and of values, a word per wave
+constexpr int paged_chosen_lds(int dh) { return 2 * 2 * 64 * dh * 2 + 8 * 4; }
 hipError_t launch_paged_chosen(hipStream_t st, int dh, unsigned grid, const PagedArgs<bf16_t>& a);

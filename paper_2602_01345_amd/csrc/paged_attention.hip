@@ -72,6 +72,7 @@ struct Plan {
   int64_t runs() const { return nsplit > 1 ? (int64_t)(items - n_whole) * nsplit : 0; }
 };
 constexpr int kCus = 256;
+constexpr size_t kMostList = 160 * 1024 / 2 - paged_chosen_lds(128);
 constexpr int kRanked = 32;          // most images that are ranked: every workgroup does it for itself, a step per image
 Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int take, bool ragged) {
   const int G = heads / c.kv_heads, rows = n * G;
@@ -90,8 +91,10 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   //          256 keys 9.5 / 9.2, 512 12.0 / 17.4, 1024 17.0 / 21.9, 2048 26.7 / 29.0, 4096 47.3 / 41.5; 4 images of 256, 16 heads of 128:
   //          256 16.4 / 12.9, 512 20.9 / 22.6, 1024 30.7 / 30.0, 2048 47.9 / 38.8)
   //   bf16, chosen pages   128 (paged_chosen.hip) where the lists of a block's queries together hold half as many pages as there are, so
-  //          that they share some, if there are blocks for a quarter of the CUs and the list leaves room for a second workgroup in the
-  //          LDS (us in blocks of 32 / of 128; 32 heads of 128 on 8, 1024 queries, of 512 pages 128 chosen 853 / 439, 32 352 / 252, 8
+  //          that they share some, if there are blocks for a quarter of the CUs and the list leaves room for a second workgroup with
+  //          heads of 128 in the LDS (16 heads of 128, 1024 queries, 32 of so many pages of 16 rows: 732 106 / 102, 736, whose list does not,
+  //          100 / 159; heads of 64 have room for longer ones, which gain with long pages alone: 1024 pages of 16 rows 69 / 88, of 64 295 /
+  //          263, 2048 of 16 78 / 105) (us in blocks of 32 / of 128; 32 heads of 128 on 8, 1024 queries, of 512 pages 128 chosen 853 / 439, 32 352 / 252, 8
   //          113 / 107, 4 60 / 64; 4 images of 64, 8 of 128 pages, 64 blocks of 128, 39 / 45; 2 of 500, 12 heads on 4, 20 of 256 pages, 96
   //          blocks, 74 / 67; 16 heads of 64, 2000 queries, 32 of 256 pages 224 / 174); 16 where blocks are few (in blocks of 16 / of 32;
   //          32 heads of 128 on 8, 2 images of 20 queries, 16 of 512 pages 25 / 31; 128 queries, 32 of 512 66 / 62)
@@ -103,7 +106,7 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   else
     p.mt = heads_all * ((rows + kPagedRows - 1) / kPagedRows) > kCus / 4 &&
            2 * (int64_t)std::min((kPagedRows - 1) / G + 2, n) * take >= (int64_t)pages &&
-           chosen_bytes(pages, listed(kPagedRows), kPagedRows / 32) <= 16384 ? 0 : 2;
+           chosen_bytes(pages, listed(kPagedRows), kPagedRows / 32) <= kMostList ? 0 : 2;
   p.block_rows = p.mt ? 16 * p.mt : kPagedRows;
   p.blocks = (rows + p.block_rows - 1) / p.block_rows;
   p.items = B * c.kv_heads * p.blocks;

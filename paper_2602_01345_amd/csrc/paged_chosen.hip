@@ -39,6 +39,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void chosen_kernel(PagedArgs<bf16_t
   constexpr int NL = 16 * ROWB / 1024, RPL = 1024 / ROWB;  // loads of 16 rows, rows per load
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
   __shared__ uint32_t odd_waves[kWaves];
+  static_assert(sizeof(lds) + sizeof(odd_waves) == paged_chosen_lds(DH), "");
   extern __shared__ uint32_t lists[];
 
   const int tid = threadIdx.x, lane = tid & 63;

@@ -141,3 +141,38 @@ def test_scores_of_minus_infinity_over_chosen_pages(nova, dtype, dh, n, H, hk, B
         cache.k_pages[_ints(table[b]).long(), :, :, 9] = -float("inf")
     out, lse = _run(nova, cache, table, q, L)
     assert torch.isnan(out).all() and torch.isneginf(lse).all()
+
+
+# ---- divisions of large calls ---------------------------------------------------------------------------------------------
+def _check_some(nova, B, H, hk, dh, p, n, kv_len, lens=None, counts=None, causal=False, take=0, seed=1, dtype="bf16"):
+    """A large call, held against the oracle at some queries of every image: the first and last row of blocks of 128 rows, the last live
+    one, some others.  What has no query is zeros."""
+    print(f"paged attention, large: B={B} H={H}/{hk} dh={dh} p={p} n={n} kv_len={kv_len} lens={lens} counts={counts} causal={causal} "
+          f"take={take}", flush=True)
+    real, live = lens or [kv_len] * B, counts or [n] * B
+    cache, table = _fill(dtype, B, hk, p, dh, real, -(-kv_len // p), seed)
+    q = torch.randn((B, n, H, dh), generator=torch.Generator().manual_seed(seed)).to(DTYPES[dtype]).cuda()
+    g = np.random.default_rng(seed)
+    chosen = None
+    if take:
+        pages = -(-kv_len // p)
+        chosen = np.sort(np.argpartition(g.random((B, n, hk, pages), dtype=np.float32), take - 1)[..., :take], axis=-1)
+    out, lse = _run(nova, cache, table, q, kv_len, lens, counts, causal, None, chosen)
+    assert torch.isfinite(out).all()
+    G, pools, queries = H // hk, [_np(cache.k_pages), _np(cache.v_pages)], _np(q)
+    for b in range(B):
+        assert (out[b, live[b]:] == 0).all() and torch.isneginf(lse[b, live[b]:]).all()
+        rows = {0, n * G - 1, live[b] * G - 1, *(128 * g.integers(0, n * G // 128, 3)), *(128 * g.integers(1, n * G // 128, 3) - 1), *g.integers(0, n * G, 4)}
+        for row in sorted(int(r) for r in rows if r >= 0):
+            s, h = row // G, int(g.integers(0, hk)) * G + row % G
+            sees = int(P.visible(real[b], live[b], n, causal)[s])
+            K, V = ([P.image_rows(pool[:, h // G:h // G + 1], table[b], real[b])[:, :sees]] for pool in pools)
+            one = None if chosen is None else chosen[b:b + 1, s:s + 1, h // G:h // G + 1]
+            ref = P.attention(queries[b:b + 1, s:s + 1, h:h + 1], K, V, dh ** -0.5, [1 if s < live[b] else 0], False, one, p)
+            _compare(out[b:b + 1, s:s + 1, h:h + 1], lse[b:b + 1, s:s + 1, h:h + 1], ref, dtype, dh, kv_len)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("pages", [720, 732, 736, 900])
+def test_lists_about_what_leaves_room_for_a_second_workgroup(nova, dh, pages):
+    _check_some(nova, 1, 16, 16, dh, 16, 600, pages * 16 - 5, take=16, causal=True)
