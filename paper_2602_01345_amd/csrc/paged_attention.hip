@@ -143,7 +143,8 @@ Plan plan(const nova_paged_cache& c, int B, int heads, int n, int kv_len, int ta
   if (rest == 0 || (p.ranked && p.items >= 2 * slots)) return p;
   // A few more items than CUs, and long ones: most CUs would have one, which is little to hide anything behind, and the others two
   // (us in three runs each / whole; 272 items of 8000 keys, heads of 128, 174 / 201, 306 186 / 230, 280 of 16 000 318 / 399; heads of 64,
-  // of which three items share a CU: 272 of 4096 72 / 71).
+  // of which three items share a CU: 272 of 4096 72 / 71; chosen pages, heads of 128: 272 items, 32 of 512 pages of 64 rows 462 / 636, of
+  // 16 rows 186 / 206, 8 of 512 of 64 248 / 301, 304 items, 32 of 256 of 64 315 / 411, 320, 16 of 128 of 64 187 / 215).
   const bool in_three = c.dh == 128 && p.items > kCus && p.items <= kCus + kCus / 4 && ntiles >= 64;
   const int s = in_three ? 3 : std::min(slots / rest, ntiles / 4);
   if (s >= 2) {

@@ -172,6 +172,33 @@ def _check_some(nova, B, H, hk, dh, p, n, kv_len, lens=None, counts=None, causal
             _compare(out[b:b + 1, s:s + 1, h:h + 1], lse[b:b + 1, s:s + 1, h:h + 1], ref, dtype, dh, kv_len)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,H,hk,n,kv_len,lens,counts", [(1, 16, 16, 2170, 4100, None, None), (2, 8, 8, 2170, 4100, [4100, 2200], None),
+                                                         (3, 32, 4, 400, 4200, [400, 4200, 90], [400, 350, 90]), (2, 10, 10, 2000, 4160, [100, 4160], [0, 1999])])
+def test_a_few_more_items_than_cus_in_three_runs(nova, B, H, hk, n, kv_len, lens, counts, causal):
+    """257 to 320 blocks of 128 rows with heads of 128 over 64 tiles or more; images of which some runs have nothing."""
+    assert 256 < B * hk * -(-n * (H // hk) // 128) <= 320
+    _check_some(nova, B, H, hk, 128, 64, n, kv_len, lens, counts, causal)
+
+
+@pytest.mark.parametrize("H,hk,n,pages,take", [(16, 16, 2150, 300, 20), (32, 8, 1080, 512, 16)])
+def test_chosen_pages_in_three_runs(nova, H, hk, n, pages, take):
+    assert 256 < hk * -(-n * (H // hk) // 128) <= 320
+    _check_some(nova, 1, H, hk, 128, 16, n, pages * 16 - 3, take=take, causal=True)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("B,hk,n,kv_len", [(4, 16, 2100, 2200), (9, 16, 500, 700), (32, 4, 1020, 1100), (5, 30, 520, 900)])
+def test_images_by_falling_length(nova, dh, B, hk, n, kv_len):
+    """More blocks than two rounds of the chip, none of them cut, and fewer, of which the last are; images of every length."""
+    assert B * hk * -(-n // 128) > 512
+    g = np.random.default_rng(B)
+    lens = [int(x) for x in g.integers(1, kv_len + 1, B)]
+    lens[1], lens[-1] = kv_len, 0
+    _check_some(nova, B, hk, hk, dh, 32, n, kv_len, lens, [min(n, x) for x in lens], causal=True)
+    _check_some(nova, B, hk, hk, dh, 32, n, kv_len, lens, None)
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("pages", [720, 732, 736, 900])
 def test_lists_about_what_leaves_room_for_a_second_workgroup(nova, dh, pages):
