@@ -563,7 +563,7 @@ int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* ca
  * have been appended:
  *   means   in/out DEVICE bf16 [pages, kv_heads, dh], 16-byte aligned: the mean of a page's rows that exist, taken in 64 bits, as the
  *           nearest w * 2^e, w a whole number (of two the even one), with one e per page and key head: the smallest, -100 <= e <= 100,
- *           for which no |w| passes 127 (from e = 100 on they stop there).  A page with a NaN or an infinity has means of NaN.
+ *           for which no mean passes 127 * 2^e (at e = 100 |w| stops at 127).  A page with a NaN or an infinity has means of NaN.
  *           Other pages' means are untouched.
  *
  * nova_paged_select chooses for every (query, key head) k of the pages it sees, by

@@ -104,7 +104,8 @@ def attention(q: np.ndarray, K: List[np.ndarray], V: List[np.ndarray], scale: fl
 
 
 def seven_bits(x: np.ndarray) -> np.ndarray:
-    """All of x as the nearest multiples w 2^e of one power of two, the smallest with |w| <= 127 everywhere, -100 <= e <= 100."""
+    """All of x as the nearest multiples w 2^e of one power of two, the smallest with |x| <= 127 2^e everywhere,
+    -100 <= e <= 100."""
     if not np.isfinite(x).all():
         return np.full_like(x, np.nan)
     e = -100

@@ -81,3 +81,8 @@ def test_pages_of_nan_come_behind_first_and_recent_ones():
     sel = lambda **kw: P.select(q, means, table, 16, [128], [1], True, **kw)[0, 0, 0].tolist()
     assert sel(first=1, recent=1, k=3) == [0, 2, 7] and sel(first=0, recent=2, k=2) == [6, 7] and sel(first=3, recent=1, k=4) == [0, 1, 2, 7]
     assert sel(first=1, recent=1, k=6) == [0, 2, 3, 4, 6, 7]
+
+
+def test_the_power_of_two_is_the_one_that_holds_the_largest_number_itself():
+    """127.25 is nearest to 127, and yet more than 127 ones: multiples of 2."""
+    assert P.seven_bits(np.array([127.25, 3.0, -1.4])).tolist() == [128.0, 4.0, -2.0] and P.seven_bits(np.array([-127.0, 1.4])).tolist() == [-127.0, 1.0]

@@ -203,3 +203,25 @@ def test_images_by_falling_length(nova, dh, B, hk, n, kv_len):
 @pytest.mark.parametrize("pages", [720, 732, 736, 900])
 def test_lists_about_what_leaves_room_for_a_second_workgroup(nova, dh, pages):
     _check_some(nova, 1, 16, 16, dh, 16, 600, pages * 16 - 5, take=16, causal=True)
+
+
+# ---- means ----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_largest_numbers_just_above_127_units(nova, dtype):
+    """127.25 takes a unit of 2, in means and in queries: a page of 100 beats one whose product with 127 would have won."""
+    rows = torch.zeros((2, 1, 16, 64))
+    rows[0, 0, ::2, 0], rows[0, 0, 1::2, 0], rows[0, 0, :, 1] = 127.0, 127.5, 3.0           # 127.25 on average
+    cache = PagedCache(*[rows.to(DTYPES[dtype]).cuda() for _ in range(2)])
+    means = torch.zeros((2, 1, 64), dtype=torch.bfloat16, device="cuda")
+    nova.paged_summarise(cache, _ints([[0, 1]]), means, 32, 32)
+    assert means[0, 0, :2].tolist() == [128.0, 4.0]
+    m = torch.zeros((2, 1, 64), dtype=torch.bfloat16, device="cuda")
+    m[0, 0, 0], m[1, 0, 1] = 1.0, 100.0
+    for scale in (1.0, 2.0 ** -9, 2.0 ** 40):
+        q = torch.zeros((1, 2, 1, 64))
+        q[0, 0, 0, :2], q[0, 1, 0, :2] = torch.tensor([127.25 if dtype == "f32" else 127.5, 1.4]) * scale, torch.tensor([126.5, 1.0]) * scale
+        q = q.to(DTYPES[dtype]).cuda()
+        chosen = torch.empty((1, 2, 1, 1), dtype=torch.int32, device="cuda")
+        nova.paged_select(m, _ints([[0, 1]]), 16, q, chosen, 32, first=0, recent=0)
+        assert np.array_equal(chosen.cpu().numpy(), P.select(_np(q), _np(m), np.array([[0, 1]]), 16, [32], [2], False, 0, 0, 1))
+        assert chosen.flatten().tolist() == [1, 0]
