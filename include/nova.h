@@ -531,7 +531,7 @@ int nova_paged_reserve(nova_ctx* ctx, void* stream, int B, int32_t* table, int p
 
 /* Rows k, v [B, n, kv_heads, dh] of the cache's dtype and any strides (rows of a projection's output, or the dense caches of
  * nova_pruned_block) to the slots [B, n]: one launch.  A slot outside [0, pages * page_rows) takes no row; two rows with one slot
- * leave 16-byte pieces of either.  B * n < 2^27. */
+ * leave 16-byte pieces of either.  k and v may be rows of the pools themselves, as long as no slot is one of them.  B * n < 2^27. */
 int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, int n, const nova_rows* k,
                       const nova_rows* v, const int32_t* slots);
 
@@ -560,7 +560,8 @@ int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* ca
  * Sparse attention: every query reads the pages it has chosen.
  *
  * nova_paged_summarise writes the means of the pages that the last n_per_row[b] rows (NULL: n) of every image lie in, after they
- * have been appended:
+ * have been appended.  An image that was cut back and gets no rows keeps the mean of its last page from before until that page is asked
+ * for: with n_per_row[b] of 1 or more.  A page that is last in several images' lists gets the mean over one of these images' rows:
  *   means   in/out DEVICE bf16 [pages, kv_heads, dh], 16-byte aligned: the mean of a page's rows that exist, taken in 64 bits, as the
  *           nearest w * 2^e, w a whole number (of two the even one), with one e per page and key head: the smallest, -100 <= e <= 100,
  *           for which no mean passes 127 * 2^e (at e = 100 |w| stops at 127).  A page with a NaN or an infinity has means of NaN.

@@ -789,7 +789,8 @@ class Nova:
 
     def paged_summarise(self, cache: PagedCache, table: torch.Tensor, means: torch.Tensor, n: int, kv_len: int,
                         n_per_row: Optional[torch.Tensor] = None, kv_len_per_row: Optional[torch.Tensor] = None):
-        """means [pages, kv_heads, dh] bf16: those of the pages that the images' last n rows lie in."""
+        """means [pages, kv_heads, dh] bf16: those of the pages that the images' last n rows lie in (of an image that was cut back and
+        gets no rows: n_per_row of 1 for its last page)."""
         c = self._pool(cache)
         B, dev, at = table.shape[0], self.device, self._table(table)
         rc = self.lib.nova_paged_summarise(

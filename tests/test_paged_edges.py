@@ -225,3 +225,39 @@ def test_largest_numbers_just_above_127_units(nova, dtype):
         nova.paged_select(m, _ints([[0, 1]]), 16, q, chosen, 32, first=0, recent=0)
         assert np.array_equal(chosen.cpu().numpy(), P.select(_np(q), _np(m), np.array([[0, 1]]), 16, [32], [2], False, 0, 0, 1))
         assert chosen.flatten().tolist() == [1, 0]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("p,keep", [(16, 37), (16, 32), (64, 1), (256, 300), (32, 0)])
+def test_means_of_images_that_were_cut_back(nova, dtype, p, keep):
+    """Without rows to come the last page's mean is the old one until it is asked for; other pages' never change."""
+    hk, dh, L = 2, 64, 310
+    cache, table = _fill(dtype, 1, hk, p, dh, [L], -(-L // p), 2)
+    tt, lens, count = _ints(table), _ints([L]), _ints([0])
+    means = torch.zeros((cache.k_pages.shape[0], hk, dh), dtype=torch.bfloat16, device="cuda")
+    nova.paged_summarise(cache, tt, means, L, L)
+    before = _np(means)
+    nova.paged_reserve(tt, p, 0, L, torch.zeros(cache.k_pages.shape[0], dtype=torch.int32, device="cuda"), count, lens, kv_len_per_row=lens,
+                       keep_per_row=_ints([keep]))
+    assert lens.item() == keep
+    nova.paged_summarise(cache, tt, means, 1, L, n_per_row=_ints([0]), kv_len_per_row=lens)
+    assert np.array_equal(_np(means), before)
+    nova.paged_summarise(cache, tt, means, 1, L, kv_len_per_row=lens)
+    want = P.summarise(_np(cache.k_pages), table, before, [keep], [1])
+    assert np.array_equal(_np(means), want) and np.array_equal(want, before) == (keep % p == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_rows_copied_within_the_pools(nova, dtype, dh):
+    """An image's last page written once more for another that begins alike: the sources are rows of the pools, no slot is one of them."""
+    p, hk, L = 32, 3, 80
+    cache, table = _fill(dtype, 1, hk, p, dh, [L], 3, 2)
+    before = [_np(t) for t in (cache.k_pages, cache.v_pages)]
+    last, spare = int(table[0, 2]), next(i for i in range(cache.k_pages.shape[0]) if i not in table)
+    slots = np.array([[spare * p + r for r in range(L - 2 * p)]])
+    k, v = (t[last:last + 1, :, :L - 2 * p].transpose(1, 2) for t in (cache.k_pages, cache.v_pages))
+    rows = [_np(k), _np(v)]
+    nova.paged_append(cache, k, v, _ints(slots))
+    for t, was, new in zip((cache.k_pages, cache.v_pages), before, rows):
+        assert np.array_equal(_np(t), P.append(was, new, slots), equal_nan=True)
