@@ -19,7 +19,7 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
 template <typename T> constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
 
 __device__ __forceinline__ bf16_t leading(float x) { return __builtin_bit_cast(bf16_t, (uint16_t)(__float_as_uint(x) >> 16)); }
-__device__ __forceinline__ void split(float x, bf16_t (&p)[1]) { p[0] = (bf16_t)x; }       // rounded: why, at many_kernel's head
+__device__ __forceinline__ void split(float x, bf16_t (&p)[1]) { p[0] = (bf16_t)x; }       // rounded: why, at the head of fourbit_attention.hip
 __device__ __forceinline__ void split(float x, bf16_t (&p)[3]) {
   p[0] = leading(x);
   const float r = x - (float)p[0];

@@ -2,8 +2,8 @@
 //
 // Page lists are integer work on a few numbers per image: every workgroup takes the prefix sums over all images for itself (what an
 // image gives back, what it needs), after which every entry of a list, slot and place of the stack of free pages has a
-// formula of its own and nothing waits for anything: a chain of dependent loads, 3 us for 256 images that get a row each, 10 and 3 for
-// 131 072 slots in two launches.  Appends are copies of whole lines, bound by HBM (134 MB, read with the stride of a joint projection, 22 us;
+// formula of its own and nothing waits for anything: a chain of dependent loads, 3 us for 256 images that get a row each; 131 072 slots
+// in two launches 10 us, four slots a thread one after the other with a chain of loads each, on 128 of the CUs, and 3.  Appends are copies of whole lines, bound by HBM (134 MB, read with the stride of a joint projection, 22 us;
 // a row each for 64 images 2.7).  Means: a wave per page and key head, sums in 64 bits, in which the sum of a page's rows is as good as
 // exact in any order (one page per image and key head 5 us: the latency of table, length and rows).
 #include <algorithm>
@@ -256,7 +256,8 @@ hipError_t launch_paged_reserve(hipStream_t st, const PagedReserve& r) {
   const uint32_t n_inv = div_inv(r.n);
   // One workgroup does it all in one launch; many entries are dealt to many, and a second launch writes what the first has read (us in one /
   // in two launches: 256 images of one new row 5.2 / 7.4, 4096 of one 15.7 / 29.9, 16 of 256 rows 6.6 / 8.5, 32 of 256 9.1 / 8.8, 64 of
-  // 2048 80 / 9.0).
+  // 2048 80 / 9.0).  With thousands of images the prefix sums, taken twice in two launches, count more than the entries do, which the rule
+  // does not look at: 2048 images of four rows 13.1 / 19.1, 4096 of two 17.9 / 30.9, in two launches both.
   const int64_t entries = std::max<int64_t>((int64_t)r.B * r.n, r.B);
   if (entries <= 4096) {
     reserve_kernel<1024><<<1, 1024, lds, st>>>(r, n_inv, 1, 1);

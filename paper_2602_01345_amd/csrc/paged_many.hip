@@ -9,7 +9,10 @@
 // MFMAs; a wave asks for priority while it issues MFMAs (below: 930 us; in the softmax instead 966, for the second product only 951; heads
 // of 64, 4 images of 1024 over 4096 172 / 199 / 172).  What bounds it is that and power: two images, 2048 queries behind 14 336 rows,
 // 32 heads of 128 on 8 (1.03 TFLOP) 930 to 1050 us by card, 1.0 to 1.1 PFLOP/s with the matrix cores busy 55 % of the cycles; 8 images of
-// 512, 36 heads of 64 (44 GFLOP) 65 to 70, where 32 exponentials stand next to 16 MFMAs.
+// 512, 36 heads of 64 (44 GFLOP) 65 to 73, MFMA busy 32 % of the cycles, where 32 exponentials stand next to 16 MFMAs.
+// Probabilities go into the second product as bf16, here and for bf16 in paged_few.hip and paged_chosen.hip: one rounding each (half a step,
+// 2^-8 at most) instead of two or three MFMAs for the parts of an fp32 number.  The sum they are divided by is that of the fp32 ones.  The
+// result's error against 64 bits goes from 1.7e-3 of it, which is its own rounding to bf16, to 1.8e-3 (the sizes above).
 // A weight of 0 times a value that is no number is NaN, so what a row does not see could show in its result.  A workgroup whose sums
 // end as anything but finite numbers goes over its tiles again, and takes those with such values in them key by key.
 #include <type_traits>

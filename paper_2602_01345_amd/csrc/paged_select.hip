@@ -7,8 +7,9 @@
 // A workgroup has up to 16 queries of one key head.  Scores on the matrix cores, 16 pages x 16 queries per MFMA, one after the other
 // for the heads that share the key head, their largest kept; as order-preserving 32-bit keys in LDS.  Then a wave per query: the
 // k-th largest key bit by bit, by counting, and the pages above it and the first of those that equal it, in ascending order.
-// What bounds it: the scalar units that count (two instructions per 64 keys and bit) for many queries, 1024 of 32 heads of 128 on 8 and 512
-// pages 32 us of which the scores' products are 3; for one the chain table, means, 32 bits, 13 us.  Registers are bounded so that two
+// What bounds it: issuing the count, per 64 keys and bit a comparison on the vector unit and a population count and an addition on the
+// scalar one, for many queries: 1024 of 32 heads of 128 on 8 and 512 pages 32 us, vector instructions in 51 % of the cycles, scalar ones in
+// 33 %, MFMA busy 6 %; for one the chain table, means, 32 bits, 13 us.  Registers are bounded so that two
 // workgroups share a CU, for some spills outside of the loops (bf16, heads of 128: 47 -> 37 us with the means; fp32 4000 queries, 16
 // heads of 128 171 -> 129, 1024 of 32 on 8 63 -> 62, but one token over four images 18.1 -> 21.3).
 #include <algorithm>
