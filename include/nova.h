@@ -572,8 +572,7 @@ int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* ca
  * w[h] being the query rounded as the means are, one e for all these heads (a query with a NaN or an infinity: zeros).  The `first`
  * pages from the front and the `recent` ones that end the rows the query sees are chosen in any case, then pages with means of NaN, the
  * lower ones first; of two scores alike the lower page's counts as higher.  These scores, of rounded numbers, are exact: what a query chooses
- * does not depend on what else
- * is in the call.
+ * does not depend on what else is in the call.
  *   chosen  out DEVICE int32 [B, n, kv_heads, k]: ordinals in the image's page list, ascending, then -1
  *   q       as in nova_paged_attention, of type dtype
  * 1 <= k <= 256, first + recent <= k, kv_len <= 16384 * page_rows, n < 2^23; with causal 1 recent >= 1 (the page a query lies in may hold rows
