@@ -547,8 +547,9 @@ int nova_paged_append(nova_ctx* ctx, void* stream, const nova_paged_cache* cache
  *              captured graphs among them, need one each.  0 bytes for sizes that the call refuses
  * No two of out, lse, the workspace (as far as it is needed) and the rows of q may share memory (out may lie between rows of q).
  * B * heads * n <= 2^30, B * kv_heads * ceil(n * heads / kv_heads / 16) < 2^24, B <= 65535.  Queries past n_per_row[b], and queries
- * that see no row, get zeros and lse = -inf; one whose scores are all -inf NaN and lse = -inf.  A row that a query does not see has no part in its result, whatever its key and value are (NaN among them).  NOVA_F32: products of fp32
- * numbers, summed in fp32; NOVA_BF16: probabilities are rounded to bf16 in front of the second product.
+ * that see no row, get zeros and lse = -inf; one whose scores are all -inf gets NaN and lse = -inf.  A row that a query does not see
+ * has no part in its result, whatever its key and value are (NaN among them).  NOVA_F32: products of fp32 numbers, summed in fp32;
+ * NOVA_BF16: probabilities are rounded to bf16 in front of the second product.
  */
 size_t nova_paged_attention_workspace_bytes(const nova_paged_cache* cache, int B, int heads, int n, int kv_len);
 int nova_paged_attention(nova_ctx* ctx, void* stream, const nova_paged_cache* cache, int B, const int32_t* table, int pitch,

@@ -22,7 +22,7 @@ constexpr int kWaves = 8;
 constexpr int kHeads = 4;                // heads whose queries are held in registers at a time
 constexpr int kAhead = 2;                // groups of 16 pages whose means a wave asks for at a time
 constexpr int kMostKeys = 32;            // keys a lane holds while the k-th largest is looked for
-constexpr uint32_t kTaken = 0xFFFFFFFFu; // key of a page that is taken whatever its score (`first`, `recent`); 0: one that the query does not see
+constexpr uint32_t kTaken = 0xFFFFFFFFu; // key of a `first` or `recent` page, whatever its score; 0: of one that the query does not see
 constexpr uint32_t kOdd = 0xFFFFFFFEu;   // of a page with a mean of NaN: in front of every score, behind those that are taken
 
 struct SelectArgs {
