@@ -4,8 +4,8 @@
 // image gives back, what it needs), after which every entry of a list, slot and place of the stack of free pages has a
 // formula of its own and nothing waits for anything: a chain of dependent loads, 3 us for 256 images that get a row each; 131 072 slots
 // in two launches 10 us, four slots a thread one after the other with a chain of loads each, on 128 of the CUs, and 3.  Appends
-// are copies of whole lines, bound by HBM (134 MB, read with the stride of a joint projection, 22 us; a row each for 64 images 2.7).  Means: a wave per page and key head, sums in 64 bits, in which the sum of a page's rows is as good as
-// exact in any order (one page per image and key head 5 us: the latency of table, length and rows).
+// are copies of whole lines, bound by HBM (134 MB, read with the stride of a joint projection, 22 us; a row each for 64 images 2.7).  Means: a
+// wave per page and key head, sums in 64 bits, in which the sum of a page's rows is as good as exact in any order (one page per image and key head 5 us: the latency of table, length and rows).
 #include <algorithm>
 
 #include "paged.h"
